@@ -23,6 +23,10 @@
  *   ld_merge_sparse_adam Recovery loop of Algorithm 1 with the paper's own update:
  *                        sparse diffs decompressed and merged through Adam into
  *                        model and optimizer state.
+ * what stands between a model's tokens and those gradients: ld_embed_lookup and
+ * ld_embed_grad (the token embedding, the largest tensor of the models that are
+ * checkpointed, and its gradient), ld_grad_norm, ld_clip_grads and
+ * ld_clip_grad_norm (the norm over all gradients of a step, and clipping by it);
  * and two helpers of the recovery path: ld_merge_sparse_from_host (the merge fed
  * from page-locked host memory, copies and merges pipelined) and ld_check_diff
  * (counts what is wrong with a diff before it is merged).
@@ -417,6 +421,103 @@ ld_status ld_combine_sparse_strategy(const int32_t* const* idx, const float* con
                             int32_t* out_idx, float* out_val, int64_t out_cap, int64_t* out_count,
                             void* workspace, size_t workspace_bytes, ld_stream stream,
                             int32_t strategy);
+
+/* ------------------------------------------------------------------------
+ * Element types of the operators below.  Arrays of these need no more than their
+ * element's alignment (whole 16 bytes are faster).
+ */
+#define LD_F32  0
+#define LD_BF16 1
+#define LD_F16  2
+#define LD_I32  0
+#define LD_I64  1
+
+/* ------------------------------------------------------------------------
+ * ld_grad_norm - sum of squares and 2-norm of a step's gradient, over many
+ * tensors.  Squares and sums are 64 bits wide, added in an order that only the
+ * sizes decide: the same input gives the same bits.
+ *   *sumsq = (accumulate ? *sumsq : 0) + sum over all elements of x^2
+ *   *norm  = fl32(sqrt(*sumsq))
+ * A step whose gradients have several types, or lie on several GPUs, calls it once
+ * for each type with accumulate, adds up the GPUs' sums, and clips by the total.
+ *
+ *   grad       host array of n_tensors dev pointers to elements of `dtype`
+ *   n_elems    host [n_tensors] int64, 0 <= n_elems[t], 2^41 in all
+ *   n_tensors  0 <= n_tensors <= LD_MAX_TENSORS
+ *   dtype      LD_F32, LD_BF16 or LD_F16
+ *   sumsq      dev, one double, 8-byte aligned
+ *   norm       dev, one float, or NULL
+ *   workspace  dev, 256-byte aligned, ld_grad_norm_workspace() bytes
+ *
+ * ld_clip_grads - scales the tensors down to a norm of max_norm:
+ *   out[t][i] = round(fl32(grad[t][i] * f)),  f = fl32(max_norm / sqrt(*sumsq)) where
+ *   sqrt(*sumsq) > max_norm, else 1
+ * A sum that is infinite or NaN scales nothing (f = 1); the caller finds that in the
+ * norm.
+ *   out        host array of n_tensors dev pointers to elements of `out_dtype`; each
+ *              is the tensor itself (in place; then out_dtype = dtype) or overlaps no
+ *              tensor of the call
+ *   max_norm   >= 0, may be infinite
+ *
+ * ld_clip_grad_norm - both in one call: *norm is the norm before clipping.
+ * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_WORKSPACE, LD_ERR_HIP.
+ */
+#define LD_MAX_TENSORS (1 << 20)
+size_t    ld_grad_norm_workspace(int32_t n_tensors);
+ld_status ld_grad_norm(const void* const* grad, const int64_t* n_elems, int32_t n_tensors, int32_t dtype,
+                       int32_t accumulate, double* sumsq, float* norm /* may be NULL */,
+                       void* workspace, size_t workspace_bytes, ld_stream stream);
+ld_status ld_clip_grads(const void* const* grad, void* const* out, const int64_t* n_elems, int32_t n_tensors,
+                        int32_t dtype, int32_t out_dtype, const double* sumsq, float max_norm, ld_stream stream);
+ld_status ld_clip_grad_norm(const void* const* grad, void* const* out, const int64_t* n_elems, int32_t n_tensors,
+                            int32_t dtype, int32_t out_dtype, float max_norm, float* norm,
+                            void* workspace, size_t workspace_bytes, ld_stream stream);
+
+/* ------------------------------------------------------------------------
+ * ld_embed_lookup - the embedding of T tokens, scaled, with a second table's rows
+ * (positions) added:
+ *   out[t][c] = round(fl32(scale * table[ids[t]][c] + pos_table[positions[t]][c]))
+ * (one fused multiply-add in 32 bits; without a second table one product).  An id or
+ * position outside its table counts as a row of zeros: tokens that are padding may
+ * be -1.
+ *
+ *   table      dev [V] rows of d elements of `dtype`, table_stride >= 0 elements apart
+ *   pos_table  dev [P] rows of d elements of `dtype`, pos_stride >= 0 apart, or NULL
+ *   ids        dev [T] of `id_dtype` (LD_I32 or LD_I64)
+ *   positions  dev [T] of `id_dtype`; read only with a pos_table
+ *   out        dev [T] rows of d elements of `out_dtype`, out_stride >= d apart
+ *   T, V, P, d >= 0 (T = 0 or d = 0 enqueues nothing)
+ * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_HIP.
+ */
+ld_status ld_embed_lookup(const void* table, int64_t V, int64_t table_stride,
+                          const void* pos_table, int64_t P, int64_t pos_stride, int32_t dtype,
+                          const void* ids, const void* positions, int32_t id_dtype, int64_t T, int32_t d,
+                          float scale, void* out, int64_t out_stride, int32_t out_dtype, ld_stream stream);
+
+/* ------------------------------------------------------------------------
+ * ld_embed_grad - gradient of a lookup by its table:
+ *   grad[v][c] = round(fl32(scale * S + (accumulate ? grad[v][c] : 0))),
+ *   S = sum of dout[t][c] over the tokens t with ids[t] = v, in 32 bits
+ * (one fused multiply-add).  The tokens are sorted by id, stably; S is added in an
+ * order that only the ids and sizes decide, without atomics: the same input gives the
+ * same bits.  Ids outside [0, V) are passed over.  Without accumulate rows that no token
+ * names become zero; with it they are not touched.  The gradient of a position table is
+ * the same call with the positions as ids and scale 1.
+ *
+ *   dout       dev [T] rows of d elements of `dtype`, dout_stride >= 0 elements apart (0: one row for all)
+ *   ids        dev [T] of `id_dtype` (LD_I32 or LD_I64)
+ *   grad       dev [V] rows of d elements of `grad_dtype`, grad_stride >= d apart; overlaps
+ *              neither dout nor ids
+ *   T          0 <= T <= LD_MAX_TOKENS;  V  0 <= V < 2^31 - 1;  d >= 0
+ *   workspace  dev, 256-byte aligned, ld_embed_grad_workspace() bytes
+ * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_WORKSPACE, LD_ERR_HIP.
+ */
+#define LD_MAX_TOKENS (1 << 24)
+size_t    ld_embed_grad_workspace(int64_t T, int64_t V, int32_t d);
+ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_t dtype,
+                        const void* ids, int32_t id_dtype, int64_t T, int32_t d, float scale,
+                        void* grad, int64_t V, int64_t grad_stride, int32_t grad_dtype, int32_t accumulate,
+                        void* workspace, size_t workspace_bytes, ld_stream stream);
 
 /* ------------------------------------------------------------------------
  * Checkpointing configuration model (Sec. V-C).  Host arithmetic only; nothing is

@@ -127,6 +127,20 @@ def load() -> ctypes.CDLL:
     lib.ld_combine_sparse.restype = i32
     lib.ld_combine_sparse_strategy.argtypes = lib.ld_combine_sparse.argtypes + [i32]
     lib.ld_combine_sparse_strategy.restype = i32
+    lib.ld_grad_norm_workspace.argtypes = [i32]
+    lib.ld_grad_norm_workspace.restype = sz
+    lib.ld_grad_norm.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+    lib.ld_grad_norm.restype = i32
+    lib.ld_clip_grads.argtypes = [vp, vp, vp, i32, i32, i32, vp, f32, vp]
+    lib.ld_clip_grads.restype = i32
+    lib.ld_clip_grad_norm.argtypes = [vp, vp, vp, i32, i32, i32, f32, vp, vp, sz, vp]
+    lib.ld_clip_grad_norm.restype = i32
+    lib.ld_embed_lookup.argtypes = [vp, i64, i64, vp, i64, i64, i32, vp, vp, i32, i64, i32, f32, vp, i64, i32, vp]
+    lib.ld_embed_lookup.restype = i32
+    lib.ld_embed_grad_workspace.argtypes = [i64, i64, i32]
+    lib.ld_embed_grad_workspace.restype = sz
+    lib.ld_embed_grad.argtypes = [vp, i64, i32, vp, i32, i64, i32, f32, vp, i64, i64, i32, i32, vp, sz, vp]
+    lib.ld_embed_grad.restype = i32
     dbl = ctypes.c_double
     lib.ld_config_wasted_time.argtypes = [vp, dbl, dbl, dbl, dbl]
     lib.ld_config_wasted_time.restype = dbl
@@ -505,6 +519,169 @@ def ld_combine_sparse(idx: Sequence[torch.Tensor], val: Sequence[torch.Tensor], 
 
 def ld_combine_sparse_workspace(n: int, N: int) -> int:
     return int(load().ld_combine_sparse_workspace(int(n), int(N)))
+
+
+_ELEM = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # LD_F32, LD_BF16, LD_F16
+_ID = {torch.int32: 0, torch.int64: 1}                           # LD_I32, LD_I64
+
+
+def _elem(t: torch.Tensor, name: str) -> int:
+    code = _ELEM.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: expected float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _lists(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]]):
+    """Tables and element types of a step's gradients and of where they go (the same, in place); None where the list is empty."""
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError("grads and outs differ in length")
+    if not len(grads):
+        return None
+    g, gt = _Table(grads, grads[0].dtype), _elem(grads[0], "grads")
+    if outs is None:
+        return g, g, gt, gt
+    o, ot = _Table(outs, outs[0].dtype), _elem(outs[0], "outs")
+    if g.sizes != o.sizes:
+        raise ValueError("grads[t] and outs[t] differ in size")
+    return g, o, gt, ot
+
+
+def ld_grad_norm(grads: Sequence[torch.Tensor], sumsq: Optional[torch.Tensor] = None, norm: Optional[torch.Tensor] = None,
+                 accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
+                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(sumsq float64[1], norm float32[1]) over all elements of the tensors, which share one of the types float32,
+    bfloat16 and float16. With `accumulate` the squares are added to what `sumsq` holds."""
+    lib = load()
+    if accumulate and sumsq is None:
+        raise ValueError("accumulate needs the sumsq to add to")
+    got = _lists(grads, None)
+    dev = grads[0].device if got else sumsq.device if sumsq is not None else torch.device("cuda", torch.cuda.current_device())
+    if sumsq is None:
+        sumsq = _record(torch.empty(1, dtype=torch.float64, device=dev), stream)
+    if norm is None:
+        norm = _record(torch.empty(1, dtype=torch.float32, device=dev), stream)
+    _one_device(sumsq, (norm, workspace), *(got[:1] if got else ()))
+    gp, sizes, gt = (got[0].checked("grads"), got[0].sizes, got[2]) if got else (None, None, 0)
+    if sumsq.numel() < 1 or norm.numel() < 1:
+        raise ValueError("sumsq and norm need an element each")
+    if workspace is None:
+        workspace = _scratch(lib.ld_grad_norm_workspace(len(grads)), dev, stream)
+    st = lib.ld_grad_norm(gp, sizes, len(grads), gt, int(accumulate), _dev(sumsq, torch.float64, "sumsq"),
+                          _dev(norm, torch.float32, "norm"), _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+                          _stream(stream))
+    _check("ld_grad_norm", st)
+    return sumsq, norm
+
+
+def ld_clip_grads(grads: Sequence[torch.Tensor], sumsq: torch.Tensor, max_norm: float,
+                  outs: Optional[Sequence[torch.Tensor]] = None, stream=None) -> None:
+    """Scales the tensors by max_norm / sqrt(sumsq) where that root is larger than max_norm: in place, or into
+    `outs` (of one type, which may be another; copied unscaled where the norm is not larger, or not finite)."""
+    got = _lists(grads, outs)
+    if sumsq.numel() < 1:
+        raise ValueError("sumsq needs an element")
+    if got is None:
+        return
+    g, o, gt, ot = got
+    _one_device(sumsq, (), g, o)
+    st = load().ld_clip_grads(g.checked("grads"), o.checked("outs"), g.sizes, len(grads), gt, ot,
+                              _dev(sumsq, torch.float64, "sumsq"), ctypes.c_float(max_norm), _stream(stream))
+    _check("ld_clip_grads", st)
+
+
+def ld_clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, outs: Optional[Sequence[torch.Tensor]] = None,
+                      norm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+    """ld_grad_norm and ld_clip_grads in one call. Returns the norm before clipping, a float32[1] on the device; a step
+    whose norm is not finite is left unscaled, and the caller sees it there."""
+    lib = load()
+    got = _lists(grads, outs)
+    dev = grads[0].device if got else norm.device if norm is not None else torch.device("cuda", torch.cuda.current_device())
+    if norm is None:
+        norm = _record(torch.empty(1, dtype=torch.float32, device=dev), stream)
+    _one_device(norm, (workspace,), *(got[:2] if got else ()))
+    gp, op, sizes, gt, ot = (got[0].checked("grads"), got[1].checked("outs"), got[0].sizes, got[2], got[3]) if got else (None, None, None, 0, 0)
+    if norm.numel() < 1:
+        raise ValueError("norm needs an element")
+    if workspace is None:
+        workspace = _scratch(lib.ld_grad_norm_workspace(len(grads)), dev, stream)
+    st = lib.ld_clip_grad_norm(gp, op, sizes, len(grads), gt, ot, ctypes.c_float(max_norm), _dev(norm, torch.float32, "norm"),
+                               _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check("ld_clip_grad_norm", st)
+    return norm
+
+
+def _rows(t: torch.Tensor, name: str, written: bool = False) -> Tuple[int, int, int]:
+    """Address, rows and row stride of a 2-D tensor on the GPU whose rows are contiguous (and apart, where they are written)."""
+    rows, width = t.shape if t.dim() == 2 else (0, 0)
+    if not t.is_cuda or t.dim() != 2 or (width > 1 and t.stride(1) != 1):
+        raise TypeError(f"{name}: expected a 2-D tensor on the GPU with contiguous rows")
+    stride = t.stride(0) if rows > 1 else width  # a view of one row keeps the stride of what it was taken from
+    if written and stride < width:
+        raise ValueError(f"{name}: rows overlap")
+    return t.data_ptr(), rows, stride
+
+
+def _ids(t: torch.Tensor, name: str) -> int:
+    code = _ID.get(t.dtype)
+    if code is None or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous int32 or int64 tensor on the GPU")
+    return code
+
+
+def ld_embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, pos_table: Optional[torch.Tensor] = None,
+                    positions: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """scale * table[ids] (+ pos_table[positions]) in `out` or a new tensor of shape ids.shape + (d,) and type
+    `out_dtype` (the table's unless given). Rows outside their table count as zeros. The tables, and an `out` of two
+    dimensions, may have any row stride."""
+    if (pos_table is None) != (positions is None):
+        raise ValueError("pos_table and positions go together")
+    d, T = table.shape[-1], ids.numel()
+    if positions is not None and (positions.numel() != T or positions.dtype != ids.dtype):
+        raise ValueError("positions must be as many as ids, and of their type")
+    if pos_table is not None and (pos_table.shape[-1] != d or pos_table.dtype != table.dtype):
+        raise ValueError("table and pos_table differ in width or type")
+    _same_device(table, ids, pos_table, positions, out)
+    code = _elem(table, "table")
+    tp, V, ts = _rows(table, "table")
+    pp, P, ps = _rows(pos_table, "pos_table") if pos_table is not None else (None, 0, 0)
+    it = _ids(ids, "ids")
+    if positions is not None:
+        _ids(positions, "positions")
+    if out is None:
+        out = _record(torch.empty(*ids.shape, d, dtype=out_dtype or table.dtype, device=table.device), stream)
+    elif out.numel() != T * d or out.shape[-1] != d or (out_dtype is not None and out.dtype != out_dtype):
+        raise ValueError("out differs in shape or type from what the lookup gives")
+    op, _, os_ = _rows(out if out.dim() == 2 else out.view(T, d), "out", written=True)
+    st = load().ld_embed_lookup(tp, V, ts, pp, P, ps, code, ids.data_ptr(), positions.data_ptr() if positions is not None else None,
+                                it, T, d, ctypes.c_float(scale), op, os_, _elem(out, "out"), _stream(stream))
+    _check("ld_embed_lookup", st)
+    return out
+
+
+def ld_embed_grad_workspace(T: int, V: int, d: int) -> int:
+    return int(load().ld_embed_grad_workspace(int(T), int(V), int(d)))
+
+
+def ld_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gradient of ld_embed_lookup by its table from that of its output, `dout` (ids.shape + (d,), or [T, d] with any
+    row stride): written to `grad` [V, d], or with `accumulate` added to it. Deterministic."""
+    lib = load()
+    T, d = ids.numel(), grad.shape[-1]
+    if dout.shape[-1] != d or dout.numel() != T * d:
+        raise ValueError("dout must have a row of grad's width for every id")
+    _same_device(dout, ids, grad, workspace)
+    gp, V, gs = _rows(grad, "grad", written=True)
+    dp, _, ds = _rows(dout if dout.dim() == 2 else dout.view(T, d), "dout")
+    it, dt, gt = _ids(ids, "ids"), _elem(dout, "dout"), _elem(grad, "grad")
+    if workspace is None:
+        workspace = _scratch(lib.ld_embed_grad_workspace(T, V, d), grad.device, stream)
+    st = lib.ld_embed_grad(dp, ds, dt, ids.data_ptr(), it, T, d, ctypes.c_float(scale), gp, V, gs, gt, int(accumulate),
+                           _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check("ld_embed_grad", st)
 
 
 class ConfigParams(ctypes.Structure):
