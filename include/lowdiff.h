@@ -486,9 +486,10 @@ ld_status ld_clip_grad_norm(const void* const* grad, void* const* out, const int
  *   ids        dev [T] of `id_dtype` (LD_I32 or LD_I64)
  *   positions  dev [T] of `id_dtype`; read only with a pos_table
  *   out        dev [T] rows of d elements of `out_dtype`, out_stride >= d apart
- *   T, V, P, d >= 0 (T = 0 or d = 0 enqueues nothing)
+ *   T, V, P >= 0;  0 <= d <= LD_MAX_WIDTH  (T = 0 or d = 0 enqueues nothing)
  * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_HIP.
  */
+#define LD_MAX_WIDTH (1 << 20)
 ld_status ld_embed_lookup(const void* table, int64_t V, int64_t table_stride,
                           const void* pos_table, int64_t P, int64_t pos_stride, int32_t dtype,
                           const void* ids, const void* positions, int32_t id_dtype, int64_t T, int32_t d,
@@ -508,7 +509,7 @@ ld_status ld_embed_lookup(const void* table, int64_t V, int64_t table_stride,
  *   ids        dev [T] of `id_dtype` (LD_I32 or LD_I64)
  *   grad       dev [V] rows of d elements of `grad_dtype`, grad_stride >= d apart; overlaps
  *              neither dout nor ids
- *   T          0 <= T <= LD_MAX_TOKENS;  V  0 <= V < 2^31 - 1;  d >= 0
+ *   T          0 <= T <= LD_MAX_TOKENS;  V  0 <= V < 2^31 - 1;  0 <= d <= LD_MAX_WIDTH
  *   workspace  dev, 256-byte aligned, ld_embed_grad_workspace() bytes
  * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_WORKSPACE, LD_ERR_HIP.
  */

@@ -83,7 +83,7 @@ extern "C" ld_status ld_embed_lookup(const void* table, int64_t V, int64_t table
                                      int64_t pos_stride, int32_t dtype, const void* ids, const void* positions, int32_t id_dtype,
                                      int64_t T, int32_t d, float scale, void* out, int64_t out_stride, int32_t out_dtype,
                                      ld_stream stream) {
-    if (V < 0 || T < 0 || d < 0 || table_stride < 0 || out_stride < d || !ld_known_type(dtype) || !ld_known_type(out_dtype) ||
+    if (V < 0 || T < 0 || d < 0 || d > LD_MAX_WIDTH || table_stride < 0 || out_stride < d || !ld_known_type(dtype) || !ld_known_type(out_dtype) ||
         (id_dtype != LD_I32 && id_dtype != LD_I64))
         return LD_ERR_RANGE;
     if (pos_table && (P < 0 || pos_stride < 0)) return LD_ERR_RANGE;

@@ -142,13 +142,26 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a) {
 
 // ------------------------------------------------------------------- rows
 
+// The sorted tokens are cut into chunks of equal size, a wave for each chunk and block of columns. It adds up run after run of
+// equal ids; a run inside the chunk is written to its row at once, one that goes on in the next chunk (or came from the one
+// before) leaves a partial sum, and k_join adds those up. Rows that no token names are cleared by workgroups of the same launch.
+constexpr int kRowThreads = 256;
+constexpr int kRowWaves = kRowThreads / LD_WAVE;
+constexpr int kAhead = 8;         // tokens whose rows a wave loads before it adds the first
+constexpr int kMostChunk = 32;    // a chunk's keys and the one on either side fit a wave
+constexpr int kClearRows = 16;    // rows that a clearing workgroup looks after
+constexpr int kJoinThreads = 1024;
+
 struct RowArgs {
     const void* dout;
     const uint32_t* keys;   // sorted
     const uint32_t* at;     // the tokens in that order
     void* grad;
-    int64_t dout_stride, grad_stride;
+    float* part;            // [2 * chunks] rows of part_stride: a chunk's sum of the run that came from the one before, and of the one that goes on
+    int64_t dout_stride, grad_stride, part_stride;
     int32_t T, V, d;
+    int32_t chunk, blocks;  // tokens of a chunk; blocks of columns
+    int32_t adding, clearing;  // workgroups of each kind
     float scale;
     int32_t accumulate;
 };
@@ -168,27 +181,158 @@ __device__ __forceinline__ int32_t lower_bound(const uint32_t* keys, int32_t n, 
     return lo;
 }
 
-// A workgroup per row of the table.
-template <int DT, int GT>
-__global__ __launch_bounds__(256) void k_rows(RowArgs a) {
-    const uint32_t v = blockIdx.x;
-    const int32_t from = lower_bound(a.keys, a.T, v), to = lower_bound(a.keys, a.T, v + 1);
-    if (from == to && a.accumulate) return;
-    const typename LdElem<DT>::type* dout = static_cast<const typename LdElem<DT>::type*>(a.dout);
-    typename LdElem<GT>::type* grad = static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(v) * a.grad_stride;
-    for (int32_t c = threadIdx.x; c < a.d; c += 256) {
-        float sum = 0.0f;
-        for (int32_t i = from; i < to; ++i) sum += static_cast<float>(dout[a.at[i] * a.dout_stride + c]);
-        grad[c] = static_cast<typename LdElem<GT>::type>(a.accumulate ? __fmaf_rn(a.scale, sum, static_cast<float>(grad[c])) : a.scale * sum);
+// The first `have` of N elements from p on, the others zero; all N in one access where they are there.
+template <int DT, int N>
+__device__ __forceinline__ typename LdVec<DT, N>::type load_some(const typename LdElem<DT>::type* p, int32_t have) {
+    typename LdVec<DT, N>::type x = typename LdVec<DT, N>::type(0);
+    if (have >= N) return *reinterpret_cast<const typename LdVec<DT, N>::type*>(p);
+#pragma unroll
+    for (int e = 0; e < N - 1; ++e)
+        if (e < have) x[e] = p[e];
+    return x;
+}
+
+template <int DT, int N>
+__device__ __forceinline__ void store_some(typename LdElem<DT>::type* p, int32_t have, typename LdVec<DT, N>::type x) {
+    if (have >= N) {
+        *reinterpret_cast<typename LdVec<DT, N>::type*>(p) = x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N - 1; ++e)
+            if (e < have) p[e] = x[e];
     }
+}
+
+// A finished sum to its row.
+template <int GT, int N>
+__device__ __forceinline__ void write_row(const RowArgs& a, uint32_t v, int32_t column, int32_t have, typename LdVec<GT, N>::wide sum) {
+    typename LdElem<GT>::type* row = static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(v) * a.grad_stride + column;
+    if (a.accumulate) {
+        const typename LdVec<GT, N>::wide old = LdVec<GT, N>::widen(load_some<GT, N>(row, have));
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] = __fmaf_rn(a.scale, sum[e], old[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] = a.scale * sum[e];
+    }
+    store_some<GT, N>(row, have, LdVec<GT, N>::narrow(sum));
+}
+
+template <int GT>
+__device__ void clear_rows(const RowArgs& a, int32_t first) {
+    constexpr int N = GT == LD_F32 ? 4 : 8;
+    __shared__ uint32_t named;
+    if (threadIdx.x < LD_WAVE) {
+        const int32_t v = first + static_cast<int32_t>(threadIdx.x);
+        bool is = false;
+        if (threadIdx.x < kClearRows && v < a.V) {
+            const int32_t i = lower_bound(a.keys, a.T, v);
+            is = i < a.T && a.keys[i] == static_cast<uint32_t>(v);
+        }
+        const uint64_t all = __ballot(is);
+        if (threadIdx.x == 0) named = static_cast<uint32_t>(all);
+    }
+    __syncthreads();
+    for (int32_t r = threadIdx.x / LD_WAVE; r < kClearRows && first + r < a.V; r += kRowWaves) {
+        if (named >> r & 1) continue;
+        typename LdElem<GT>::type* row = static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(first + r) * a.grad_stride;
+        for (int32_t c = ld_lane() * N; c < a.d; c += LD_WAVE * N) store_some<GT, N>(row + c, a.d - c, typename LdVec<GT, N>::type(0));
+    }
+}
+
+template <int DT, int GT>
+__global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
+    constexpr int N = DT == LD_F32 ? 4 : 8;
+    typedef LdVec<DT, N> X;
+    int32_t block = blockIdx.x;
+    if (a.clearing > 0) {  // the two kinds mixed evenly
+        const int64_t all = a.adding + a.clearing;
+        const int32_t before = static_cast<int32_t>(static_cast<int64_t>(block) * a.clearing / all);
+        if (static_cast<int32_t>(static_cast<int64_t>(block + 1) * a.clearing / all) > before) {
+            clear_rows<GT>(a, before * kClearRows);
+            return;
+        }
+        block -= before;
+    }
+    const int32_t unit = __builtin_amdgcn_readfirstlane(block * kRowWaves + static_cast<int32_t>(threadIdx.x / LD_WAVE));
+    const int32_t c = unit / a.blocks, column = ((unit - c * a.blocks) * LD_WAVE + ld_lane()) * N, have = a.d - column;
+    const int32_t from = c * a.chunk;
+    if (from >= a.T) return;
+    // lane l holds the key of token from - 1 + l; none is V
+    const int32_t i = from - 1 + ld_lane();
+    const bool in = i >= 0 && i < a.T && ld_lane() <= a.chunk + 1;
+    const uint32_t key = in ? a.keys[i] : a.V, at = in ? a.at[i] : 0;
+    const auto key_of = [&](int32_t j) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key), j)); };
+    uint32_t run = key_of(1);
+    if (run >= static_cast<uint32_t>(a.V)) return;
+    const typename X::elem* dout = static_cast<const typename X::elem*>(a.dout) + column;
+    float* part = a.part + 2 * static_cast<int64_t>(c) * a.part_stride + column;
+    const bool came = key_of(0) == run;
+    bool first = true;
+    typename X::wide sum = typename X::wide(0.0f);
+    for (int32_t j0 = 1; j0 <= a.chunk; j0 += kAhead) {
+        typename X::type x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t t = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), j0 + u));
+            x[u] = typename X::type(0);
+            if (key_of(j0 + u) < static_cast<uint32_t>(a.V) && have > 0) x[u] = load_some<DT, N>(dout + t * a.dout_stride, have);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t k = key_of(j0 + u);
+            if (k != run) {
+                if (run < static_cast<uint32_t>(a.V) && have > 0) {
+                    if (first && came) store_some<LD_F32, N>(part, have, sum);
+                    else write_row<GT, N>(a, run, column, have, sum);
+                }
+                first = false;
+                run = k;
+                sum = typename X::wide(0.0f);
+            }
+            sum += X::widen(x[u]);
+        }
+    }
+    if (run >= static_cast<uint32_t>(a.V) || have <= 0) return;
+    if (first && came) store_some<LD_F32, N>(part, have, sum);
+    else if (key_of(a.chunk + 1) == run) store_some<LD_F32, N>(part + a.part_stride, have, sum);
+    else write_row<GT, N>(a, run, column, have, sum);
+}
+
+// Adds up the partial sums of the run that begins in a chunk and does not end there, in their order: a workgroup per chunk and
+// 256 columns, its waves taking partial sums in turn.
+template <int GT>
+__global__ __launch_bounds__(kJoinThreads) void k_join(RowArgs a) {
+    constexpr int N = 4, kWaves = kJoinThreads / LD_WAVE;
+    __shared__ ld_f32x4 sh[kWaves][LD_WAVE];
+    const int32_t c = blockIdx.x, from = c * a.chunk, next = from + a.chunk;
+    if (next >= a.T) return;
+    const uint32_t v = a.keys[next];
+    if (v >= static_cast<uint32_t>(a.V) || a.keys[next - 1] != v || (from > 0 && a.keys[from - 1] == v)) return;
+    const int32_t end = lower_bound(a.keys, a.T, v + 1), last = (end - 1) / a.chunk;
+    const int32_t column = (blockIdx.y * LD_WAVE + ld_lane()) * N, have = a.d - column, wave = threadIdx.x / LD_WAVE;
+    ld_f32x4 sum = ld_f32x4(0.0f);
+    if (have > 0) {
+        for (int32_t j = c + wave; j <= last; j += kWaves)
+            sum += load_some<LD_F32, N>(a.part + (2 * static_cast<int64_t>(j) + (j == c)) * a.part_stride + column, have);
+    }
+    sh[wave][ld_lane()] = sum;
+    __syncthreads();
+    if (wave > 0 || have <= 0) return;
+    sum = sh[0][ld_lane()];
+    const int32_t waves = last - c + 1 < kWaves ? last - c + 1 : kWaves;
+    for (int32_t w = 1; w < waves; ++w) sum += sh[w][ld_lane()];
+    write_row<GT, N>(a, v, column, have, sum);
 }
 
 struct Layout {
     int32_t passes, bits, tiles;
-    size_t keys, at, counts, bytes;  // byte offsets: two buffers each of keys and tokens
+    int32_t chunk, chunks;
+    int64_t part_stride;
+    size_t keys, at, counts, part, bytes;  // byte offsets: two buffers each of keys and tokens
 };
 
-Layout layout_of(int64_t T, int64_t V) {
+Layout layout_of(int64_t T, int64_t V, int32_t d) {
     Layout l;
     int32_t all = 1;
     while ((V >> all) != 0) ++all;  // bits of the keys 0 .. V
@@ -199,18 +343,22 @@ Layout layout_of(int64_t T, int64_t V) {
     l.keys = 0;
     l.at = 2 * list;
     l.counts = 4 * list;
-    l.bytes = ld_round_up(l.counts + (static_cast<size_t>(l.tiles) << l.bits) * 4, 256);
+    l.part = ld_round_up(l.counts + (static_cast<size_t>(l.tiles) << l.bits) * 4, 256);
+    l.chunk = kMostChunk;
+    l.chunks = static_cast<int32_t>((T + l.chunk - 1) / l.chunk);
+    l.part_stride = (static_cast<int64_t>(d) + 3) / 4 * 4;
+    l.bytes = ld_round_up(l.part + 2 * static_cast<size_t>(l.chunks) * l.part_stride * 4, 256);
     return l;
 }
 
 bool sizes_fit(int64_t T, int64_t V, int32_t d) {
-    return T >= 0 && V >= 0 && d >= 0 && T <= LD_MAX_TOKENS && V < INT32_MAX;
+    return T >= 0 && V >= 0 && d >= 0 && d <= LD_MAX_WIDTH && T <= LD_MAX_TOKENS && V < INT32_MAX;
 }
 
 }  // namespace
 
 extern "C" size_t ld_embed_grad_workspace(int64_t T, int64_t V, int32_t d) {
-    return sizes_fit(T, V, d) ? layout_of(T, V).bytes : 0;
+    return sizes_fit(T, V, d) ? layout_of(T, V, d).bytes : 0;
 }
 
 extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_t dtype, const void* ids, int32_t id_dtype, int64_t T,
@@ -224,7 +372,7 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     if (!ld_aligned(dout, ld_type_bytes(dtype)) || !ld_aligned(grad, ld_type_bytes(grad_dtype)) ||
         !ld_aligned(ids, id_dtype == LD_I32 ? 4 : 8))
         return LD_ERR_ALIGN;
-    const Layout l = layout_of(T, V);
+    const Layout l = layout_of(T, V, d);
     if (l.bytes > 0 && (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < l.bytes)) return LD_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -240,12 +388,22 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
     }
     const int32_t last = (l.passes + 1) & 1;
-    const RowArgs a = {dout, keys[last], at[last], grad, dout_stride, grad_stride, static_cast<int32_t>(T), static_cast<int32_t>(V), d, scale,
-                       accumulate};
+    const int32_t columns = LD_WAVE * (dtype == LD_F32 ? 4 : 8), blocks = static_cast<int32_t>((static_cast<int64_t>(d) + columns - 1) / columns);
+    const int64_t adding = (static_cast<int64_t>(l.chunks) * blocks + kRowWaves - 1) / kRowWaves;
+    const int64_t clearing = accumulate ? 0 : (V + kClearRows - 1) / kClearRows;
+    if (adding + clearing > INT32_MAX / kRowWaves) return LD_ERR_RANGE;
+    const RowArgs a = {dout, keys[last], at[last], grad, reinterpret_cast<float*>(ws + l.part), dout_stride, grad_stride, l.part_stride,
+                       static_cast<int32_t>(T), static_cast<int32_t>(V), d, l.chunk, blocks, static_cast<int32_t>(adding),
+                       static_cast<int32_t>(clearing), scale, accumulate};
     ld_with_type(dtype, [&](auto type) {
         ld_with_type(grad_dtype, [&](auto grad_type) {
-            k_rows<type, grad_type><<<dim3(static_cast<uint32_t>(V)), dim3(256), 0, s>>>(a);
+            k_rows<type, grad_type><<<dim3(static_cast<uint32_t>(adding + clearing)), dim3(kRowThreads), 0, s>>>(a);
         });
+    });
+    if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
+    if (l.chunks < 2) return LD_OK;
+    ld_with_type(grad_dtype, [&](auto grad_type) {
+        k_join<grad_type><<<dim3(l.chunks, static_cast<uint32_t>((d + 255) / 256)), dim3(kJoinThreads), 0, s>>>(a);
     });
     return ld_launch_status();
 }

@@ -65,7 +65,7 @@ def test_lookup_refusals():
         return lib.ld_embed_lookup(V(table), rows, ts, V(pos), P, ps, dtype, V(ids), V(at), it, T, d, F(1.0), V(out), os, ot, None)
 
     assert call(table=0) == NULL and call(ids=0) == NULL and call(out=0) == NULL and call(pos=FAKE, P=5, ps=64) == NULL
-    for bad in (dict(rows=-1), dict(T=-1), dict(d=-1), dict(ts=-1), dict(os=63), dict(dtype=3), dict(ot=-1), dict(it=2),
+    for bad in (dict(rows=-1), dict(T=-1), dict(d=-1), dict(d=(1 << 20) + 1, ts=1 << 21, os=1 << 21), dict(ts=-1), dict(os=63), dict(dtype=3), dict(ot=-1), dict(it=2),
                 dict(pos=FAKE, at=FAKE, P=-1, ps=64), dict(pos=FAKE, at=FAKE, P=5, ps=-1)):
         assert call(**bad) == RANGE, bad
     for bad in (dict(table=FAKE + 1), dict(out=FAKE + 1), dict(ids=FAKE + 4), dict(it=0, ids=FAKE + 2), dict(ot=0, out=FAKE + 2),
@@ -78,14 +78,14 @@ def test_embed_grad_refusals():
     lib = ld.load()
     wsb = lib.ld_embed_grad_workspace(8, 100, 64)
     assert wsb > 0
-    for bad in ((-1, 100, 64), (8, -1, 64), (8, 100, -1), ((1 << 24) + 1, 100, 64), (8, 2 ** 31 - 1, 64)):
+    for bad in ((-1, 100, 64), (8, -1, 64), (8, 100, -1), (8, 100, (1 << 20) + 1), ((1 << 24) + 1, 100, 64), (8, 2 ** 31 - 1, 64)):
         assert lib.ld_embed_grad_workspace(*bad) == 0
 
     def call(dout=FAKE, ds=64, dtype=1, ids=FAKE, it=1, T=8, d=64, grad=FAKE, rows=100, gs=64, gt=0, acc=0, ws=FAKE, wsb=wsb):
         return lib.ld_embed_grad(V(dout), ds, dtype, V(ids), it, T, d, F(1.0), V(grad), rows, gs, gt, acc, V(ws), wsb, None)
 
     assert call(dout=0) == NULL and call(ids=0) == NULL and call(grad=0) == NULL
-    for bad in (dict(T=-1), dict(T=(1 << 24) + 1), dict(rows=-1), dict(rows=2 ** 31 - 1), dict(d=-1), dict(ds=-1), dict(gs=63), dict(dtype=5),
+    for bad in (dict(T=-1), dict(T=(1 << 24) + 1), dict(rows=-1), dict(rows=2 ** 31 - 1), dict(d=-1), dict(d=(1 << 20) + 1, gs=1 << 21), dict(ds=-1), dict(gs=63), dict(dtype=5),
                 dict(gt=3), dict(it=-1)):
         assert call(**bad) == RANGE, bad
     for bad in (dict(dout=FAKE + 1), dict(grad=FAKE + 2), dict(ids=FAKE + 4), dict(it=0, ids=FAKE + 1)):
