@@ -142,25 +142,27 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a) {
 
 // ------------------------------------------------------------------- rows
 
-// The sorted tokens are cut into chunks of equal size, a wave for each chunk and block of columns. It adds up run after run of
-// equal ids; a run inside the chunk is written to its row at once, one that goes on in the next chunk (or came from the one
-// before) leaves a partial sum, and k_join adds those up. Rows that no token names are cleared by workgroups of the same launch.
+// The sorted tokens are cut into chunks of 32, a wave for each chunk and block of columns. It adds up, one after the other, the
+// runs of equal ids that begin in its chunk, to their ends where it can see them (64 tokens from the chunk's first on), and
+// writes their rows. A run that goes on further is long: every chunk that it touches leaves a partial sum, and k_join adds those
+// up. Rows that no token names are cleared by workgroups of the same launch.
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / LD_WAVE;
 constexpr int kAhead = 8;         // tokens whose rows a wave loads before it adds the first
-constexpr int kMostChunk = 32;    // a chunk's keys and the one on either side fit a wave
+constexpr int kChunk = 32;
 constexpr int kClearRows = 16;    // rows that a clearing workgroup looks after
-constexpr int kJoinThreads = 1024;
+constexpr int kJoinThreads = 512;
+constexpr int kJoinSplit = 4;     // workgroups of a long run, the blocks of columns dealt out to them
 
 struct RowArgs {
     const void* dout;
     const uint32_t* keys;   // sorted
     const uint32_t* at;     // the tokens in that order
     void* grad;
-    float* part;            // [2 * chunks] rows of part_stride: a chunk's sum of the run that came from the one before, and of the one that goes on
+    float* part;            // [2 * chunks] rows of part_stride: a chunk's sum of the long run that came to it, and of the one that begins in it
     int64_t dout_stride, grad_stride, part_stride;
     int32_t T, V, d;
-    int32_t chunk, blocks;  // tokens of a chunk; blocks of columns
+    int32_t blocks;         // of columns
     int32_t adding, clearing;  // workgroups of each kind
     float scale;
     int32_t accumulate;
@@ -240,6 +242,30 @@ __device__ void clear_rows(const RowArgs& a, int32_t first) {
     }
 }
 
+// The runs of equal ids around a chunk.
+struct Runs {
+    uint32_t key;        // lane l: of token from + l; what lies past the tokens has none's
+    uint64_t heads;      // bit l: another run begins with token from + l
+    bool began_before;   // some run begins in the chunk before
+    int32_t valid;       // tokens from the chunk's first on that name a row
+};
+constexpr uint64_t kOwn = (1ull << kChunk) - 1;  // the chunk's own tokens
+
+__device__ __forceinline__ Runs runs_of(const RowArgs& a, int32_t from) {
+    constexpr int kShr1 = 0x138;  // to a lane from the one below
+    Runs r;
+    const int32_t i = from + ld_lane(), b = i - kChunk - 1;
+    r.key = i < a.T ? a.keys[i] : UINT32_MAX;
+    const uint32_t before = b >= 0 && b < a.T ? a.keys[b] : UINT32_MAX;
+    const uint32_t last = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(before), kChunk));
+    const uint32_t below = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(last), static_cast<int>(r.key), kShr1, 0xf, 0xf, false));
+    const uint32_t below_before = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(before), kShr1, 0xf, 0xf, false));
+    r.heads = __ballot(r.key != below);
+    r.began_before = (__ballot(before != below_before) >> 1 & kOwn) != 0;
+    r.valid = __popcll(__ballot(r.key < static_cast<uint32_t>(a.V)));
+    return r;
+}
+
 template <int DT, int GT>
 __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
     constexpr int N = DT == LD_F32 ? 4 : 8;
@@ -256,78 +282,91 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
     }
     const int32_t unit = __builtin_amdgcn_readfirstlane(block * kRowWaves + static_cast<int32_t>(threadIdx.x / LD_WAVE));
     const int32_t c = unit / a.blocks, column = ((unit - c * a.blocks) * LD_WAVE + ld_lane()) * N, have = a.d - column;
-    const int32_t from = c * a.chunk;
+    const int32_t from = c * kChunk;
     if (from >= a.T) return;
-    // lane l holds the key of token from - 1 + l; none is V
-    const int32_t i = from - 1 + ld_lane();
-    const bool in = i >= 0 && i < a.T && ld_lane() <= a.chunk + 1;
-    const uint32_t key = in ? a.keys[i] : a.V, at = in ? a.at[i] : 0;
-    const auto key_of = [&](int32_t j) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key), j)); };
-    uint32_t run = key_of(1);
-    if (run >= static_cast<uint32_t>(a.V)) return;
+    const Runs r = runs_of(a, from);
+    const uint32_t at = from + ld_lane() < a.T ? a.at[from + ld_lane()] : 0;
+    const uint64_t own = r.heads & kOwn, later = r.heads & ~1ull;
+    // tokens [i, end) from the chunk's first on
+    int32_t i = 0;
+    bool came = false;
+    if (!(r.heads & 1)) {
+        const int32_t left = later ? __builtin_ctzll(later) : LD_WAVE;
+        if (r.began_before && left < kChunk) i = left;  // the chunk before adds that run up
+        else came = true;
+    }
+    const bool goes_on = (r.heads & ~kOwn) == 0;  // the last run that begins here, past what is seen of it
+    int32_t end = own == 0 || goes_on ? kChunk : __builtin_ctzll(r.heads & ~kOwn);
+    if (end > r.valid) end = r.valid;
     const typename X::elem* dout = static_cast<const typename X::elem*>(a.dout) + column;
     float* part = a.part + 2 * static_cast<int64_t>(c) * a.part_stride + column;
-    const bool came = key_of(0) == run;
-    bool first = true;
     typename X::wide sum = typename X::wide(0.0f);
-    for (int32_t j0 = 1; j0 <= a.chunk; j0 += kAhead) {
+    int32_t run = i;  // where the run being added up begins
+    while (i < end) {
         typename X::type x[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const uint32_t t = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), j0 + u));
+            const uint32_t t = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), (i + u) & (LD_WAVE - 1)));
             x[u] = typename X::type(0);
-            if (key_of(j0 + u) < static_cast<uint32_t>(a.V) && have > 0) x[u] = load_some<DT, N>(dout + t * a.dout_stride, have);
+            if (i + u < end && have > 0) x[u] = load_some<DT, N>(dout + t * a.dout_stride, have);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const uint32_t k = key_of(j0 + u);
-            if (k != run) {
-                if (run < static_cast<uint32_t>(a.V) && have > 0) {
-                    if (first && came) store_some<LD_F32, N>(part, have, sum);
-                    else write_row<GT, N>(a, run, column, have, sum);
+            if (i + u >= end) break;
+            if (i + u > run && (r.heads >> (i + u) & 1)) {
+                if (have > 0) {
+                    if (came) store_some<LD_F32, N>(part, have, sum);
+                    else write_row<GT, N>(a, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), run)), column, have, sum);
                 }
-                first = false;
-                run = k;
+                came = false;
+                run = i + u;
                 sum = typename X::wide(0.0f);
             }
             sum += X::widen(x[u]);
         }
+        i += kAhead;
     }
-    if (run >= static_cast<uint32_t>(a.V) || have <= 0) return;
-    if (first && came) store_some<LD_F32, N>(part, have, sum);
-    else if (key_of(a.chunk + 1) == run) store_some<LD_F32, N>(part + a.part_stride, have, sum);
-    else write_row<GT, N>(a, run, column, have, sum);
+    if (run >= end || have <= 0) return;
+    if (came) store_some<LD_F32, N>(part, have, sum);
+    else if (goes_on && end == kChunk) store_some<LD_F32, N>(part + a.part_stride, have, sum);
+    else write_row<GT, N>(a, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), run)), column, have, sum);
 }
 
-// Adds up the partial sums of the run that begins in a chunk and does not end there, in their order: a workgroup per chunk and
-// 256 columns, its waves taking partial sums in turn.
+// Adds up the partial sums of the long run that begins in a chunk, in their order: workgroups per chunk, each with every
+// kJoinSplit-th block of 256 columns, its waves taking partial sums in turn.
 template <int GT>
 __global__ __launch_bounds__(kJoinThreads) void k_join(RowArgs a) {
     constexpr int N = 4, kWaves = kJoinThreads / LD_WAVE;
     __shared__ ld_f32x4 sh[kWaves][LD_WAVE];
-    const int32_t c = blockIdx.x, from = c * a.chunk, next = from + a.chunk;
-    if (next >= a.T) return;
-    const uint32_t v = a.keys[next];
-    if (v >= static_cast<uint32_t>(a.V) || a.keys[next - 1] != v || (from > 0 && a.keys[from - 1] == v)) return;
-    const int32_t end = lower_bound(a.keys, a.T, v + 1), last = (end - 1) / a.chunk;
-    const int32_t column = (blockIdx.y * LD_WAVE + ld_lane()) * N, have = a.d - column, wave = threadIdx.x / LD_WAVE;
-    ld_f32x4 sum = ld_f32x4(0.0f);
-    if (have > 0) {
-        for (int32_t j = c + wave; j <= last; j += kWaves)
-            sum += load_some<LD_F32, N>(a.part + (2 * static_cast<int64_t>(j) + (j == c)) * a.part_stride + column, have);
+    const int32_t c = blockIdx.x, from = c * kChunk;
+    const Runs r = runs_of(a, from);
+    const uint64_t own = r.heads & kOwn;
+    if (own == 0 || (r.heads & ~kOwn) != 0) return;
+    const int32_t first = LD_WAVE - 1 - __builtin_clzll(own);
+    if (first >= r.valid) return;
+    const uint32_t v = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), first));
+    const int32_t last = (lower_bound(a.keys, a.T, v + 1) - 1) / kChunk, wave = threadIdx.x / LD_WAVE;
+    for (int32_t block = blockIdx.y * LD_WAVE * N; block < a.d; block += kJoinSplit * LD_WAVE * N) {
+        const int32_t column = block + ld_lane() * N, have = a.d - column;
+        ld_f32x4 sum = ld_f32x4(0.0f);
+        if (have > 0) {
+            for (int32_t j = c + wave; j <= last; j += kWaves)
+                sum += load_some<LD_F32, N>(a.part + (2 * static_cast<int64_t>(j) + (j == c)) * a.part_stride + column, have);
+        }
+        sh[wave][ld_lane()] = sum;
+        __syncthreads();
+        if (wave == 0 && have > 0) {
+            const int32_t waves = last - c + 1 < kWaves ? last - c + 1 : kWaves;
+            for (int32_t w = 1; w < waves; ++w) sum += sh[w][ld_lane()];
+            write_row<GT, N>(a, v, column, have, sum);
+        }
+        __syncthreads();
     }
-    sh[wave][ld_lane()] = sum;
-    __syncthreads();
-    if (wave > 0 || have <= 0) return;
-    sum = sh[0][ld_lane()];
-    const int32_t waves = last - c + 1 < kWaves ? last - c + 1 : kWaves;
-    for (int32_t w = 1; w < waves; ++w) sum += sh[w][ld_lane()];
-    write_row<GT, N>(a, v, column, have, sum);
 }
 
 struct Layout {
     int32_t passes, bits, tiles;
-    int32_t chunk, chunks;
+    int32_t chunks;
     int64_t part_stride;
     size_t keys, at, counts, part, bytes;  // byte offsets: two buffers each of keys and tokens
 };
@@ -344,8 +383,7 @@ Layout layout_of(int64_t T, int64_t V, int32_t d) {
     l.at = 2 * list;
     l.counts = 4 * list;
     l.part = ld_round_up(l.counts + (static_cast<size_t>(l.tiles) << l.bits) * 4, 256);
-    l.chunk = kMostChunk;
-    l.chunks = static_cast<int32_t>((T + l.chunk - 1) / l.chunk);
+    l.chunks = static_cast<int32_t>((T + kChunk - 1) / kChunk);
     l.part_stride = (static_cast<int64_t>(d) + 3) / 4 * 4;
     l.bytes = ld_round_up(l.part + 2 * static_cast<size_t>(l.chunks) * l.part_stride * 4, 256);
     return l;
@@ -393,7 +431,7 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     const int64_t clearing = accumulate ? 0 : (V + kClearRows - 1) / kClearRows;
     if (adding + clearing > INT32_MAX / kRowWaves) return LD_ERR_RANGE;
     const RowArgs a = {dout, keys[last], at[last], grad, reinterpret_cast<float*>(ws + l.part), dout_stride, grad_stride, l.part_stride,
-                       static_cast<int32_t>(T), static_cast<int32_t>(V), d, l.chunk, blocks, static_cast<int32_t>(adding),
+                       static_cast<int32_t>(T), static_cast<int32_t>(V), d, blocks, static_cast<int32_t>(adding),
                        static_cast<int32_t>(clearing), scale, accumulate};
     ld_with_type(dtype, [&](auto type) {
         ld_with_type(grad_dtype, [&](auto grad_type) {
@@ -401,9 +439,10 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
         });
     });
     if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
-    if (l.chunks < 2) return LD_OK;
+    if (T < 2 * kChunk) return LD_OK;  // no run is long
     ld_with_type(grad_dtype, [&](auto grad_type) {
-        k_join<grad_type><<<dim3(l.chunks, static_cast<uint32_t>((d + 255) / 256)), dim3(kJoinThreads), 0, s>>>(a);
+        const int32_t split = (d + 255) / 256 < kJoinSplit ? (d + 255) / 256 : kJoinSplit;
+        k_join<grad_type><<<dim3(l.chunks, split), dim3(kJoinThreads), 0, s>>>(a);
     });
     return ld_launch_status();
 }
