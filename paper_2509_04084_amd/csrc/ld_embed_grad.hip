@@ -142,17 +142,21 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a) {
 
 // ------------------------------------------------------------------- rows
 
-// The sorted tokens are cut into chunks of 32, a wave for each chunk and block of columns. It adds up, one after the other, the
-// runs of equal ids that begin in its chunk, to their ends where it can see them (64 tokens from the chunk's first on), and
+// The sorted tokens are cut into chunks of 4 to 32, a wave for each chunk and block of columns. It adds up, one after the other,
+// the runs of equal ids that begin in its chunk, to their ends where it can see them (64 tokens from the chunk's first on), and
 // writes their rows. A run that goes on further is long: every chunk that it touches leaves a partial sum, and k_join adds those
 // up. Rows that no token names are cleared by workgroups of the same launch.
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / LD_WAVE;
 constexpr int kAhead = 8;         // tokens whose rows a wave loads before it adds the first
-constexpr int kChunk = 32;
+constexpr int kMostChunk = 32;
 constexpr int kClearRows = 16;    // rows that a clearing workgroup looks after
-constexpr int kJoinThreads = 512;
-constexpr int kJoinSplit = 4;     // workgroups of a long run, the blocks of columns dealt out to them
+// dout past the 256 MB that the last cache holds is read around it. GPT-2 XL's 52 MB (three batches in turn) 108 us from the cache, 124
+// around it; 537 MB of bf16 at Llama's width 217 and 210, all of one id 269 and 222. Finished rows are always written around it, partial
+// sums never (one id 285 us).
+constexpr int64_t kStreamed = 256 << 20;
+constexpr int kJoinWaves = 8;     // chunks of a joining workgroup
+constexpr int kJoinAlone = 8;     // partial sums that a wave adds up by itself
 
 struct RowArgs {
     const void* dout;
@@ -162,7 +166,7 @@ struct RowArgs {
     float* part;            // [2 * chunks] rows of part_stride: a chunk's sum of the long run that came to it, and of the one that begins in it
     int64_t dout_stride, grad_stride, part_stride;
     int32_t T, V, d;
-    int32_t blocks;         // of columns
+    int32_t chunk, blocks;  // tokens of a chunk; blocks of columns
     int32_t adding, clearing;  // workgroups of each kind
     float scale;
     int32_t accumulate;
@@ -183,41 +187,70 @@ __device__ __forceinline__ int32_t lower_bound(const uint32_t* keys, int32_t n, 
     return lo;
 }
 
-// The first `have` of N elements from p on, the others zero; all N in one access where they are there.
-template <int DT, int N>
-__device__ __forceinline__ typename LdVec<DT, N>::type load_some(const typename LdElem<DT>::type* p, int32_t have) {
+// The same, looked for by the wave together: 64 keys at a time.
+__device__ __forceinline__ int32_t wave_lower_bound(const uint32_t* keys, int32_t n, uint32_t v) {
+    int32_t lo = 0;
+    while (n > 0) {
+        const int32_t step = (n + LD_WAVE - 1) / LD_WAVE, i = ld_lane() * step;
+        const int32_t less = __popcll(__ballot(i < n && keys[lo + i] < v));
+        if (less == 0) break;
+        const int32_t skip = (less - 1) * step + 1;
+        lo += skip;
+        n = step - 1 < n - skip ? step - 1 : n - skip;
+    }
+    return lo;
+}
+
+// The columns of a lane: N from `column` on, of which the last `own` are its own. In the row's last vector, which ends with the
+// row, the first are the lane's before (their sums are made twice and written once); in rows of fewer than N columns they are none.
+struct Columns {
+    int32_t column, own;
+};
+
+template <int N>
+__device__ __forceinline__ Columns columns_of(int32_t vector, int32_t d) {
+    const int32_t begin = vector * N, left = d - begin;
+    return {left >= N ? begin : d - N, left >= N ? N : left > 0 ? left : 0};
+}
+
+template <int DT, int N, bool STREAM>
+__device__ __forceinline__ typename LdVec<DT, N>::type load_columns(const typename LdElem<DT>::type* row, Columns c) {
+    if (c.column >= 0) {
+        const typename LdVec<DT, N>::type* p = reinterpret_cast<const typename LdVec<DT, N>::type*>(row + c.column);
+        return STREAM ? __builtin_nontemporal_load(p) : *p;
+    }
     typename LdVec<DT, N>::type x = typename LdVec<DT, N>::type(0);
-    if (have >= N) return *reinterpret_cast<const typename LdVec<DT, N>::type*>(p);
 #pragma unroll
-    for (int e = 0; e < N - 1; ++e)
-        if (e < have) x[e] = p[e];
+    for (int e = 1; e < N; ++e)
+        if (e + c.column >= 0) x[e] = row[e + c.column];
     return x;
 }
 
-template <int DT, int N>
-__device__ __forceinline__ void store_some(typename LdElem<DT>::type* p, int32_t have, typename LdVec<DT, N>::type x) {
-    if (have >= N) {
-        *reinterpret_cast<typename LdVec<DT, N>::type*>(p) = x;
+template <int DT, int N, bool STREAM>
+__device__ __forceinline__ void store_columns(typename LdElem<DT>::type* row, Columns c, typename LdVec<DT, N>::type x) {
+    if (c.own == N) {
+        if (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<typename LdVec<DT, N>::type*>(row + c.column));
+        else *reinterpret_cast<typename LdVec<DT, N>::type*>(row + c.column) = x;
     } else {
 #pragma unroll
-        for (int e = 0; e < N - 1; ++e)
-            if (e < have) p[e] = x[e];
+        for (int e = 1; e < N; ++e)
+            if (e >= N - c.own) row[c.column + e] = x[e];
     }
 }
 
 // A finished sum to its row.
 template <int GT, int N>
-__device__ __forceinline__ void write_row(const RowArgs& a, uint32_t v, int32_t column, int32_t have, typename LdVec<GT, N>::wide sum) {
-    typename LdElem<GT>::type* row = static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(v) * a.grad_stride + column;
+__device__ __forceinline__ void write_row(const RowArgs& a, uint32_t v, Columns c, typename LdVec<GT, N>::wide sum) {
+    typename LdElem<GT>::type* row = static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(v) * a.grad_stride;
     if (a.accumulate) {
-        const typename LdVec<GT, N>::wide old = LdVec<GT, N>::widen(load_some<GT, N>(row, have));
+        const typename LdVec<GT, N>::wide old = LdVec<GT, N>::widen(load_columns<GT, N, false>(row, c));
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[e] = __fmaf_rn(a.scale, sum[e], old[e]);
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[e] = a.scale * sum[e];
     }
-    store_some<GT, N>(row, have, LdVec<GT, N>::narrow(sum));
+    store_columns<GT, N, true>(row, c, LdVec<GT, N>::narrow(sum));
 }
 
 template <int GT>
@@ -238,7 +271,7 @@ __device__ void clear_rows(const RowArgs& a, int32_t first) {
     for (int32_t r = threadIdx.x / LD_WAVE; r < kClearRows && first + r < a.V; r += kRowWaves) {
         if (named >> r & 1) continue;
         typename LdElem<GT>::type* row = static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(first + r) * a.grad_stride;
-        for (int32_t c = ld_lane() * N; c < a.d; c += LD_WAVE * N) store_some<GT, N>(row + c, a.d - c, typename LdVec<GT, N>::type(0));
+        for (int32_t l = ld_lane(); l * N < a.d; l += LD_WAVE) store_columns<GT, N, true>(row, columns_of<N>(l, a.d), typename LdVec<GT, N>::type(0));
     }
 }
 
@@ -246,27 +279,29 @@ __device__ void clear_rows(const RowArgs& a, int32_t first) {
 struct Runs {
     uint32_t key;        // lane l: of token from + l; what lies past the tokens has none's
     uint64_t heads;      // bit l: another run begins with token from + l
-    bool began_before;   // some run begins in the chunk before
+    uint64_t own;        // the bits of the chunk itself
+    int32_t began;       // where the last run before the chunk began, if that is one of the 63 tokens before, else -1
     int32_t valid;       // tokens from the chunk's first on that name a row
 };
-constexpr uint64_t kOwn = (1ull << kChunk) - 1;  // the chunk's own tokens
 
 __device__ __forceinline__ Runs runs_of(const RowArgs& a, int32_t from) {
     constexpr int kShr1 = 0x138;  // to a lane from the one below
     Runs r;
-    const int32_t i = from + ld_lane(), b = i - kChunk - 1;
+    const int32_t i = from + ld_lane(), b = i - LD_WAVE;
     r.key = i < a.T ? a.keys[i] : UINT32_MAX;
-    const uint32_t before = b >= 0 && b < a.T ? a.keys[b] : UINT32_MAX;
-    const uint32_t last = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(before), kChunk));
+    const uint32_t before = b >= 0 ? a.keys[b] : UINT32_MAX;
+    const uint32_t last = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(before), LD_WAVE - 1));
     const uint32_t below = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(last), static_cast<int>(r.key), kShr1, 0xf, 0xf, false));
     const uint32_t below_before = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(before), kShr1, 0xf, 0xf, false));
+    r.own = (1ull << a.chunk) - 1;
     r.heads = __ballot(r.key != below);
-    r.began_before = (__ballot(before != below_before) >> 1 & kOwn) != 0;
+    const uint64_t heads_before = __ballot(before != below_before) & ~1ull;
+    r.began = heads_before ? from - 1 - __builtin_clzll(heads_before) : -1;
     r.valid = __popcll(__ballot(r.key < static_cast<uint32_t>(a.V)));
     return r;
 }
 
-template <int DT, int GT>
+template <int DT, int GT, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
     constexpr int N = DT == LD_F32 ? 4 : 8;
     typedef LdVec<DT, N> X;
@@ -281,84 +316,123 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
         block -= before;
     }
     const int32_t unit = __builtin_amdgcn_readfirstlane(block * kRowWaves + static_cast<int32_t>(threadIdx.x / LD_WAVE));
-    const int32_t c = unit / a.blocks, column = ((unit - c * a.blocks) * LD_WAVE + ld_lane()) * N, have = a.d - column;
-    const int32_t from = c * kChunk;
+    const int32_t c = unit / a.blocks;
+    const Columns cols = columns_of<N>((unit - c * a.blocks) * LD_WAVE + ld_lane(), a.d);
+    const int32_t from = c * a.chunk;
     if (from >= a.T) return;
     const Runs r = runs_of(a, from);
     const uint32_t at = from + ld_lane() < a.T ? a.at[from + ld_lane()] : 0;
-    const uint64_t own = r.heads & kOwn, later = r.heads & ~1ull;
+    const uint64_t after = r.heads & ~r.own, later = r.heads & ~1ull;
     // tokens [i, end) from the chunk's first on
     int32_t i = 0;
     bool came = false;
     if (!(r.heads & 1)) {
         const int32_t left = later ? __builtin_ctzll(later) : LD_WAVE;
-        if (r.began_before && left < kChunk) i = left;  // the chunk before adds that run up
+        // whether the chunk that this run began in sees its end, and so adds it up
+        if (r.began >= 0 && from + left < (r.began & -a.chunk) + LD_WAVE) i = left;
         else came = true;
     }
-    const bool goes_on = (r.heads & ~kOwn) == 0;  // the last run that begins here, past what is seen of it
-    int32_t end = own == 0 || goes_on ? kChunk : __builtin_ctzll(r.heads & ~kOwn);
+    // the last run that begins here is long, or none begins; else it is followed to its end
+    const bool goes_on = after == 0;
+    int32_t end = goes_on || (r.heads & r.own) == 0 ? a.chunk : __builtin_ctzll(after);
     if (end > r.valid) end = r.valid;
-    const typename X::elem* dout = static_cast<const typename X::elem*>(a.dout) + column;
-    float* part = a.part + 2 * static_cast<int64_t>(c) * a.part_stride + column;
+    const typename X::elem* dout = static_cast<const typename X::elem*>(a.dout);
+    float* part = a.part + 2 * static_cast<int64_t>(c) * a.part_stride;
     typename X::wide sum = typename X::wide(0.0f);
     int32_t run = i;  // where the run being added up begins
-    while (i < end) {
+    const auto load = [&](int32_t j) {
+        return load_columns<DT, N, STREAM>(dout + static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), j)) * a.dout_stride, cols);
+    };
+    const auto add = [&](int32_t j, typename X::type x) {
+        if (j > run && (r.heads >> j & 1)) {
+            if (came) store_columns<LD_F32, N, false>(part, cols, sum);
+            else write_row<GT, N>(a, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), run)), cols, sum);
+            came = false;
+            run = j;
+            sum = X::widen(x);
+        } else {
+            sum += X::widen(x);
+        }
+    };
+    for (; i + kAhead <= end; i += kAhead) {
         typename X::type x[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const uint32_t t = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), (i + u) & (LD_WAVE - 1)));
-            x[u] = typename X::type(0);
-            if (i + u < end && have > 0) x[u] = load_some<DT, N>(dout + t * a.dout_stride, have);
-        }
+        for (int u = 0; u < kAhead; ++u) x[u] = load(i + u);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (i + u >= end) break;
-            if (i + u > run && (r.heads >> (i + u) & 1)) {
-                if (have > 0) {
-                    if (came) store_some<LD_F32, N>(part, have, sum);
-                    else write_row<GT, N>(a, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), run)), column, have, sum);
-                }
-                came = false;
-                run = i + u;
-                sum = typename X::wide(0.0f);
-            }
-            sum += X::widen(x[u]);
-        }
-        i += kAhead;
+        for (int u = 0; u < kAhead; ++u) add(i + u, x[u]);
     }
-    if (run >= end || have <= 0) return;
-    if (came) store_some<LD_F32, N>(part, have, sum);
-    else if (goes_on && end == kChunk) store_some<LD_F32, N>(part + a.part_stride, have, sum);
-    else write_row<GT, N>(a, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), run)), column, have, sum);
+    if (i < end) {
+        typename X::type x[kAhead - 1];
+#pragma unroll
+        for (int u = 0; u < kAhead - 1; ++u)
+            if (i + u < end) x[u] = load(i + u);
+#pragma unroll
+        for (int u = 0; u < kAhead - 1; ++u)
+            if (i + u < end) add(i + u, x[u]);
+    }
+    if (run >= end) return;
+    if (came) store_columns<LD_F32, N, false>(part, cols, sum);
+    else if (goes_on && end == a.chunk) store_columns<LD_F32, N, false>(part + a.part_stride, cols, sum);
+    else write_row<GT, N>(a, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), run)), cols, sum);
 }
 
-// Adds up the partial sums of the long run that begins in a chunk, in their order: workgroups per chunk, each with every
-// kJoinSplit-th block of 256 columns, its waves taking partial sums in turn.
+// Adds up the partial sums of long runs, each from the chunk that it begins in to the one that it ends in, in their order. A wave
+// looks at a chunk, with 256 columns; what it would be long busy with is shared by the workgroup's waves, which take partial sums in turn.
 template <int GT>
-__global__ __launch_bounds__(kJoinThreads) void k_join(RowArgs a) {
-    constexpr int N = 4, kWaves = kJoinThreads / LD_WAVE;
-    __shared__ ld_f32x4 sh[kWaves][LD_WAVE];
-    const int32_t c = blockIdx.x, from = c * kChunk;
-    const Runs r = runs_of(a, from);
-    const uint64_t own = r.heads & kOwn;
-    if (own == 0 || (r.heads & ~kOwn) != 0) return;
-    const int32_t first = LD_WAVE - 1 - __builtin_clzll(own);
-    if (first >= r.valid) return;
-    const uint32_t v = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), first));
-    const int32_t last = (lower_bound(a.keys, a.T, v + 1) - 1) / kChunk, wave = threadIdx.x / LD_WAVE;
-    for (int32_t block = blockIdx.y * LD_WAVE * N; block < a.d; block += kJoinSplit * LD_WAVE * N) {
-        const int32_t column = block + ld_lane() * N, have = a.d - column;
+__global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_t chunks) {
+    constexpr int N = 4;
+    __shared__ ld_f32x4 sh[kJoinWaves][LD_WAVE];
+    __shared__ int32_t shared_last[kJoinWaves];
+    __shared__ uint32_t shared_run[kJoinWaves];
+    const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LD_WAVE), c0 = blockIdx.x * kJoinWaves, c = c0 + wave;
+    const Columns cols = columns_of<N>(blockIdx.y * LD_WAVE + ld_lane(), a.d);
+    const auto sum_of = [&](int32_t first, int32_t from, int32_t last, int32_t step) {
         ld_f32x4 sum = ld_f32x4(0.0f);
-        if (have > 0) {
-            for (int32_t j = c + wave; j <= last; j += kWaves)
-                sum += load_some<LD_F32, N>(a.part + (2 * static_cast<int64_t>(j) + (j == c)) * a.part_stride + column, have);
+        for (int32_t j = from; j <= last; j += step * kJoinAlone) {
+            ld_f32x4 x[kJoinAlone];
+#pragma unroll
+            for (int u = 0; u < kJoinAlone; ++u) {
+                const int64_t k = j + u * step;
+                x[u] = k <= last ? load_columns<LD_F32, N, false>(a.part + (2 * k + (k == first)) * a.part_stride, cols) : ld_f32x4(0.0f);
+            }
+#pragma unroll
+            for (int u = 0; u < kJoinAlone; ++u) sum += x[u];
         }
-        sh[wave][ld_lane()] = sum;
+        return sum;
+    };
+    int32_t last = -1;
+    uint32_t run = 0;
+    if (c < chunks) {
+        const Runs r = runs_of(a, c * a.chunk);
+        const uint64_t own = r.heads & r.own;
+        if (own != 0 && (r.heads & ~r.own) == 0) {
+            const int32_t first = LD_WAVE - 1 - __builtin_clzll(own);
+            if (first < r.valid) {
+                run = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), first));
+                last = (wave_lower_bound(a.keys, a.T, run + 1) - 1) / a.chunk;
+            }
+        }
+    }
+    const bool alone = last - c < kJoinAlone;
+    if (ld_lane() == 0) {
+        shared_last[wave] = alone ? -1 : last;
+        shared_run[wave] = run;
+    }
+    __syncthreads();
+    if (last >= 0 && alone) {
+        const ld_f32x4 sum = sum_of(c, c, last, 1);
+        write_row<GT, N>(a, run, cols, sum);
+    }
+    for (int32_t w = 0; w < kJoinWaves; ++w) {
+        const int32_t to = shared_last[w];
+        if (to < 0) continue;
+        sh[wave][ld_lane()] = sum_of(c0 + w, c0 + w + wave, to, kJoinWaves);
         __syncthreads();
-        if (wave == 0 && have > 0) {
-            const int32_t waves = last - c + 1 < kWaves ? last - c + 1 : kWaves;
-            for (int32_t w = 1; w < waves; ++w) sum += sh[w][ld_lane()];
-            write_row<GT, N>(a, v, column, have, sum);
+        if (wave == 0) {
+            ld_f32x4 sum = sh[0][ld_lane()];
+#pragma unroll
+            for (int i = 1; i < kJoinWaves; ++i) sum += sh[i][ld_lane()];
+            write_row<GT, N>(a, shared_run[w], cols, sum);
         }
         __syncthreads();
     }
@@ -366,7 +440,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join(RowArgs a) {
 
 struct Layout {
     int32_t passes, bits, tiles;
-    int32_t chunks;
+    int32_t chunk, chunks;
     int64_t part_stride;
     size_t keys, at, counts, part, bytes;  // byte offsets: two buffers each of keys and tokens
 };
@@ -383,7 +457,10 @@ Layout layout_of(int64_t T, int64_t V, int32_t d) {
     l.at = 2 * list;
     l.counts = 4 * list;
     l.part = ld_round_up(l.counts + (static_cast<size_t>(l.tiles) << l.bits) * 4, 256);
-    l.chunks = static_cast<int32_t>((T + kChunk - 1) / kChunk);
+    l.chunk = kMostChunk;
+    // few tokens: smaller chunks, so that more waves share them
+    while (l.chunk > 4 && (T / l.chunk) * ((d + 511) / 512) < 2048) l.chunk /= 2;
+    l.chunks = static_cast<int32_t>((T + l.chunk - 1) / l.chunk);
     l.part_stride = (static_cast<int64_t>(d) + 3) / 4 * 4;
     l.bytes = ld_round_up(l.part + 2 * static_cast<size_t>(l.chunks) * l.part_stride * 4, 256);
     return l;
@@ -431,18 +508,21 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     const int64_t clearing = accumulate ? 0 : (V + kClearRows - 1) / kClearRows;
     if (adding + clearing > INT32_MAX / kRowWaves) return LD_ERR_RANGE;
     const RowArgs a = {dout, keys[last], at[last], grad, reinterpret_cast<float*>(ws + l.part), dout_stride, grad_stride, l.part_stride,
-                       static_cast<int32_t>(T), static_cast<int32_t>(V), d, blocks, static_cast<int32_t>(adding),
+                       static_cast<int32_t>(T), static_cast<int32_t>(V), d, l.chunk, blocks, static_cast<int32_t>(adding),
                        static_cast<int32_t>(clearing), scale, accumulate};
+    const dim3 grid(static_cast<uint32_t>(adding + clearing));
+    const bool streamed = T * static_cast<int64_t>(d) * ld_type_bytes(dtype) > kStreamed;
     ld_with_type(dtype, [&](auto type) {
         ld_with_type(grad_dtype, [&](auto grad_type) {
-            k_rows<type, grad_type><<<dim3(static_cast<uint32_t>(adding + clearing)), dim3(kRowThreads), 0, s>>>(a);
+            if (streamed) k_rows<type, grad_type, true><<<grid, dim3(kRowThreads), 0, s>>>(a);
+            else k_rows<type, grad_type, false><<<grid, dim3(kRowThreads), 0, s>>>(a);
         });
     });
     if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
-    if (T < 2 * kChunk) return LD_OK;  // no run is long
+    if (T < LD_WAVE) return LD_OK;  // no run is long
     ld_with_type(grad_dtype, [&](auto grad_type) {
-        const int32_t split = (d + 255) / 256 < kJoinSplit ? (d + 255) / 256 : kJoinSplit;
-        k_join<grad_type><<<dim3(l.chunks, split), dim3(kJoinThreads), 0, s>>>(a);
+        const dim3 joins((l.chunks + kJoinWaves - 1) / kJoinWaves, (d + 4 * LD_WAVE - 1) / (4 * LD_WAVE));
+        k_join<grad_type><<<joins, dim3(kJoinWaves * LD_WAVE), 0, s>>>(a, l.chunks);
     });
     return ld_launch_status();
 }
