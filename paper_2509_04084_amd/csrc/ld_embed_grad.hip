@@ -11,196 +11,6 @@
 
 namespace {
 
-// ------------------------------------------------------------------ sort
-
-// Least significant digit first, two launches a digit: every tile counts its digits, then finds from all tiles' counts where
-// each of its digits goes and moves its tokens there.
-constexpr int kSortThreads = 1024;
-constexpr int kSortWaves = kSortThreads / LD_WAVE;
-constexpr int kSortRounds = 4;                             // tokens of a lane
-constexpr int kTile = kSortThreads * kSortRounds;          // tokens of a workgroup
-constexpr int kWaveTokens = LD_WAVE * kSortRounds;         // consecutive tokens of a wave
-constexpr int kDigitBits = 11;                             // most bits of a digit
-constexpr int kBins = 1 << kDigitBits;
-
-struct SortArgs {
-    const void* ids;         // the first digit's input, else NULL
-    int32_t wide_ids;
-    const uint32_t* keys_in;
-    const uint32_t* at_in;
-    uint32_t* keys_out;
-    uint32_t* at_out;
-    uint32_t* counts;        // [tiles][1 << bits]
-    int64_t V;
-    int32_t T, tiles, shift, bits;
-};
-
-// A token's key: its id, or V for one that names no row.
-__device__ __forceinline__ uint32_t key_of(const SortArgs& a, int32_t i) {
-    if (!a.ids) return a.keys_in[i];
-    const int64_t id = a.wide_ids ? static_cast<const int64_t*>(a.ids)[i] : static_cast<const int32_t*>(a.ids)[i];
-    return static_cast<uint32_t>(id >= 0 && id < a.V ? id : a.V);
-}
-
-__global__ __launch_bounds__(kSortThreads) void k_sort_count(SortArgs a) {
-    __shared__ uint32_t count[kBins];
-    const int32_t bins = 1 << a.bits;
-    for (int32_t i = threadIdx.x; i < bins; i += kSortThreads) count[i] = 0;
-    __syncthreads();
-    const int32_t base = blockIdx.x * kTile;
-#pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-        const int32_t i = base + r * kSortThreads + threadIdx.x;
-        if (i < a.T) atomicAdd(&count[(key_of(a, i) >> a.shift) & (bins - 1)], 1u);
-    }
-    __syncthreads();
-    for (int32_t i = threadIdx.x; i < bins; i += kSortThreads) a.counts[static_cast<size_t>(blockIdx.x) * bins + i] = count[i];
-}
-
-__global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a) {
-    __shared__ uint32_t first[kBins];                 // where this tile's tokens of a digit begin in the output
-    __shared__ uint16_t before[kSortWaves][kBins];    // of a digit, in the waves before (while counting: in this wave so far)
-    __shared__ uint32_t wave_total[kSortWaves];
-    const int32_t bins = 1 << a.bits, wave = threadIdx.x / LD_WAVE;
-    const uint32_t mask = bins - 1;
-
-    // a digit's tokens in the tiles before this one, and in all of them
-    constexpr int kPer = kBins / kSortThreads;
-    uint32_t mine[kPer], all[kPer], sum = 0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const int32_t b = threadIdx.x * kPer + j;
-        mine[j] = all[j] = 0;
-        if (b < bins) {
-            for (int32_t t = 0; t < a.tiles; ++t) {
-                const uint32_t c = a.counts[static_cast<size_t>(t) * bins + b];
-                all[j] += c;
-                if (t < static_cast<int32_t>(blockIdx.x)) mine[j] += c;
-            }
-        }
-        sum += all[j];
-    }
-    const uint32_t upto = ld_wave_iscan(sum);
-    if (ld_lane() == LD_WAVE - 1) wave_total[wave] = upto;
-    for (int32_t i = threadIdx.x; i < bins; i += kSortThreads)
-        for (int w = 0; w < kSortWaves; ++w) before[w][i] = 0;
-    __syncthreads();
-    uint32_t from = upto - sum;
-    for (int w = 0; w < wave; ++w) from += wave_total[w];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const int32_t b = threadIdx.x * kPer + j;
-        if (b < bins) first[b] = from + mine[j];
-        from += all[j];
-    }
-
-    // a token's rank among those of its digit in its wave: earlier rounds, and the lanes below in its own
-    uint32_t key[kSortRounds], at[kSortRounds], rank[kSortRounds];
-    const int32_t base = blockIdx.x * kTile + wave * kWaveTokens + ld_lane();
-#pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-        const int32_t i = base + r * LD_WAVE;
-        const bool in = i < a.T;
-        key[r] = in ? key_of(a, i) : 0;
-        at[r] = in && a.at_in ? a.at_in[i] : static_cast<uint32_t>(i);
-        const uint32_t digit = (key[r] >> a.shift) & mask;
-        uint64_t same = __ballot(in);
-        for (int32_t b = 0; b < a.bits; ++b) {
-            const uint64_t set = __ballot((digit >> b) & 1);
-            same &= (digit >> b) & 1 ? set : ~set;
-        }
-        const uint32_t below = ld_mbcnt(same);
-        uint32_t so_far = 0;
-        if (in) so_far = before[wave][digit];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (in && below == 0) before[wave][digit] = static_cast<uint16_t>(so_far + __popcll(same));
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        rank[r] = so_far + below;
-    }
-    __syncthreads();
-    for (int32_t i = threadIdx.x; i < bins; i += kSortThreads) {
-        uint32_t total = 0;
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = before[w][i];
-            before[w][i] = static_cast<uint16_t>(total);
-            total += c;
-        }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-        if (base + r * LD_WAVE < a.T) {
-            const uint32_t digit = (key[r] >> a.shift) & mask;
-            const uint32_t to = first[digit] + before[wave][digit] + rank[r];
-            a.keys_out[to] = key[r];
-            a.at_out[to] = at[r];
-        }
-    }
-}
-
-// ------------------------------------------------------------------- rows
-
-// The sorted tokens are cut into chunks of 4 to 32, a wave for each chunk and block of columns. It adds up, one after the other,
-// the runs of equal ids that begin in its chunk, to their ends where it can see them (64 tokens from the chunk's first on), and
-// writes their rows. A run that goes on further is long: every chunk that it touches leaves a partial sum, and k_join adds those
-// up. Rows that no token names are cleared by workgroups of the same launch.
-constexpr int kRowThreads = 256;
-constexpr int kRowWaves = kRowThreads / LD_WAVE;
-constexpr int kAhead = 8;         // tokens whose rows a wave loads before it adds the first
-constexpr int kMostChunk = 32;
-constexpr int kClearRows = 16;    // rows that a clearing workgroup looks after
-// dout past the 256 MB that the last cache holds is read around it. GPT-2 XL's 52 MB (three batches in turn) 108 us from the cache, 124
-// around it; 537 MB of bf16 at Llama's width 217 and 210, all of one id 269 and 222. Finished rows are always written around it, partial
-// sums never (one id 285 us).
-constexpr int64_t kStreamed = 256 << 20;
-constexpr int kJoinWaves = 8;     // chunks of a joining workgroup
-constexpr int kJoinAlone = 8;     // partial sums that a wave adds up by itself
-
-struct RowArgs {
-    const void* dout;
-    const uint32_t* keys;   // sorted
-    const uint32_t* at;     // the tokens in that order
-    void* grad;
-    float* part;            // [2 * chunks] rows of part_stride: a chunk's sum of the long run that came to it, and of the one that begins in it
-    int64_t dout_stride, grad_stride, part_stride;
-    int32_t T, V, d;
-    int32_t chunk, blocks;  // tokens of a chunk; blocks of columns
-    int32_t adding, clearing;  // workgroups of each kind
-    float scale;
-    int32_t accumulate;
-};
-
-// First of the sorted keys that is at least v.
-__device__ __forceinline__ int32_t lower_bound(const uint32_t* keys, int32_t n, uint32_t v) {
-    int32_t lo = 0;
-    while (n > 0) {
-        const int32_t half = n >> 1;
-        if (keys[lo + half] < v) {
-            lo += half + 1;
-            n -= half + 1;
-        } else {
-            n = half;
-        }
-    }
-    return lo;
-}
-
-// The same, looked for by the wave together: 64 keys at a time.
-__device__ __forceinline__ int32_t wave_lower_bound(const uint32_t* keys, int32_t n, uint32_t v) {
-    int32_t lo = 0;
-    while (n > 0) {
-        const int32_t step = (n + LD_WAVE - 1) / LD_WAVE, i = ld_lane() * step;
-        const int32_t less = __popcll(__ballot(i < n && keys[lo + i] < v));
-        if (less == 0) break;
-        const int32_t skip = (less - 1) * step + 1;
-        lo += skip;
-        n = step - 1 < n - skip ? step - 1 : n - skip;
-    }
-    return lo;
-}
-
 // The columns of a lane: N from `column` on, of which the last `own` are its own. In the row's last vector, which ends with the
 // row, the first are the lane's before (their sums are made twice and written once); in rows of fewer than N columns they are none.
 struct Columns {
@@ -236,6 +46,361 @@ __device__ __forceinline__ void store_columns(typename LdElem<DT>::type* row, Co
         for (int e = 1; e < N; ++e)
             if (e >= N - c.own) row[c.column + e] = x[e];
     }
+}
+
+// Rows cleared by workgroups that a launch of the sort has besides its own: what the chip has to spare there.
+struct Clearing {
+    void* grad;
+    int64_t stride;
+    int32_t d, wide;     // wide: elements of four bytes, else two
+    int32_t from, rows;  // rows [from, from + rows)
+};
+
+template <int DT>
+__device__ __forceinline__ void clear_span(const Clearing& c, int32_t wave, int32_t waves) {
+    constexpr int N = DT == LD_F32 ? 4 : 8;
+    for (int32_t r = wave; r < c.rows; r += waves) {
+        typename LdElem<DT>::type* row = static_cast<typename LdElem<DT>::type*>(c.grad) + static_cast<int64_t>(c.from + r) * c.stride;
+        for (int32_t l = ld_lane(); l * N < c.d; l += LD_WAVE)
+            store_columns<DT, N, true>(row, columns_of<N>(l, c.d), typename LdVec<DT, N>::type(0));
+    }
+}
+
+// Bytes that a launch of the sort clears: about what is written in its time. GPT-2 XL's 16 K tokens without it 97.7 us, with 16 MB 89.5,
+// 32 MB 86.8, 48 MB 88.8. Rows that tokens name are written twice so: at Llama's width 65 K tokens of 32 K rows 182 and 192 us; it is done
+// where there are fewer tokens than rows.
+constexpr int64_t kHidden = 32 << 20;
+
+// Whether a workgroup is one of those, its work then done.
+__device__ __forceinline__ bool cleared(const Clearing& c, int32_t own_blocks) {
+    const int32_t block = static_cast<int32_t>(blockIdx.x) - own_blocks;
+    if (block < 0) return false;
+    const int32_t per = blockDim.x / LD_WAVE, wave = block * per + threadIdx.x / LD_WAVE, waves = (static_cast<int32_t>(gridDim.x) - own_blocks) * per;
+    if (c.wide) clear_span<LD_F32>(c, wave, waves);
+    else clear_span<LD_BF16>(c, wave, waves);
+    return true;
+}
+
+// ------------------------------------------------------------------ sort
+
+// Least significant digit first, and stable. A workgroup finds the rank of its tokens among those of the same digit: a wave takes 64
+// consecutive tokens a round, the lanes of equal digits found by a vote on each bit, and counts what it has had of a digit in shared
+// memory; then the waves' counts are added up.
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / LD_WAVE;
+
+struct SortArgs {
+    const void* ids;         // the first digit's input, else NULL
+    int32_t wide_ids;
+    const uint32_t* keys_in;
+    const uint32_t* at_in;
+    uint32_t* keys_out;
+    uint32_t* at_out;
+    uint32_t* counts;        // [tiles][1 << bits]
+    int64_t V;
+    int32_t T, tiles, per_tile, shift, bits;
+};
+
+// A token's key: its id, or V for one that names no row.
+__device__ __forceinline__ uint32_t key_of(const SortArgs& a, int32_t i) {
+    if (!a.ids) return a.keys_in[i];
+    const int64_t id = a.wide_ids ? static_cast<const int64_t*>(a.ids)[i] : static_cast<const int32_t*>(a.ids)[i];
+    return static_cast<uint32_t>(id >= 0 && id < a.V ? id : a.V);
+}
+
+// The token's place among those of its digit that its wave has had, `seen` (a count for each digit) being moved on.
+__device__ __forceinline__ uint32_t rank_in_wave(uint32_t digit, bool in, int32_t bits, uint16_t* seen) {
+    const uint64_t valid = __ballot(in);
+    uint32_t lo = static_cast<uint32_t>(valid), hi = static_cast<uint32_t>(valid >> 32);
+    for (int32_t b = 0; b < bits; ++b) {
+        const uint32_t mine = static_cast<uint32_t>(static_cast<int32_t>(digit << (31 - b)) >> 31);  // the bit, in every place
+        const uint64_t set = __ballot(mine != 0);
+        lo &= ~(static_cast<uint32_t>(set) ^ mine);
+        hi &= ~(static_cast<uint32_t>(set >> 32) ^ mine);
+    }
+    const uint64_t same = static_cast<uint64_t>(hi) << 32 | lo;
+    const uint32_t below = ld_mbcnt(same);
+    uint32_t before = 0;
+    if (in) before = seen[digit];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (in && below == 0) seen[digit] = static_cast<uint16_t>(before + __popcll(same));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    return before + below;
+}
+
+// A workgroup's exclusive scan of a value a thread; `sh` holds a word for each wave.
+__device__ __forceinline__ uint32_t block_escan(uint32_t x, uint32_t* sh) {
+    const uint32_t upto = ld_wave_iscan(x);
+    const int32_t wave = threadIdx.x / LD_WAVE;
+    if (ld_lane() == LD_WAVE - 1) sh[wave] = upto;
+    __syncthreads();
+    uint32_t from = upto - x;
+    for (int w = 0; w < wave; ++w) from += sh[w];
+    return from;
+}
+
+// Up to 1024 * ROUNDS tokens: all digits by one workgroup, the tokens staying in registers and shared memory. 1024 tokens 5.3 us, 4096 9.8
+// (as tiles 17 to 21); 8192 would be 23 (as tiles 19), the vector units of the one compute unit being busy with the votes.
+constexpr int kAloneBits = 9;                 // most bits of a digit
+constexpr int kAloneBins = 1 << kAloneBits;
+constexpr int kAloneMost = 4 * kSortThreads;
+
+template <int ROUNDS>
+__global__ __launch_bounds__(kSortThreads) void k_sort_alone(SortArgs a, int32_t passes, Clearing c) {
+    __shared__ uint32_t keys[ROUNDS * kSortThreads];
+    __shared__ uint16_t tokens[ROUNDS * kSortThreads];
+    __shared__ uint16_t seen[kSortWaves][kAloneBins];
+    __shared__ uint32_t first[kAloneBins], sh[kSortWaves];
+    const int32_t bins = 1 << a.bits, wave = threadIdx.x / LD_WAVE, base = wave * (LD_WAVE * ROUNDS) + ld_lane();
+    if (cleared(c, 1)) return;
+    uint32_t key[ROUNDS], at[ROUNDS], rank[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int32_t i = base + r * LD_WAVE;
+        key[r] = i < a.T ? key_of(a, i) : 0;
+        at[r] = i;
+    }
+    for (int32_t p = 0; p < passes; ++p) {
+        const int32_t shift = p * a.bits;
+        for (int32_t i = ld_lane(); i < bins; i += LD_WAVE) seen[wave][i] = 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            rank[r] = rank_in_wave((key[r] >> shift) & (bins - 1), base + r * LD_WAVE < a.T, a.bits, seen[wave]);
+        __syncthreads();
+        uint32_t total = 0;
+        const int32_t b = threadIdx.x;
+        if (b < bins) {
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = seen[w][b];
+                seen[w][b] = static_cast<uint16_t>(total);
+                total += c;
+            }
+        }
+        const uint32_t from = block_escan(total, sh);
+        if (b < bins) first[b] = from;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            if (base + r * LD_WAVE < a.T) {
+                const uint32_t digit = (key[r] >> shift) & (bins - 1), to = first[digit] + seen[wave][digit] + rank[r];
+                keys[to] = key[r];
+                tokens[to] = static_cast<uint16_t>(at[r]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int32_t i = base + r * LD_WAVE;
+            if (i < a.T) {
+                key[r] = keys[i];
+                at[r] = tokens[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int32_t i = base + r * LD_WAVE;
+        if (i < a.T) {
+            a.keys_out[i] = key[r];
+            a.at_out[i] = at[r];
+        }
+    }
+}
+
+// More tokens, two launches a digit: every tile counts its digits, then finds from all tiles' counts where each of its digits goes
+// and moves its tokens there. A tile is 2048 tokens, or as many times that as keep the tiles at 256. (16384 tokens of 16 bits 21.7 us, in
+// tiles of 4096 27.4, of 1024 19.6; 262,144 35.7, 35.5 and 45.2. Tiles that count all tokens themselves, without the launch before: no
+// faster at 16384, slower beyond.)
+constexpr int kSortRounds = 2;
+constexpr int kTile = kSortThreads * kSortRounds;
+constexpr int kMostTiles = 256;
+constexpr int kDigitBits = 11;
+constexpr int kBins = 1 << kDigitBits;
+
+__global__ __launch_bounds__(kSortThreads) void k_sort_count(SortArgs a, Clearing c) {
+    __shared__ uint32_t count[kBins];
+    const int32_t bins = 1 << a.bits, base = blockIdx.x * a.per_tile;
+    if (cleared(c, a.tiles)) return;
+    for (int32_t i = threadIdx.x; i < bins; i += kSortThreads) count[i] = 0;
+    __syncthreads();
+    for (int32_t j = 0; j < a.per_tile && base + j < a.T; j += kTile) {
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            const int32_t i = base + j + r * kSortThreads + threadIdx.x;
+            if (i < a.T) atomicAdd(&count[(key_of(a, i) >> a.shift) & (bins - 1)], 1u);
+        }
+    }
+    __syncthreads();
+    for (int32_t i = threadIdx.x; i < bins; i += kSortThreads) a.counts[static_cast<size_t>(blockIdx.x) * bins + i] = count[i];
+}
+
+__global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a, Clearing c) {
+    constexpr int kPer = kBins / kSortThreads, kLoads = 8;
+    __shared__ uint32_t first[kBins];                // where this tile's next tokens of a digit go
+    __shared__ uint16_t seen[kSortWaves][kBins];
+    __shared__ uint32_t part_before[kBins], part_all[kBins], sh[kSortWaves];
+    const int32_t bins = 1 << a.bits, wave = threadIdx.x / LD_WAVE;
+    const uint32_t mask = bins - 1;
+
+    if (cleared(c, a.tiles)) return;
+    // a digit's tokens in the tiles before this one, and in all of them: with fewer digits than threads the tiles are shared out
+    const int32_t parts = bins < kSortThreads ? kSortThreads / bins : 1;
+    for (int32_t i = threadIdx.x; i < bins * parts; i += kSortThreads) {
+        const int32_t b = i & mask, part = i >> a.bits;
+        uint32_t before = 0, all = 0;
+        for (int32_t t0 = part; t0 < a.tiles; t0 += parts * kLoads) {
+            uint32_t c[kLoads];
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                const int32_t t = t0 + u * parts;
+                c[u] = t < a.tiles ? a.counts[static_cast<size_t>(t) * bins + b] : 0;
+            }
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                all += c[u];
+                if (t0 + u * parts < static_cast<int32_t>(blockIdx.x)) before += c[u];
+            }
+        }
+        part_before[i] = before;
+        part_all[i] = all;
+    }
+    __syncthreads();
+    uint32_t before[kPer], all[kPer], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int32_t b = threadIdx.x * kPer + j;
+        before[j] = all[j] = 0;
+        if (b < bins) {
+            for (int32_t p = 0; p < parts; ++p) {
+                before[j] += part_before[(p << a.bits) + b];
+                all[j] += part_all[(p << a.bits) + b];
+            }
+        }
+        sum += all[j];
+    }
+    uint32_t from = block_escan(sum, sh);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int32_t b = threadIdx.x * kPer + j;
+        if (b < bins) first[b] = from + before[j];
+        from += all[j];
+    }
+
+    for (int32_t j = 0; j < a.per_tile; j += kTile) {
+        const int32_t begin = blockIdx.x * a.per_tile + j;
+        if (begin >= a.T) return;
+        const int32_t base = begin + wave * (LD_WAVE * kSortRounds) + ld_lane();
+        uint32_t key[kSortRounds], at[kSortRounds], rank[kSortRounds];
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            const int32_t i = base + r * LD_WAVE;
+            key[r] = i < a.T ? key_of(a, i) : 0;
+            at[r] = i < a.T && a.at_in ? a.at_in[i] : static_cast<uint32_t>(i);
+        }
+        for (int32_t i = ld_lane(); i < bins; i += LD_WAVE) seen[wave][i] = 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) rank[r] = rank_in_wave((key[r] >> a.shift) & mask, base + r * LD_WAVE < a.T, a.bits, seen[wave]);
+        __syncthreads();
+        uint32_t moved[kPer];
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int32_t b = threadIdx.x + k * kSortThreads;
+            moved[k] = 0;
+            if (b < bins) {
+#pragma unroll
+                for (int w = 0; w < kSortWaves; ++w) {
+                    const uint32_t c = seen[w][b];
+                    seen[w][b] = static_cast<uint16_t>(moved[k]);
+                    moved[k] += c;
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            if (base + r * LD_WAVE < a.T) {
+                const uint32_t digit = (key[r] >> a.shift) & mask, to = first[digit] + seen[wave][digit] + rank[r];
+                a.keys_out[to] = key[r];
+                a.at_out[to] = at[r];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int32_t b = threadIdx.x + k * kSortThreads;
+            if (b < bins) first[b] += moved[k];
+        }
+        // the next round's counts are cleared and made by their own waves; its barrier is before `first` is read
+    }
+}
+
+// ------------------------------------------------------------------- rows
+
+// The sorted tokens are cut into chunks of 4 to 32, a wave for each chunk and block of columns. It adds up, one after the other,
+// the runs of equal ids that begin in its chunk, to their ends where it can see them (64 tokens from the chunk's first on), and
+// writes their rows. A run that goes on further is long: every chunk that it touches leaves a partial sum, and k_join adds those
+// up. Rows that no token names are cleared by workgroups of the same launch.
+constexpr int kRowThreads = 256;
+constexpr int kRowWaves = kRowThreads / LD_WAVE;
+constexpr int kAhead = 8;         // tokens whose rows a wave loads before it adds the first
+constexpr int kMostChunk = 32;
+constexpr int kClearRows = 4;     // rows that a clearing workgroup looks after (16: GPT-2 XL 102 us instead of 97)
+// dout past the 256 MB that the last cache holds is read around it. GPT-2 XL's 52 MB (three batches in turn) 108 us from the cache, 124
+// around it; 537 MB of bf16 at Llama's width 217 and 210, all of one id 269 and 222. Finished rows are always written around it, partial
+// sums never (one id 285 us).
+constexpr int64_t kStreamed = 256 << 20;
+constexpr int kJoinWaves = 8;     // chunks of a joining workgroup
+constexpr int kJoinAlone = 8;     // partial sums that a wave adds up by itself
+
+struct RowArgs {
+    const void* dout;
+    const uint32_t* keys;   // sorted
+    const uint32_t* at;     // the tokens in that order
+    void* grad;
+    float* part;            // [2 * chunks] rows of part_stride: a chunk's sum of the long run that came to it, and of the one that begins in it
+    int64_t dout_stride, grad_stride, part_stride;
+    int32_t T, V, d;
+    int32_t chunk, blocks;  // tokens of a chunk; blocks of columns
+    int32_t adding, clearing;  // workgroups of each kind
+    int32_t clear_from;        // rows before it have been cleared, all of them
+    float scale;
+    int32_t accumulate;
+};
+
+// First of the sorted keys that is at least v.
+__device__ __forceinline__ int32_t lower_bound(const uint32_t* keys, int32_t n, uint32_t v) {
+    int32_t lo = 0;
+    while (n > 0) {
+        const int32_t half = n >> 1;
+        if (keys[lo + half] < v) {
+            lo += half + 1;
+            n -= half + 1;
+        } else {
+            n = half;
+        }
+    }
+    return lo;
+}
+
+// The same, looked for by the wave together: 64 keys at a time.
+__device__ __forceinline__ int32_t wave_lower_bound(const uint32_t* keys, int32_t n, uint32_t v) {
+    int32_t lo = 0;
+    while (n > 0) {
+        const int32_t step = (n + LD_WAVE - 1) / LD_WAVE, i = ld_lane() * step;
+        const int32_t less = __popcll(__ballot(i < n && keys[lo + i] < v));
+        if (less == 0) break;
+        const int32_t skip = (less - 1) * step + 1;
+        lo += skip;
+        n = step - 1 < n - skip ? step - 1 : n - skip;
+    }
+    return lo;
 }
 
 // A finished sum to its row.
@@ -310,7 +475,7 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
         const int64_t all = a.adding + a.clearing;
         const int32_t before = static_cast<int32_t>(static_cast<int64_t>(block) * a.clearing / all);
         if (static_cast<int32_t>(static_cast<int64_t>(block + 1) * a.clearing / all) > before) {
-            clear_rows<GT>(a, before * kClearRows);
+            clear_rows<GT>(a, a.clear_from + before * kClearRows);
             return;
         }
         block -= before;
@@ -439,7 +604,7 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
 }
 
 struct Layout {
-    int32_t passes, bits, tiles;
+    int32_t passes, bits, per_tile, tiles;  // one tile: sorted by a workgroup alone
     int32_t chunk, chunks;
     int64_t part_stride;
     size_t keys, at, counts, part, bytes;  // byte offsets: two buffers each of keys and tokens
@@ -449,9 +614,11 @@ Layout layout_of(int64_t T, int64_t V, int32_t d) {
     Layout l;
     int32_t all = 1;
     while ((V >> all) != 0) ++all;  // bits of the keys 0 .. V
-    l.passes = (all + kDigitBits - 1) / kDigitBits;
+    const int32_t most = T <= kAloneMost ? kAloneBits : kDigitBits;
+    l.passes = (all + most - 1) / most;
     l.bits = (all + l.passes - 1) / l.passes;
-    l.tiles = static_cast<int32_t>((T + kTile - 1) / kTile);
+    l.per_tile = T <= kAloneMost ? kAloneMost : static_cast<int32_t>((T + kTile * kMostTiles - 1) / (kTile * kMostTiles)) * kTile;
+    l.tiles = static_cast<int32_t>((T + l.per_tile - 1) / l.per_tile);
     const size_t list = ld_round_up(static_cast<size_t>(T) * 4, 256);
     l.keys = 0;
     l.at = 2 * list;
@@ -459,7 +626,7 @@ Layout layout_of(int64_t T, int64_t V, int32_t d) {
     l.part = ld_round_up(l.counts + (static_cast<size_t>(l.tiles) << l.bits) * 4, 256);
     l.chunk = kMostChunk;
     // few tokens: smaller chunks, so that more waves share them
-    while (l.chunk > 4 && (T / l.chunk) * ((d + 511) / 512) < 2048) l.chunk /= 2;
+    while (l.chunk > 4 && (T / l.chunk) * ((d + 511) / 512) < 2048 && T <= 256 * l.chunk) l.chunk /= 2;
     l.chunks = static_cast<int32_t>((T + l.chunk - 1) / l.chunk);
     l.part_stride = (static_cast<int64_t>(d) + 3) / 4 * 4;
     l.bytes = ld_round_up(l.part + 2 * static_cast<size_t>(l.chunks) * l.part_stride * 4, 256);
@@ -494,22 +661,47 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + l.keys), reinterpret_cast<uint32_t*>(ws + l.keys + l.at / 2)};
     uint32_t* at[2] = {reinterpret_cast<uint32_t*>(ws + l.at), reinterpret_cast<uint32_t*>(ws + l.at + l.at / 2)};
     ld_begin_call();
-    for (int32_t p = 0; p < l.passes && T > 0; ++p) {
-        const SortArgs a = {p == 0 ? ids : nullptr, id_dtype == LD_I64, keys[(p + 1) & 1], p == 0 ? nullptr : at[(p + 1) & 1], keys[p & 1],
-                            at[p & 1], reinterpret_cast<uint32_t*>(ws + l.counts), V, static_cast<int32_t>(T), l.tiles, p * l.bits, l.bits};
-        k_sort_count<<<dim3(l.tiles), dim3(kSortThreads), 0, s>>>(a);
-        if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
-        k_sort_move<<<dim3(l.tiles), dim3(kSortThreads), 0, s>>>(a);
+    SortArgs sort = {ids, id_dtype == LD_I64, nullptr, nullptr, keys[0], at[0], reinterpret_cast<uint32_t*>(ws + l.counts), V,
+                     static_cast<int32_t>(T), l.tiles, l.per_tile, 0, l.bits};
+    Clearing clear = {grad, grad_stride, d, ld_type_bytes(grad_dtype) == 4, 0, 0};
+    const int64_t hidden = accumulate || T > V ? 0 : kHidden / (static_cast<int64_t>(d) * ld_type_bytes(grad_dtype));  // rows a launch
+    const auto blocks_of = [&](int32_t own) {  // of a launch that clears the next rows as well
+        clear.from += clear.rows;
+        clear.rows = static_cast<int32_t>(V - clear.from < hidden ? V - clear.from : hidden);
+        const int32_t more = (clear.rows + kSortWaves - 1) / kSortWaves;
+        return dim3(own + (more < 256 ? more : 256));
+    };
+    int32_t last = 0;
+    if (l.tiles == 1) {
+        const dim3 grid = blocks_of(1);
+        if (T <= kSortThreads) k_sort_alone<1><<<grid, dim3(kSortThreads), 0, s>>>(sort, l.passes, clear);
+        else if (T <= 2 * kSortThreads) k_sort_alone<2><<<grid, dim3(kSortThreads), 0, s>>>(sort, l.passes, clear);
+        else k_sort_alone<4><<<grid, dim3(kSortThreads), 0, s>>>(sort, l.passes, clear);
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
     }
-    const int32_t last = (l.passes + 1) & 1;
+    for (int32_t p = 0; p < l.passes && l.tiles > 1; ++p) {
+        last = p & 1;
+        sort.keys_out = keys[last];
+        sort.at_out = at[last];
+        sort.shift = p * l.bits;
+        dim3 grid = blocks_of(l.tiles);
+        k_sort_count<<<grid, dim3(kSortThreads), 0, s>>>(sort, clear);
+        if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
+        grid = blocks_of(l.tiles);
+        k_sort_move<<<grid, dim3(kSortThreads), 0, s>>>(sort, clear);
+        if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
+        sort.ids = nullptr;
+        sort.keys_in = keys[last];
+        sort.at_in = at[last];
+    }
+    clear.from += clear.rows;
     const int32_t columns = LD_WAVE * (dtype == LD_F32 ? 4 : 8), blocks = static_cast<int32_t>((static_cast<int64_t>(d) + columns - 1) / columns);
     const int64_t adding = (static_cast<int64_t>(l.chunks) * blocks + kRowWaves - 1) / kRowWaves;
-    const int64_t clearing = accumulate ? 0 : (V + kClearRows - 1) / kClearRows;
+    const int64_t clearing = accumulate ? 0 : (V - clear.from + kClearRows - 1) / kClearRows;
     if (adding + clearing > INT32_MAX / kRowWaves) return LD_ERR_RANGE;
     const RowArgs a = {dout, keys[last], at[last], grad, reinterpret_cast<float*>(ws + l.part), dout_stride, grad_stride, l.part_stride,
                        static_cast<int32_t>(T), static_cast<int32_t>(V), d, l.chunk, blocks, static_cast<int32_t>(adding),
-                       static_cast<int32_t>(clearing), scale, accumulate};
+                       static_cast<int32_t>(clearing), clear.from, scale, accumulate};
     const dim3 grid(static_cast<uint32_t>(adding + clearing));
     const bool streamed = T * static_cast<int64_t>(d) * ld_type_bytes(dtype) > kStreamed;
     ld_with_type(dtype, [&](auto type) {

@@ -180,7 +180,9 @@ def test_embed_grad_types(T, V, d, kind, dtype, grad_dtype):
 
 
 @pytest.mark.parametrize("T,V,d,kind", [(70001, 50257, 24, "heavy"), (40000, 1024, 100, "descending"), (65536, 3, 32, "uniform"),
-                                        (300000, 9, 4, "heavy"), (20000, 5000, 520, "one"), (16385, 4_200_000, 3, "uniform")])
+                                        (300000, 9, 4, "heavy"), (20000, 5000, 520, "one"), (16385, 4_200_000, 3, "uniform"),
+                                        (1024, 300_000, 20, "outside"), (1025, 600, 20, "heavy"), (16384, 50257, 9, "outside"),
+                                        (16384, 300_000, 3, "uniform"), (1_100_000, 3000, 2, "heavy"), (2_200_000, 70_000, 1, "outside")])
 def test_embed_grad_of_many_tokens(T, V, d, kind):
     check_grad(T, V, d, kind, BF16, F32, seed=5)
 
