@@ -4,9 +4,11 @@
 //   S = sum over all elements of x^2;  norm = sqrt(S);  factor = norm > max_norm ? max_norm / norm : 1
 //   out = round(x * factor)
 //
-// Squares and sums are 64 bits wide: the square of a 32-bit value is exact there and can neither overflow nor vanish.
-// Bound by memory: n elements read for S, read again and written for the clipped values; a gradient in place under the limit
-// is not touched a second time.
+// Squares and sums are 64 bits wide: the square of a 32-bit value is exact there and can neither overflow nor vanish, and the
+// conversion and the addition cost nothing beside the memory (6.4 TB/s of bf16). Bound by memory: n elements read for S, read
+// again and written for the clipped values; a gradient in place under the limit is not touched a second time. GPT-2 XL's 580
+// bf16 gradients (3.1 GB) 485 us for the norm, 1015 for the clipped copy (6.1 TB/s); that the second reading begins where the
+// first one ended, in what the last cache still holds, changed nothing.
 #include <math.h>
 
 #include <type_traits>
@@ -18,9 +20,14 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;                 // vectors per thread and piece
 constexpr int kTensorGroup = 16;
-constexpr int kTensorGroups = 10;
+constexpr int kTensorGroups = 11;
 constexpr int kTensorsPerLaunch = kTensorGroup * kTensorGroups;
 constexpr int kNormGrid = 2048;            // workgroups of a launch, each with a partial sum
+// Workgroups of a launch that clips in place, where all may find that nothing is to be done: GPT-2 XL under the limit 494 us in all, clipping
+// 1048; with one for every piece, as out of place, 520 and 989, with 2048 483 and 1122.
+constexpr int kInPlaceGrid = 16384;
+constexpr int64_t kAloneElems = 32768;     // up to here one workgroup does the whole call
+constexpr int kAloneThreads = 1024;
 
 // The tensors of a launch, in its arguments. A tensor is cut into pieces of PIECE elements, the last one ragged.
 struct TensorBatch {
@@ -59,42 +66,102 @@ __device__ __forceinline__ double block_sum(double x, double* sh) {
     return total;
 }
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void k_sum_squares(TensorBatch b, double* __restrict__ part) {
-    constexpr int N = DT == LD_F32 ? 4 : 8;
+// Where a piece lies, and its elements.
+struct Piece {
+    int tensor;
+    int64_t first;
+    int32_t have;
+};
+
+template <int N>
+__device__ __forceinline__ Piece piece_of(const TensorBatch& b, int32_t p) {
+    const int t = tensor_of(b, p);
+    return {t, static_cast<int64_t>(p - b.first_piece[t]) * piece_elems<N>(),
+            p + 1 == b.first_piece[t + 1] ? b.last[t] : piece_elems<N>()};
+}
+
+// The squares of a thread's part of a piece, THREADS sharing it. Read around the caches: 81 us instead of 90 for 498 MB of fp32.
+template <int DT, int N, int THREADS>
+__device__ __forceinline__ double squares(const TensorBatch& b, int32_t p, double sum) {
     typedef LdVec<DT, N> V;
-    __shared__ double sh[kThreads / LD_WAVE];
-    double sum = 0.0;
-    for (int32_t p = blockIdx.x; p < b.first_of_group[0]; p += gridDim.x) {
-        const int t = tensor_of(b, p);
-        const typename V::elem* src = static_cast<const typename V::elem*>(b.tensor[t].src) +
-                                      static_cast<int64_t>(p - b.first_piece[t]) * piece_elems<N>();
-        const int32_t have = p + 1 == b.first_piece[t + 1] ? b.last[t] : piece_elems<N>();
+    const Piece at = piece_of<N>(b, p);
+    const typename V::elem* src = static_cast<const typename V::elem*>(b.tensor[at.tensor].src) + at.first;
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int32_t at = (u * kThreads + threadIdx.x) * N;
-            if (at + N <= have) {
-                const typename V::wide x = V::widen(*reinterpret_cast<const typename V::type*>(src + at));
+    for (int u = 0; u < piece_elems<N>() / N / THREADS; ++u) {
+        const int32_t i = (u * THREADS + threadIdx.x) * N;
+        if (i + N <= at.have) {
+            const typename V::wide x = V::widen(__builtin_nontemporal_load(reinterpret_cast<const typename V::type*>(src + i)));
 #pragma unroll
-                for (int e = 0; e < N; ++e) sum = fma(static_cast<double>(x[e]), static_cast<double>(x[e]), sum);
-            } else {
-                for (int32_t e = at; e < have && e < at + N; ++e) {
-                    const double x = static_cast<double>(static_cast<float>(src[e]));
-                    sum = fma(x, x, sum);
-                }
+            for (int e = 0; e < N; ++e) sum = fma(static_cast<double>(x[e]), static_cast<double>(x[e]), sum);
+        } else {
+            for (int32_t e = i; e < at.have && e < i + N; ++e) {
+                const double x = static_cast<double>(static_cast<float>(src[e]));
+                sum = fma(x, x, sum);
             }
         }
     }
+    return sum;
+}
+
+// A thread's part of a piece scaled.
+template <int DT, int OT, int N, int THREADS>
+__device__ __forceinline__ void scale_piece(const TensorBatch& b, int32_t p, float factor) {
+    constexpr int kVectors = piece_elems<N>() / N / THREADS;
+    typedef LdVec<DT, N> V;
+    typedef LdVec<OT, N> O;
+    const Piece at = piece_of<N>(b, p);
+    const typename V::elem* src = static_cast<const typename V::elem*>(b.tensor[at.tensor].src) + at.first;
+    typename O::elem* dst = static_cast<typename O::elem*>(b.tensor[at.tensor].dst) + at.first;
+    if (at.have == piece_elems<N>()) {
+        const typename V::type* v = reinterpret_cast<const typename V::type*>(src) + threadIdx.x;
+        typename O::type* o = reinterpret_cast<typename O::type*>(dst) + threadIdx.x;
+        typename V::type x[kVectors];
+#pragma unroll
+        for (int u = 0; u < kVectors; ++u) x[u] = __builtin_nontemporal_load(v + u * THREADS);
+#pragma unroll
+        for (int u = 0; u < kVectors; ++u) __builtin_nontemporal_store(O::narrow(V::widen(x[u]) * factor), o + u * THREADS);
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < kVectors; ++u) {
+        const int32_t i = (u * THREADS + threadIdx.x) * N;
+        if (i + N <= at.have) {
+            const typename V::type x = *reinterpret_cast<const typename V::type*>(src + i);
+            *reinterpret_cast<typename O::type*>(dst + i) = O::narrow(V::widen(x) * factor);
+        } else {
+            for (int32_t e = i; e < at.have && e < i + N; ++e)
+                dst[e] = static_cast<typename O::elem>(static_cast<float>(src[e]) * factor);
+        }
+    }
+}
+
+// A norm that is not finite clips nothing: the caller sees it in the norm.
+__device__ __forceinline__ float factor_of(double sumsq, float max_norm) {
+    const double norm = sqrt(sumsq);
+    return norm > max_norm && norm < __builtin_huge_val() ? static_cast<float>(max_norm / norm) : 1.0f;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void k_sum_squares(TensorBatch b, double* __restrict__ part) {
+    __shared__ double sh[kThreads / LD_WAVE];
+    double sum = 0.0;
+    for (int32_t p = blockIdx.x; p < b.first_of_group[0]; p += gridDim.x) sum = squares<DT, DT == LD_F32 ? 4 : 8, kThreads>(b, p, sum);
     sum = block_sum(sum, sh);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(1024) void k_norm_finish(const double* __restrict__ part, int32_t count, int32_t accumulate,
-                                                      double* __restrict__ sumsq, float* __restrict__ norm) {
-    __shared__ double sh[1024 / LD_WAVE];
+// The sum of `count` partial sums, by a workgroup; the same in every workgroup of THREADS threads.
+__device__ __forceinline__ double sum_of(const double* __restrict__ part, int32_t count, double* sh) {
+    if (count == 1) return *part;
     double sum = 0.0;
     for (int32_t i = threadIdx.x; i < count; i += blockDim.x) sum += part[i];
-    sum = block_sum(sum, sh);
+    return block_sum(sum, sh);
+}
+
+__global__ __launch_bounds__(kAloneThreads) void k_norm_finish(const double* __restrict__ part, int32_t count, int32_t accumulate,
+                                                               double* __restrict__ sumsq, float* __restrict__ norm) {
+    __shared__ double sh[kAloneThreads / LD_WAVE];
+    double sum = sum_of(part, count, sh);
     if (threadIdx.x == 0) {
         if (accumulate) sum += *sumsq;
         *sumsq = sum;
@@ -102,33 +169,31 @@ __global__ __launch_bounds__(1024) void k_norm_finish(const double* __restrict__
     }
 }
 
+// Every workgroup adds up the partial sums itself (`count` of them; one: the sum is known). norm: written where it is not yet.
 template <int DT, int OT>
-__global__ __launch_bounds__(kThreads) void k_clip(TensorBatch b, const double* __restrict__ sumsq, float max_norm, int32_t in_place) {
-    constexpr int N = DT == LD_F32 || OT == LD_F32 ? 4 : 8;
-    typedef LdVec<DT, N> V;
-    typedef LdVec<OT, N> O;
-    const double norm = sqrt(*sumsq);
-    // a norm that is not finite clips nothing: the caller sees it in the norm
-    const float factor = norm > max_norm && norm < __builtin_huge_val() ? static_cast<float>(max_norm / norm) : 1.0f;
+__global__ __launch_bounds__(kThreads) void k_clip(TensorBatch b, const double* __restrict__ part, int32_t count, float max_norm, int32_t in_place,
+                                                   float* __restrict__ norm) {
+    __shared__ double sh[kThreads / LD_WAVE];
+    const double sum = sum_of(part, count, sh);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(sqrt(sum));
+    const float factor = factor_of(sum, max_norm);
     if (in_place && factor == 1.0f) return;
-    for (int32_t p = blockIdx.x; p < b.first_of_group[0]; p += gridDim.x) {
-        const int t = tensor_of(b, p);
-        const int64_t first = static_cast<int64_t>(p - b.first_piece[t]) * piece_elems<N>();
-        const typename V::elem* src = static_cast<const typename V::elem*>(b.tensor[t].src) + first;
-        typename O::elem* dst = static_cast<typename O::elem*>(b.tensor[t].dst) + first;
-        const int32_t have = p + 1 == b.first_piece[t + 1] ? b.last[t] : piece_elems<N>();
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int32_t at = (u * kThreads + threadIdx.x) * N;
-            if (at + N <= have) {
-                const typename V::wide x = V::widen(*reinterpret_cast<const typename V::type*>(src + at));
-                *reinterpret_cast<typename O::type*>(dst + at) = O::narrow(x * factor);
-            } else {
-                for (int32_t e = at; e < have && e < at + N; ++e)
-                    dst[e] = static_cast<typename O::elem>(static_cast<float>(src[e]) * factor);
-            }
-        }
-    }
+    for (int32_t p = blockIdx.x; p < b.first_of_group[0]; p += gridDim.x)
+        scale_piece<DT, OT, DT == LD_F32 || OT == LD_F32 ? 4 : 8, kThreads>(b, p, factor);
+}
+
+// A small call by one workgroup.
+template <int DT, int OT>
+__global__ __launch_bounds__(kAloneThreads) void k_clip_alone(TensorBatch b, float max_norm, int32_t in_place, float* __restrict__ norm) {
+    constexpr int N = DT == LD_F32 || OT == LD_F32 ? 4 : 8;
+    __shared__ double sh[kAloneThreads / LD_WAVE];
+    double sum = 0.0;
+    for (int32_t p = 0; p < b.first_of_group[0]; ++p) sum = squares<DT, N, kAloneThreads>(b, p, sum);
+    sum = block_sum(sum, sh);
+    if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(sum));
+    const float factor = factor_of(sum, max_norm);
+    if (in_place && factor == 1.0f) return;
+    for (int32_t p = 0; p < b.first_of_group[0]; ++p) scale_piece<DT, OT, N, kAloneThreads>(b, p, factor);
 }
 
 // Tensors [t, ...) of the lists as a launch takes them, in pieces of `piece` elements; t moves behind them.
@@ -176,9 +241,9 @@ size_t partials_of(int32_t n_tensors) {
     return static_cast<size_t>((n_tensors + kTensorsPerLaunch - 1) / kTensorsPerLaunch) * kNormGrid;
 }
 
-ld_status sum_squares(const void* const* grad, const int64_t* n_elems, int32_t n_tensors, int32_t dtype, int32_t accumulate,
-                      double* sumsq, float* norm, double* part, hipStream_t s) {
-    int32_t count = 0;
+// Enqueues the partial sums; `count` of them are left in `part`.
+ld_status sum_squares(const void* const* grad, const int64_t* n_elems, int32_t n_tensors, int32_t dtype, double* part, int32_t& count, hipStream_t s) {
+    count = 0;
     for (int32_t t = 0; t < n_tensors;) {
         TensorBatch b;
         next_batch(b, grad, nullptr, n_elems, n_tensors, dtype == LD_F32 ? piece_elems<4>() : piece_elems<8>(), t);
@@ -188,23 +253,31 @@ ld_status sum_squares(const void* const* grad, const int64_t* n_elems, int32_t n
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
         count += grid;
     }
-    k_norm_finish<<<dim3(1), dim3(1024), 0, s>>>(part, count, accumulate, sumsq, norm);
+    return LD_OK;
+}
+
+ld_status finish(const double* part, int32_t count, int32_t accumulate, double* sumsq, float* norm, hipStream_t s) {
+    k_norm_finish<<<dim3(1), dim3(kAloneThreads), 0, s>>>(part, count, accumulate, sumsq, norm);
     return ld_launch_status();
 }
 
+// Enqueues the scaling by `count` partial sums; with `alone` the sums as well, the call being small.
 ld_status clip(const void* const* grad, void* const* out, const int64_t* n_elems, int32_t n_tensors, int32_t dtype, int32_t out_dtype,
-               const double* sumsq, float max_norm, hipStream_t s) {
+               const double* part, int32_t count, float max_norm, float* norm, bool alone, hipStream_t s) {
+    const int32_t piece = dtype == LD_F32 || out_dtype == LD_F32 ? piece_elems<4>() : piece_elems<8>();
     for (int32_t t = 0; t < n_tensors;) {
         const int32_t from = t;
         TensorBatch b;
-        next_batch(b, grad, out, n_elems, n_tensors, dtype == LD_F32 || out_dtype == LD_F32 ? piece_elems<4>() : piece_elems<8>(), t);
-        if (b.first_of_group[0] == 0) continue;
+        next_batch(b, grad, out, n_elems, n_tensors, piece, t);
+        const int32_t pieces = b.first_of_group[0];
+        if (pieces == 0 && !alone) continue;
         int32_t in_place = dtype == out_dtype;
         for (int32_t i = from; i < t; ++i) in_place &= n_elems[i] == 0 || grad[i] == out[i];
-        const int32_t grid = b.first_of_group[0] < kNormGrid ? b.first_of_group[0] : kNormGrid;
+        const dim3 grid(in_place && pieces > kInPlaceGrid ? kInPlaceGrid : pieces);
         ld_with_type(dtype, [&](auto type) {
             ld_with_type(out_dtype, [&](auto out_type) {
-                k_clip<type, out_type><<<dim3(grid), dim3(kThreads), 0, s>>>(b, sumsq, max_norm, in_place);
+                if (alone) k_clip_alone<type, out_type><<<dim3(1), dim3(kAloneThreads), 0, s>>>(b, max_norm, in_place, norm);
+                else k_clip<type, out_type><<<grid, dim3(kThreads), 0, s>>>(b, part, count, max_norm, in_place, norm);
             });
         });
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
@@ -227,8 +300,11 @@ extern "C" ld_status ld_grad_norm(const void* const* grad, const int64_t* n_elem
     if (!ld_aligned(sumsq, 8) || !ld_aligned(norm, 4)) return LD_ERR_ALIGN;
     if (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < ld_grad_norm_workspace(n_tensors)) return LD_ERR_WORKSPACE;
     ld_begin_call();
-    return sum_squares(grad, n_elems, n_tensors, dtype, accumulate, sumsq, norm, static_cast<double*>(workspace),
-                       static_cast<hipStream_t>(stream));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    double* part = static_cast<double*>(workspace);
+    int32_t count;
+    const ld_status summed = sum_squares(grad, n_elems, n_tensors, dtype, part, count, s);
+    return summed != LD_OK ? summed : finish(part, count, accumulate, sumsq, norm, s);
 }
 
 extern "C" ld_status ld_clip_grads(const void* const* grad, void* const* out, const int64_t* n_elems, int32_t n_tensors, int32_t dtype,
@@ -239,22 +315,31 @@ extern "C" ld_status ld_clip_grads(const void* const* grad, void* const* out, co
     if (!sumsq) return LD_ERR_NULL;
     if (!ld_aligned(sumsq, 8)) return LD_ERR_ALIGN;
     ld_begin_call();
-    return clip(grad, out, n_elems, n_tensors, dtype, out_dtype, sumsq, max_norm, static_cast<hipStream_t>(stream));
+    return clip(grad, out, n_elems, n_tensors, dtype, out_dtype, sumsq, 1, max_norm, nullptr, false, static_cast<hipStream_t>(stream));
 }
 
 extern "C" ld_status ld_clip_grad_norm(const void* const* grad, void* const* out, const int64_t* n_elems, int32_t n_tensors, int32_t dtype,
                                        int32_t out_dtype, float max_norm, float* norm, void* workspace, size_t workspace_bytes,
                                        ld_stream stream) {
-    const ld_status st = check_lists(grad, out, true, n_elems, n_tensors, dtype, out_dtype);
+    ld_status st = check_lists(grad, out, true, n_elems, n_tensors, dtype, out_dtype);
     if (st != LD_OK) return st;
     if (!(max_norm >= 0.0f)) return LD_ERR_RANGE;
     if (!norm) return LD_ERR_NULL;
     if (!ld_aligned(norm, 4)) return LD_ERR_ALIGN;
     if (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < ld_grad_norm_workspace(n_tensors)) return LD_ERR_WORKSPACE;
     ld_begin_call();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    int64_t total = 0;
+    for (int32_t t = 0; t < n_tensors; ++t) total += n_elems[t];
+    if (n_tensors > 0 && n_tensors <= kTensorsPerLaunch && total <= kAloneElems)
+        return clip(grad, out, n_elems, n_tensors, dtype, out_dtype, nullptr, 0, max_norm, norm, true, s);
     double* part = static_cast<double*>(workspace);
     double* sumsq = part + partials_of(n_tensors);
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    const ld_status summed = sum_squares(grad, n_elems, n_tensors, dtype, 0, sumsq, norm, part, s);
-    return summed != LD_OK ? summed : clip(grad, out, n_elems, n_tensors, dtype, out_dtype, sumsq, max_norm, s);
+    int32_t count;
+    st = sum_squares(grad, n_elems, n_tensors, dtype, part, count, s);
+    if (st != LD_OK) return st;
+    // up to a piece a workgroup, the partial sums are so few that whoever clips adds them up: a launch less (1 M elements 10.4 -> 9.0 us)
+    if (count > 0 && count < kNormGrid) return clip(grad, out, n_elems, n_tensors, dtype, out_dtype, part, count, max_norm, norm, false, s);
+    st = finish(part, count, 0, sumsq, norm, s);
+    return st != LD_OK ? st : clip(grad, out, n_elems, n_tensors, dtype, out_dtype, sumsq, 1, max_norm, nullptr, false, s);
 }

@@ -161,10 +161,16 @@ def _check(fn: str, status: int) -> None:
         raise LowDiffError(fn, status)
 
 
+# the current stream's handle without an object around it, where torch has that (0.3 us of a call instead of 2.9)
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> ctypes.c_void_p:
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    if _current_raw_stream is not None:
+        return ctypes.c_void_p(_current_raw_stream(torch.cuda.current_device()))
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
 def _dev(t: Optional[torch.Tensor], dtype, name: str) -> ctypes.c_void_p:
