@@ -344,13 +344,15 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a, Clearing
 // ------------------------------------------------------------------- rows
 
 // The sorted tokens are cut into chunks of 4 to 32, a wave for each chunk and block of columns. It adds up, one after the other,
-// the runs of equal ids that begin in its chunk, to their ends where it can see them (64 tokens from the chunk's first on), and
-// writes their rows. A run that goes on further is long: every chunk that it touches leaves a partial sum, and k_join adds those
+// the runs of equal ids that begin in its chunk, to their ends where it can see them (in a window of 16 to 64 tokens from the
+// chunk's first on), and writes their rows. A run that goes on further is long: every chunk that it touches leaves a partial sum, and k_join adds those
 // up. Rows that no token names are cleared by workgroups of the same launch.
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / LD_WAVE;
-constexpr int kAhead = 8;         // tokens whose rows a wave loads before it adds the first
-constexpr int kMostChunk = 32;
+// Tokens whose rows a wave loads before it adds the first; where sums are added to what is there, the rows of grad that they end in with
+// them. (Read when a run is done instead, one after the other: 16 K tokens of GPT-2 XL added 63 us instead of 58. 12 or 16 tokens: 85 -> 92 us
+// without adding.)
+constexpr int kAhead = 8;
 constexpr int kClearRows = 4;     // rows that a clearing workgroup looks after (16: GPT-2 XL 102 us instead of 97)
 // dout past the 256 MB that the last cache holds is read around it. GPT-2 XL's 52 MB (three batches in turn) 108 us from the cache, 124
 // around it; 537 MB of bf16 at Llama's width 217 and 210, all of one id 269 and 222. Finished rows are always written around it, partial
@@ -358,6 +360,7 @@ constexpr int kClearRows = 4;     // rows that a clearing workgroup looks after 
 constexpr int64_t kStreamed = 256 << 20;
 constexpr int kJoinWaves = 8;     // chunks of a joining workgroup
 constexpr int kJoinAlone = 8;     // partial sums that a wave adds up by itself
+constexpr int kJoinAhead = 16;    // else partial sums that each of the waves loads before it adds the first (8: 16384 tokens of one id 83 us instead of 63)
 
 struct RowArgs {
     const void* dout;
@@ -367,11 +370,10 @@ struct RowArgs {
     float* part;            // [2 * chunks] rows of part_stride: a chunk's sum of the long run that came to it, and of the one that begins in it
     int64_t dout_stride, grad_stride, part_stride;
     int32_t T, V, d;
-    int32_t chunk, blocks;  // tokens of a chunk; blocks of columns
+    int32_t chunk, window, blocks;  // tokens of a chunk, and those that it sees from its first on; blocks of columns
     int32_t adding, clearing;  // workgroups of each kind
     int32_t clear_from;        // rows before it have been cleared, all of them
     float scale;
-    int32_t accumulate;
 };
 
 // First of the sorted keys that is at least v.
@@ -403,19 +405,18 @@ __device__ __forceinline__ int32_t wave_lower_bound(const uint32_t* keys, int32_
     return lo;
 }
 
-// A finished sum to its row.
-template <int GT, int N>
-__device__ __forceinline__ void write_row(const RowArgs& a, uint32_t v, Columns c, typename LdVec<GT, N>::wide sum) {
-    typename LdElem<GT>::type* row = static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(v) * a.grad_stride;
-    if (a.accumulate) {
-        const typename LdVec<GT, N>::wide old = LdVec<GT, N>::widen(load_columns<GT, N, false>(row, c));
+template <int GT>
+__device__ __forceinline__ typename LdElem<GT>::type* grad_row(const RowArgs& a, uint32_t v) {
+    return static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(v) * a.grad_stride;
+}
+
+// A finished sum to its row, added to what the row held where ADD.
+template <int GT, int N, bool ADD>
+__device__ __forceinline__ void write_row(const RowArgs& a, uint32_t v, Columns c, typename LdVec<GT, N>::wide sum, typename LdVec<GT, N>::type held) {
+    const typename LdVec<GT, N>::wide old = LdVec<GT, N>::widen(held);
 #pragma unroll
-        for (int e = 0; e < N; ++e) sum[e] = __fmaf_rn(a.scale, sum[e], old[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) sum[e] = a.scale * sum[e];
-    }
-    store_columns<GT, N, true>(row, c, LdVec<GT, N>::narrow(sum));
+    for (int e = 0; e < N; ++e) sum[e] = ADD ? __fmaf_rn(a.scale, sum[e], old[e]) : a.scale * sum[e];
+    store_columns<GT, N, true>(grad_row<GT>(a, v), c, LdVec<GT, N>::narrow(sum));
 }
 
 template <int GT>
@@ -459,17 +460,18 @@ __device__ __forceinline__ Runs runs_of(const RowArgs& a, int32_t from) {
     const uint32_t below = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(last), static_cast<int>(r.key), kShr1, 0xf, 0xf, false));
     const uint32_t below_before = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(before), kShr1, 0xf, 0xf, false));
     r.own = (1ull << a.chunk) - 1;
-    r.heads = __ballot(r.key != below);
+    r.heads = __ballot(r.key != below && ld_lane() < a.window);
     const uint64_t heads_before = __ballot(before != below_before) & ~1ull;
     r.began = heads_before ? from - 1 - __builtin_clzll(heads_before) : -1;
     r.valid = __popcll(__ballot(r.key < static_cast<uint32_t>(a.V)));
     return r;
 }
 
-template <int DT, int GT, bool STREAM>
+template <int DT, int GT, bool STREAM, bool ADD>
 __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
     constexpr int N = DT == LD_F32 ? 4 : 8;
     typedef LdVec<DT, N> X;
+    typedef LdVec<GT, N> G;
     int32_t block = blockIdx.x;
     if (a.clearing > 0) {  // the two kinds mixed evenly
         const int64_t all = a.adding + a.clearing;
@@ -494,7 +496,7 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
     if (!(r.heads & 1)) {
         const int32_t left = later ? __builtin_ctzll(later) : LD_WAVE;
         // whether the chunk that this run began in sees its end, and so adds it up
-        if (r.began >= 0 && from + left < (r.began & -a.chunk) + LD_WAVE) i = left;
+        if (r.began >= 0 && from + left < (r.began & -a.chunk) + a.window) i = left;
         else came = true;
     }
     // the last run that begins here is long, or none begins; else it is followed to its end
@@ -505,45 +507,79 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
     float* part = a.part + 2 * static_cast<int64_t>(c) * a.part_stride;
     typename X::wide sum = typename X::wide(0.0f);
     int32_t run = i;  // where the run being added up begins
+    typename G::type held = typename G::type(0);  // its row of grad, where that is added to
+    const auto key_at = [&](int32_t j) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), j)); };
     const auto load = [&](int32_t j) {
         return load_columns<DT, N, STREAM>(dout + static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), j)) * a.dout_stride, cols);
     };
-    const auto add = [&](int32_t j, typename X::type x) {
-        if (j > run && (r.heads >> j & 1)) {
-            if (came) store_columns<LD_F32, N, false>(part, cols, sum);
-            else write_row<GT, N>(a, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), run)), cols, sum);
-            came = false;
-            run = j;
+    const auto begins = [&](int32_t j) { return (r.heads >> j & 1) != 0; };
+    const auto add = [&](int32_t j, typename X::type x, typename G::type row) {
+        if (begins(j)) {
+            if (j > run) {
+                if (came) store_columns<LD_F32, N, false>(part, cols, sum);
+                else write_row<GT, N, ADD>(a, key_at(run), cols, sum, held);
+                came = false;
+                run = j;
+            }
             sum = X::widen(x);
+            held = row;
         } else {
             sum += X::widen(x);
         }
     };
     for (; i + kAhead <= end; i += kAhead) {
         typename X::type x[kAhead];
+        typename G::type row[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) x[u] = load(i + u);
+        for (int u = 0; u < kAhead; ++u) {
+            x[u] = load(i + u);
+            row[u] = typename G::type(0);
+            if (ADD && begins(i + u)) row[u] = load_columns<GT, N, false>(grad_row<GT>(a, key_at(i + u)), cols);
+        }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) add(i + u, x[u]);
+        for (int u = 0; u < kAhead; ++u) add(i + u, x[u], row[u]);
     }
     if (i < end) {
         typename X::type x[kAhead - 1];
+        typename G::type row[kAhead - 1];
+#pragma unroll
+        for (int u = 0; u < kAhead - 1; ++u) {
+            row[u] = typename G::type(0);
+            if (i + u < end) {
+                x[u] = load(i + u);
+                if (ADD && begins(i + u)) row[u] = load_columns<GT, N, false>(grad_row<GT>(a, key_at(i + u)), cols);
+            }
+        }
 #pragma unroll
         for (int u = 0; u < kAhead - 1; ++u)
-            if (i + u < end) x[u] = load(i + u);
-#pragma unroll
-        for (int u = 0; u < kAhead - 1; ++u)
-            if (i + u < end) add(i + u, x[u]);
+            if (i + u < end) add(i + u, x[u], row[u]);
     }
     if (run >= end) return;
     if (came) store_columns<LD_F32, N, false>(part, cols, sum);
     else if (goes_on && end == a.chunk) store_columns<LD_F32, N, false>(part + a.part_stride, cols, sum);
-    else write_row<GT, N>(a, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), run)), cols, sum);
+    else write_row<GT, N, ADD>(a, key_at(run), cols, sum, held);
+}
+
+// Partial sums from, from + step, ... up to last of a long run that begins in chunk `first`.
+template <int AHEAD>
+__device__ __forceinline__ ld_f32x4 sum_parts(const RowArgs& a, Columns cols, int32_t first, int32_t from, int32_t last, int32_t step) {
+    ld_f32x4 sum = ld_f32x4(0.0f);
+    for (int32_t j = from; j <= last; j += step * AHEAD) {
+        ld_f32x4 x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t k = static_cast<int64_t>(j) + u * step;
+            x[u] = k <= last ? load_columns<LD_F32, 4, false>(a.part + (2 * k + (k == first)) * a.part_stride, cols) : ld_f32x4(0.0f);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) sum += x[u];
+    }
+    return sum;
 }
 
 // Adds up the partial sums of long runs, each from the chunk that it begins in to the one that it ends in, in their order. A wave
 // looks at a chunk, with 256 columns; what it would be long busy with is shared by the workgroup's waves, which take partial sums in turn.
-template <int GT>
+template <int GT, bool ADD>
 __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_t chunks) {
     constexpr int N = 4;
     __shared__ ld_f32x4 sh[kJoinWaves][LD_WAVE];
@@ -551,20 +587,6 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
     __shared__ uint32_t shared_run[kJoinWaves];
     const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LD_WAVE), c0 = blockIdx.x * kJoinWaves, c = c0 + wave;
     const Columns cols = columns_of<N>(blockIdx.y * LD_WAVE + ld_lane(), a.d);
-    const auto sum_of = [&](int32_t first, int32_t from, int32_t last, int32_t step) {
-        ld_f32x4 sum = ld_f32x4(0.0f);
-        for (int32_t j = from; j <= last; j += step * kJoinAlone) {
-            ld_f32x4 x[kJoinAlone];
-#pragma unroll
-            for (int u = 0; u < kJoinAlone; ++u) {
-                const int64_t k = j + u * step;
-                x[u] = k <= last ? load_columns<LD_F32, N, false>(a.part + (2 * k + (k == first)) * a.part_stride, cols) : ld_f32x4(0.0f);
-            }
-#pragma unroll
-            for (int u = 0; u < kJoinAlone; ++u) sum += x[u];
-        }
-        return sum;
-    };
     int32_t last = -1;
     uint32_t run = 0;
     if (c < chunks) {
@@ -585,19 +607,23 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
     }
     __syncthreads();
     if (last >= 0 && alone) {
-        const ld_f32x4 sum = sum_of(c, c, last, 1);
-        write_row<GT, N>(a, run, cols, sum);
+        typename LdVec<GT, N>::type held = typename LdVec<GT, N>::type(0);
+        if (ADD) held = load_columns<GT, N, false>(grad_row<GT>(a, run), cols);
+        const ld_f32x4 sum = sum_parts<kJoinAlone>(a, cols, c, c, last, 1);
+        write_row<GT, N, ADD>(a, run, cols, sum, held);
     }
     for (int32_t w = 0; w < kJoinWaves; ++w) {
         const int32_t to = shared_last[w];
         if (to < 0) continue;
-        sh[wave][ld_lane()] = sum_of(c0 + w, c0 + w + wave, to, kJoinWaves);
+        sh[wave][ld_lane()] = sum_parts<kJoinAhead>(a, cols, c0 + w, c0 + w + wave, to, kJoinWaves);
         __syncthreads();
         if (wave == 0) {
             ld_f32x4 sum = sh[0][ld_lane()];
 #pragma unroll
             for (int i = 1; i < kJoinWaves; ++i) sum += sh[i][ld_lane()];
-            write_row<GT, N>(a, shared_run[w], cols, sum);
+            typename LdVec<GT, N>::type held = typename LdVec<GT, N>::type(0);
+            if (ADD) held = load_columns<GT, N, false>(grad_row<GT>(a, shared_run[w]), cols);
+            write_row<GT, N, ADD>(a, shared_run[w], cols, sum, held);
         }
         __syncthreads();
     }
@@ -605,7 +631,7 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
 
 struct Layout {
     int32_t passes, bits, per_tile, tiles;  // one tile: sorted by a workgroup alone
-    int32_t chunk, chunks;
+    int32_t chunk, window, chunks;
     int64_t part_stride;
     size_t keys, at, counts, part, bytes;  // byte offsets: two buffers each of keys and tokens
 };
@@ -624,9 +650,12 @@ Layout layout_of(int64_t T, int64_t V, int32_t d) {
     l.at = 2 * list;
     l.counts = 4 * list;
     l.part = ld_round_up(l.counts + (static_cast<size_t>(l.tiles) << l.bits) * 4, 256);
-    l.chunk = kMostChunk;
-    // few tokens: smaller chunks, so that more waves share them
-    while (l.chunk > 4 && (T / l.chunk) * ((d + 511) / 512) < 2048 && T <= 256 * l.chunk) l.chunk /= 2;
+    // Few waves: shorter chunks and windows, so that none is long busy with its tokens one after the other; many: fewer partial sums.
+    // 4 and 16, 8 and 16, 16 and 32, 32 and 64 tokens: 1024 of 1600 columns 17, 18, 22, 27 us; 16384 of 256 40, 37, 40, 46; 65536 of 64 69, 53,
+    // 49, 51; 16384 of 1600 84, 84, 85, 86; 65536 of 4096 303, 228, 201, 197
+    const int64_t waves = T * ((static_cast<int64_t>(d) + 511) / 512);
+    l.chunk = waves >= 256 << 10 ? 32 : waves >= 32 << 10 ? 16 : waves >= 8 << 10 ? 8 : 4;
+    l.window = l.chunk < 8 ? 16 : 2 * l.chunk;
     l.chunks = static_cast<int32_t>((T + l.chunk - 1) / l.chunk);
     l.part_stride = (static_cast<int64_t>(d) + 3) / 4 * 4;
     l.bytes = ld_round_up(l.part + 2 * static_cast<size_t>(l.chunks) * l.part_stride * 4, 256);
@@ -700,21 +729,27 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     const int64_t clearing = accumulate ? 0 : (V - clear.from + kClearRows - 1) / kClearRows;
     if (adding + clearing > INT32_MAX / kRowWaves) return LD_ERR_RANGE;
     const RowArgs a = {dout, keys[last], at[last], grad, reinterpret_cast<float*>(ws + l.part), dout_stride, grad_stride, l.part_stride,
-                       static_cast<int32_t>(T), static_cast<int32_t>(V), d, l.chunk, blocks, static_cast<int32_t>(adding),
-                       static_cast<int32_t>(clearing), clear.from, scale, accumulate};
+                       static_cast<int32_t>(T), static_cast<int32_t>(V), d, l.chunk, l.window, blocks, static_cast<int32_t>(adding),
+                       static_cast<int32_t>(clearing), clear.from, scale};
     const dim3 grid(static_cast<uint32_t>(adding + clearing));
     const bool streamed = T * static_cast<int64_t>(d) * ld_type_bytes(dtype) > kStreamed;
     ld_with_type(dtype, [&](auto type) {
         ld_with_type(grad_dtype, [&](auto grad_type) {
-            if (streamed) k_rows<type, grad_type, true><<<grid, dim3(kRowThreads), 0, s>>>(a);
-            else k_rows<type, grad_type, false><<<grid, dim3(kRowThreads), 0, s>>>(a);
+            if (accumulate) {
+                if (streamed) k_rows<type, grad_type, true, true><<<grid, dim3(kRowThreads), 0, s>>>(a);
+                else k_rows<type, grad_type, false, true><<<grid, dim3(kRowThreads), 0, s>>>(a);
+            } else {
+                if (streamed) k_rows<type, grad_type, true, false><<<grid, dim3(kRowThreads), 0, s>>>(a);
+                else k_rows<type, grad_type, false, false><<<grid, dim3(kRowThreads), 0, s>>>(a);
+            }
         });
     });
     if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
-    if (T < LD_WAVE) return LD_OK;  // no run is long
+    if (T < l.window) return LD_OK;  // no run is long
     ld_with_type(grad_dtype, [&](auto grad_type) {
         const dim3 joins((l.chunks + kJoinWaves - 1) / kJoinWaves, (d + 4 * LD_WAVE - 1) / (4 * LD_WAVE));
-        k_join<grad_type><<<joins, dim3(kJoinWaves * LD_WAVE), 0, s>>>(a, l.chunks);
+        if (accumulate) k_join<grad_type, true><<<joins, dim3(kJoinWaves * LD_WAVE), 0, s>>>(a, l.chunks);
+        else k_join<grad_type, false><<<joins, dim3(kJoinWaves * LD_WAVE), 0, s>>>(a, l.chunks);
     });
     return ld_launch_status();
 }
