@@ -685,6 +685,9 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
         return LD_ERR_ALIGN;
     const Layout l = layout_of(T, V, d);
     if (l.bytes > 0 && (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < l.bytes)) return LD_ERR_WORKSPACE;
+    const int32_t columns = LD_WAVE * (dtype == LD_F32 ? 4 : 8), blocks = static_cast<int32_t>((static_cast<int64_t>(d) + columns - 1) / columns);
+    const int64_t adding = (static_cast<int64_t>(l.chunks) * blocks + kRowWaves - 1) / kRowWaves;
+    if (adding + V / kClearRows >= INT32_MAX / kRowWaves) return LD_ERR_RANGE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + l.keys), reinterpret_cast<uint32_t*>(ws + l.keys + l.at / 2)};
@@ -724,10 +727,7 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
         sort.at_in = at[last];
     }
     clear.from += clear.rows;
-    const int32_t columns = LD_WAVE * (dtype == LD_F32 ? 4 : 8), blocks = static_cast<int32_t>((static_cast<int64_t>(d) + columns - 1) / columns);
-    const int64_t adding = (static_cast<int64_t>(l.chunks) * blocks + kRowWaves - 1) / kRowWaves;
     const int64_t clearing = accumulate ? 0 : (V - clear.from + kClearRows - 1) / kClearRows;
-    if (adding + clearing > INT32_MAX / kRowWaves) return LD_ERR_RANGE;
     const RowArgs a = {dout, keys[last], at[last], grad, reinterpret_cast<float*>(ws + l.part), dout_stride, grad_stride, l.part_stride,
                        static_cast<int32_t>(T), static_cast<int32_t>(V), d, l.chunk, l.window, blocks, static_cast<int32_t>(adding),
                        static_cast<int32_t>(clearing), clear.from, scale};

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib
+import math
 import os
 from typing import List, Optional, Sequence, Tuple
 
@@ -592,7 +593,7 @@ def ld_clip_grads(grads: Sequence[torch.Tensor], sumsq: torch.Tensor, max_norm: 
     g, o, gt, ot = got
     _one_device(sumsq, (), g, o)
     st = load().ld_clip_grads(g.checked("grads"), o.checked("outs"), g.sizes, len(grads), gt, ot,
-                              _dev(sumsq, torch.float64, "sumsq"), ctypes.c_float(max_norm), _stream(stream))
+                              _dev(sumsq, torch.float64, "sumsq"), max_norm, _stream(stream))
     _check("ld_clip_grads", st)
 
 
@@ -612,21 +613,27 @@ def ld_clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, outs: Opti
         raise ValueError("norm needs an element")
     if workspace is None:
         workspace = _scratch(lib.ld_grad_norm_workspace(len(grads)), dev, stream)
-    st = lib.ld_clip_grad_norm(gp, op, sizes, len(grads), gt, ot, ctypes.c_float(max_norm), _dev(norm, torch.float32, "norm"),
+    st = lib.ld_clip_grad_norm(gp, op, sizes, len(grads), gt, ot, max_norm, _dev(norm, torch.float32, "norm"),
                                _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
     _check("ld_clip_grad_norm", st)
     return norm
 
 
-def _rows(t: torch.Tensor, name: str, written: bool = False) -> Tuple[int, int, int]:
-    """Address, rows and row stride of a 2-D tensor on the GPU whose rows are contiguous (and apart, where they are written)."""
-    rows, width = t.shape if t.dim() == 2 else (0, 0)
-    if not t.is_cuda or t.dim() != 2 or (width > 1 and t.stride(1) != 1):
-        raise TypeError(f"{name}: expected a 2-D tensor on the GPU with contiguous rows")
-    stride = t.stride(0) if rows > 1 else width  # a view of one row keeps the stride of what it was taken from
-    if written and stride < width:
+def _rows(t: torch.Tensor, name: str, dims: Optional[int] = 2, written: bool = False) -> Tuple[int, int, int]:
+    """Address, rows and row stride of a tensor on the GPU, taken as rows of its last dimension: one that is contiguous (of any
+    number of dimensions with dims = None), or of two dimensions with rows that are, and that do not overlap where they are written."""
+    shape = t.shape
+    if not t.is_cuda or not shape or (dims is not None and len(shape) != dims):
+        raise TypeError(f"{name}: expected a{' 2-D' if dims == 2 else ''} tensor on the GPU")
+    width = shape[-1]
+    if t.is_contiguous():
+        return t.data_ptr(), shape[0] if len(shape) == 2 else math.prod(shape[:-1]), width
+    if len(shape) != 2 or (width > 1 and t.stride(1) != 1):
+        raise TypeError(f"{name}: expected contiguous rows")
+    stride = t.stride(0)
+    if written and shape[0] > 1 and stride < width:
         raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), rows, stride
+    return t.data_ptr(), shape[0], stride
 
 
 def _ids(t: torch.Tensor, name: str) -> int:
@@ -645,24 +652,26 @@ def ld_embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, 
     if (pos_table is None) != (positions is None):
         raise ValueError("pos_table and positions go together")
     d, T = table.shape[-1], ids.numel()
-    if positions is not None and (positions.numel() != T or positions.dtype != ids.dtype):
-        raise ValueError("positions must be as many as ids, and of their type")
-    if pos_table is not None and (pos_table.shape[-1] != d or pos_table.dtype != table.dtype):
-        raise ValueError("table and pos_table differ in width or type")
-    _same_device(table, ids, pos_table, positions, out)
-    code = _elem(table, "table")
+    if pos_table is not None:
+        if positions.numel() != T or positions.dtype != ids.dtype:
+            raise ValueError("positions must be as many as ids, and of their type")
+        if pos_table.shape[-1] != d or pos_table.dtype != table.dtype:
+            raise ValueError("table and pos_table differ in width or type")
+    _one_device(table, (ids, pos_table, positions, out))
+    code, it = _elem(table, "table"), _ids(ids, "ids")
     tp, V, ts = _rows(table, "table")
-    pp, P, ps = _rows(pos_table, "pos_table") if pos_table is not None else (None, 0, 0)
-    it = _ids(ids, "ids")
-    if positions is not None:
+    pp, P, ps, at = None, 0, 0, None
+    if pos_table is not None:
+        pp, P, ps = _rows(pos_table, "pos_table")
         _ids(positions, "positions")
+        at = positions.data_ptr()
     if out is None:
         out = _record(torch.empty(*ids.shape, d, dtype=out_dtype or table.dtype, device=table.device), stream)
     elif out.numel() != T * d or out.shape[-1] != d or (out_dtype is not None and out.dtype != out_dtype):
         raise ValueError("out differs in shape or type from what the lookup gives")
-    op, _, os_ = _rows(out if out.dim() == 2 else out.view(T, d), "out", written=True)
-    st = load().ld_embed_lookup(tp, V, ts, pp, P, ps, code, ids.data_ptr(), positions.data_ptr() if positions is not None else None,
-                                it, T, d, ctypes.c_float(scale), op, os_, _elem(out, "out"), _stream(stream))
+    op, _, os_ = _rows(out, "out", None, written=True)
+    st = load().ld_embed_lookup(tp, V, ts, pp, P, ps, code, ids.data_ptr(), at, it, T, d, scale, op, os_, _elem(out, "out"),
+                                _stream(stream))
     _check("ld_embed_lookup", st)
     return out
 
@@ -679,13 +688,13 @@ def ld_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, sca
     T, d = ids.numel(), grad.shape[-1]
     if dout.shape[-1] != d or dout.numel() != T * d:
         raise ValueError("dout must have a row of grad's width for every id")
-    _same_device(dout, ids, grad, workspace)
-    gp, V, gs = _rows(grad, "grad", written=True)
-    dp, _, ds = _rows(dout if dout.dim() == 2 else dout.view(T, d), "dout")
+    _one_device(grad, (dout, ids, workspace))
     it, dt, gt = _ids(ids, "ids"), _elem(dout, "dout"), _elem(grad, "grad")
+    dp, _, ds = _rows(dout, "dout", None)
+    gp, V, gs = _rows(grad, "grad", written=True)
     if workspace is None:
         workspace = _scratch(lib.ld_embed_grad_workspace(T, V, d), grad.device, stream)
-    st = lib.ld_embed_grad(dp, ds, dt, ids.data_ptr(), it, T, d, ctypes.c_float(scale), gp, V, gs, gt, int(accumulate),
+    st = lib.ld_embed_grad(dp, ds, dt, ids.data_ptr(), it, T, d, scale, gp, V, gs, gt, int(accumulate),
                            _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
     _check("ld_embed_grad", st)
 

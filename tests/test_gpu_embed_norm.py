@@ -408,6 +408,45 @@ def test_on_another_stream_with_the_bindings_own_memory():
     assert abs(float(first[2]) - float(want.square().sum().sqrt())) < 1e-4 * float(first[2])
 
 
+def test_what_the_binding_refuses_on_the_gpu():
+    t, ids = torch.zeros(10, 8, device=DEV), torch.zeros(4, dtype=torch.int64, device=DEV)
+    for bad in (lambda: ld.ld_embed_lookup(t.double(), ids), lambda: ld.ld_embed_lookup(t, ids.to(torch.int16)), lambda: ld.ld_embed_lookup(t, ids.cpu()),
+                lambda: ld.ld_embed_lookup(t.view(2, 5, 8), ids), lambda: ld.ld_embed_lookup(t.t(), ids), lambda: ld.ld_embed_lookup(t, ids[::2]),
+                lambda: ld.ld_embed_lookup(t, ids, out=torch.zeros(8, 4, device=DEV).t()),
+                lambda: ld.ld_embed_lookup(t, ids, out=torch.zeros(4, 7, device=DEV)),
+                lambda: ld.ld_embed_lookup(t, ids, out=torch.zeros(8, device=DEV).expand(4, 8)),
+                lambda: ld.ld_embed_lookup(t, ids, out=torch.zeros(4, 8, device=DEV), out_dtype=BF16),
+                lambda: ld.ld_embed_grad(t[:4], ids, torch.zeros(8, device=DEV).expand(10, 8)),
+                lambda: ld.ld_embed_grad(t[:4], ids, torch.zeros(2, 5, 8, device=DEV)),
+                lambda: ld.ld_embed_grad(torch.zeros(2, 4, 8, device=DEV)[:, :2], ids.view(2, 2), t),
+                lambda: ld.ld_embed_grad(t[:4].double(), ids, t), lambda: ld.ld_embed_grad(t[:4], ids.int().short(), t),
+                lambda: ld.ld_clip_grad_norm([t, t.to(BF16)], 1.0), lambda: ld.ld_clip_grad_norm([t.t()], 1.0),
+                lambda: ld.ld_clip_grad_norm([t, t.cpu()], 1.0), lambda: ld.ld_clip_grad_norm([t], 1.0, [t.cpu()]),
+                lambda: ld.ld_grad_norm([t], sumsq=torch.zeros(1, device=DEV)), lambda: ld.ld_grad_norm([t], sumsq=torch.zeros(0, device=DEV).double()),
+                lambda: ld.ld_clip_grads([t], torch.zeros(0, device=DEV).double(), 1.0)):
+        with pytest.raises((TypeError, ValueError)):
+            bad()
+    for bad in (lambda: ld.ld_clip_grad_norm([t], -1.0), lambda: ld.ld_clip_grad_norm([t], math.nan),
+                lambda: ld.ld_embed_grad(t[:4], ids, t, workspace=torch.zeros(256, dtype=torch.uint8, device=DEV))):
+        with pytest.raises(ld.LowDiffError):
+            bad()
+    assert not t.any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_infinities_and_nan_pass_through_rounding(dtype):
+    """What is not finite stays so in every output type, and what 16 bits do not hold becomes infinite."""
+    row = torch.tensor([[math.inf, -math.inf, math.nan, 1e38, -1e38, 0.0, -0.0, 3.0, 65519.0, 65520.0]])
+    out = ld.ld_embed_lookup(row.to(DEV), torch.zeros(3, dtype=torch.int64, device=DEV), out_dtype=dtype)
+    grad = torch.zeros(2, 10, dtype=dtype, device=DEV)
+    ld.ld_embed_grad(row.to(DEV), torch.ones(1, dtype=torch.int32, device=DEV), grad)
+    clipped = torch.zeros(1, 10, dtype=dtype, device=DEV)
+    ld.ld_clip_grad_norm([row.to(DEV)], 1.0, [clipped])
+    want = row.to(dtype)
+    for got in (out[2:], grad[1:], clipped):
+        assert torch.equal(got.cpu().isnan(), want.isnan()) and torch.equal(got.cpu().nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
+
+
 def test_recorded_in_a_graph():
     g = gen(10)
     V, d, T = 700, 130, 9000
@@ -439,3 +478,16 @@ def test_recorded_in_a_graph():
         step()
         torch.cuda.synchronize()
         assert all(same_bits(a, b) for a, b in zip(got, (out, grad, norm, *parts))), r
+
+
+def test_the_example_learns_and_recovers():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "tied_embedding.py")
+    spec = importlib.util.spec_from_file_location("tied_embedding", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses, norms, recovered = example.train(steps=40)
+    assert recovered and losses[0] > 5.0 and losses[-1] < 0.5 * losses[0]
+    again = example.train(steps=3)
+    assert again[1] == norms[:3]  # the same inputs, the same gradients
