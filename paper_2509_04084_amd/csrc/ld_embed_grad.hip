@@ -148,13 +148,17 @@ constexpr int kAloneBins = 1 << kAloneBits;
 constexpr int kAloneMost = 4 * kSortThreads;
 
 template <int ROUNDS>
-__global__ __launch_bounds__(kSortThreads) void k_sort_alone(SortArgs a, int32_t passes, Clearing c) {
-    __shared__ uint32_t keys[ROUNDS * kSortThreads];
-    __shared__ uint16_t tokens[ROUNDS * kSortThreads];
-    __shared__ uint16_t seen[kSortWaves][kAloneBins];
-    __shared__ uint32_t first[kAloneBins], sh[kSortWaves];
+struct SortShared {
+    uint32_t keys[ROUNDS * kSortThreads];
+    uint16_t tokens[ROUNDS * kSortThreads];
+    uint16_t seen[kSortWaves][kAloneBins];
+    uint32_t first[kAloneBins], sh[kSortWaves];
+};
+
+// Leaves the sorted keys and tokens in shared memory.
+template <int ROUNDS>
+__device__ __forceinline__ void sort_in_shared(const SortArgs& a, int32_t passes, SortShared<ROUNDS>& m) {
     const int32_t bins = 1 << a.bits, wave = threadIdx.x / LD_WAVE, base = wave * (LD_WAVE * ROUNDS) + ld_lane();
-    if (cleared(c, 1)) return;
     uint32_t key[ROUNDS], at[ROUNDS], rank[ROUNDS];
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
@@ -164,50 +168,58 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_alone(SortArgs a, int32_t
     }
     for (int32_t p = 0; p < passes; ++p) {
         const int32_t shift = p * a.bits;
-        for (int32_t i = ld_lane(); i < bins; i += LD_WAVE) seen[wave][i] = 0;
+        for (int32_t i = ld_lane(); i < bins; i += LD_WAVE) m.seen[wave][i] = 0;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r)
-            rank[r] = rank_in_wave((key[r] >> shift) & (bins - 1), base + r * LD_WAVE < a.T, a.bits, seen[wave]);
+            rank[r] = rank_in_wave((key[r] >> shift) & (bins - 1), base + r * LD_WAVE < a.T, a.bits, m.seen[wave]);
         __syncthreads();
         uint32_t total = 0;
         const int32_t b = threadIdx.x;
         if (b < bins) {
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t c = seen[w][b];
-                seen[w][b] = static_cast<uint16_t>(total);
+                const uint32_t c = m.seen[w][b];
+                m.seen[w][b] = static_cast<uint16_t>(total);
                 total += c;
             }
         }
-        const uint32_t from = block_escan(total, sh);
-        if (b < bins) first[b] = from;
+        const uint32_t from = block_escan(total, m.sh);
+        if (b < bins) m.first[b] = from;
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             if (base + r * LD_WAVE < a.T) {
-                const uint32_t digit = (key[r] >> shift) & (bins - 1), to = first[digit] + seen[wave][digit] + rank[r];
-                keys[to] = key[r];
-                tokens[to] = static_cast<uint16_t>(at[r]);
+                const uint32_t digit = (key[r] >> shift) & (bins - 1), to = m.first[digit] + m.seen[wave][digit] + rank[r];
+                m.keys[to] = key[r];
+                m.tokens[to] = static_cast<uint16_t>(at[r]);
             }
         }
         __syncthreads();
+        if (p + 1 == passes) break;
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             const int32_t i = base + r * LD_WAVE;
             if (i < a.T) {
-                key[r] = keys[i];
-                at[r] = tokens[i];
+                key[r] = m.keys[i];
+                at[r] = m.tokens[i];
             }
         }
     }
+}
+
+template <int ROUNDS>
+__global__ __launch_bounds__(kSortThreads) void k_sort_alone(SortArgs a, int32_t passes, Clearing c) {
+    __shared__ SortShared<ROUNDS> m;
+    if (cleared(c, 1)) return;
+    sort_in_shared<ROUNDS>(a, passes, m);
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
-        const int32_t i = base + r * LD_WAVE;
+        const int32_t i = r * kSortThreads + threadIdx.x;
         if (i < a.T) {
-            a.keys_out[i] = key[r];
-            a.at_out[i] = at[r];
+            a.keys_out[i] = m.keys[i];
+            a.at_out[i] = m.tokens[i];
         }
     }
 }
@@ -629,6 +641,158 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
     }
 }
 
+// ------------------------------------------------------------- few tokens
+
+// All in one launch. Every workgroup sorts all tokens for itself, takes a block of columns and a share of the tokens, from where one
+// run begins to where another does, and deals them out to its waves; a run that goes on in the next wave's tokens is added up in
+// shared memory. Other workgroups clear the rows that no token names. Added to 50257 rows of 1600 columns, as three launches and so:
+// 8 tokens 10.4 and 5.5 us, 64 12.5 and 6.6, 256 14.6 and 8.5, 512 15.2 and 10.5, 1024 17.8 and 11.2; 1024 of one id 19.7 and 27.
+constexpr int kFewThreads = kSortThreads;
+constexpr int kFewWaves = kFewThreads / LD_WAVE;
+constexpr int kFewTokens = kSortThreads;
+constexpr int kFewVector = 2;       // columns of a lane: narrow blocks, for more workgroups
+constexpr int kFewColumns = kFewVector * LD_WAVE;
+constexpr int kFewClear = 64;       // rows of a clearing workgroup
+// Tokens of a share at least, and at most: so many that a share is no more than 8 tokens for a wave. Shares of 32, 64 and 128: 1024 tokens of
+// 256 columns 10.9, 11.2, 12.8 us, of 4096 24.9, 16.9, 15.8: no more workgroups than compute units, each sorts.
+constexpr int kFewShare = 32;
+constexpr int kFewMostShare = 128;
+constexpr int kFewGroups = 256;
+constexpr int kCountedBits = 8;     // up to so many tokens (their bits) a token's place is found by counting those that go before it: 8 tokens
+constexpr int kCounted = 1 << kCountedBits;  // 5.5 us instead of 8.1, 256 8.5 instead of 9.9 (512 11.8 instead of 10.5)
+
+// Sorts tokens of keys below 2^24 - 1, like sort_in_shared.
+__device__ __forceinline__ void count_in_shared(const SortArgs& a, SortShared<1>& m) {
+    // a key with the token behind it: all are different
+    __shared__ __attribute__((aligned(16))) uint32_t both[kCounted];
+    __shared__ uint32_t place[kCounted];
+    const int32_t me = threadIdx.x;
+    if (me < kCounted) {
+        both[me] = me < a.T ? key_of(a, me) << kCountedBits | me : UINT32_MAX;
+        place[me] = 0;
+    }
+    __syncthreads();
+    constexpr int kShares = kSortThreads / kCounted, kQuads = kCounted / 4 / kShares;  // the threads of a token share the others out
+    const int32_t i = me % kCounted, q0 = me / kCounted * kQuads;
+    const uint32_t mine = both[i];
+    const ld_u32x4* quads = reinterpret_cast<const ld_u32x4*>(both);
+    uint32_t before = 0;
+#pragma unroll 8
+    for (int32_t q = q0; q < q0 + kQuads; ++q) {
+        if (4 * q >= a.T) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) before += quads[q][e] < mine;
+    }
+    if (i < a.T) atomicAdd(&place[i], before);
+    __syncthreads();
+    if (me < a.T) {
+        m.keys[place[me]] = both[me] >> kCountedBits;
+        m.tokens[place[me]] = static_cast<uint16_t>(me);
+    }
+    __syncthreads();
+}
+
+template <int GT>
+__device__ void clear_unnamed(const RowArgs& a, const SortArgs& s, int32_t first) {
+    constexpr int N = GT == LD_F32 ? 4 : 8;
+    __shared__ unsigned long long named;
+    if (threadIdx.x == 0) named = 0;
+    __syncthreads();
+    for (int32_t i = threadIdx.x; i < a.T; i += kFewThreads) {
+        const uint32_t r = key_of(s, i) - static_cast<uint32_t>(first);  // of an id before the first: a large number
+        if (r < kFewClear) atomicOr(&named, 1ull << r);
+    }
+    __syncthreads();
+    for (int32_t r = threadIdx.x / LD_WAVE; r < kFewClear && first + r < a.V; r += kFewWaves) {
+        if (named >> r & 1) continue;
+        for (int32_t l = ld_lane(); l * N < a.d; l += LD_WAVE)
+            store_columns<GT, N, true>(grad_row<GT>(a, first + r), columns_of<N>(l, a.d), typename LdVec<GT, N>::type(0));
+    }
+}
+
+template <int DT, int GT, bool ADD>
+__global__ __launch_bounds__(kFewThreads) void k_few(RowArgs a, SortArgs s, int32_t passes) {
+    constexpr int N = kFewVector;
+    typedef LdVec<DT, N> X;
+    typedef LdVec<GT, N> G;
+    __shared__ SortShared<1> m;
+    __shared__ typename X::wide came_sum[kFewWaves][LD_WAVE];
+    __shared__ int32_t shared_valid;
+    if (static_cast<int32_t>(blockIdx.x) >= a.adding) {
+        clear_unnamed<GT>(a, s, (static_cast<int32_t>(blockIdx.x) - a.adding) * kFewClear);
+        return;
+    }
+    if (threadIdx.x == 0) shared_valid = 0;
+    if (passes == 0) count_in_shared(s, m);
+    else sort_in_shared<1>(s, passes, m);
+    {
+        const int32_t i = threadIdx.x;
+        if (i < a.T && m.keys[i] < static_cast<uint32_t>(a.V) && (i + 1 == a.T || m.keys[i + 1] >= static_cast<uint32_t>(a.V))) shared_valid = i + 1;
+    }
+    __syncthreads();
+    // the workgroups of a block of columns share the tokens out from one run's beginning to another's
+    const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LD_WAVE), block = blockIdx.x % a.blocks, share = blockIdx.x / a.blocks;
+    const int32_t all = shared_valid, shares = a.adding / a.blocks, per_share = (all + shares - 1) / shares;
+    const auto next_run = [&](int32_t from) {  // the first run that begins at or behind a token
+        for (int32_t i0 = from; i0 < all; i0 += LD_WAVE) {
+            const int32_t i = i0 + ld_lane();
+            const uint64_t found = __ballot(i >= all || i == 0 || m.keys[i] != m.keys[i - 1]);
+            if (found) return i0 + static_cast<int32_t>(__builtin_ctzll(found)) < all ? i0 + static_cast<int32_t>(__builtin_ctzll(found)) : all;
+        }
+        return all;
+    };
+    const int32_t begin = __builtin_amdgcn_readfirstlane(next_run(share * per_share)), valid = __builtin_amdgcn_readfirstlane(next_run((share + 1) * per_share));
+    const int32_t per = (valid - begin + kFewWaves - 1) / kFewWaves, from = begin + wave * per;
+    const int32_t count = valid - from < per ? (valid > from ? valid - from : 0) : per;  // at most 64
+    const Columns cols = columns_of<N>(block * LD_WAVE + ld_lane(), a.d);
+    const bool mine = ld_lane() < count;
+    const uint32_t key = mine ? m.keys[from + ld_lane()] : UINT32_MAX, at = mine ? m.tokens[from + ld_lane()] : 0;
+    const uint32_t before = mine && from + ld_lane() > 0 ? m.keys[from + ld_lane() - 1] : UINT32_MAX;
+    const uint64_t heads = __ballot(mine && key != before);
+    const bool goes_on = count > 0 && from + count < valid && m.keys[from + count] == m.keys[from + count - 1];
+    const auto key_at = [&](int32_t j) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key), j)); };
+    const typename X::elem* dout = static_cast<const typename X::elem*>(a.dout);
+    typename X::wide sum = typename X::wide(0.0f);
+    typename G::type held = typename G::type(0);
+    bool came = count > 0 && !(heads & 1);
+    int32_t run = 0;
+    for (int32_t i = 0; i < count; i += kAhead) {
+        typename X::type x[kAhead];
+        typename G::type row[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u < count) {
+                x[u] = load_columns<DT, N, false>(dout + static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), i + u)) * a.dout_stride, cols);
+                if (ADD && (heads >> (i + u) & 1)) row[u] = load_columns<GT, N, false>(grad_row<GT>(a, key_at(i + u)), cols);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u < count) {
+                if (heads >> (i + u) & 1) {
+                    if (i + u > run) {
+                        if (came) came_sum[wave][ld_lane()] = sum;
+                        else write_row<GT, N, ADD>(a, key_at(run), cols, sum, held);
+                        came = false;
+                        run = i + u;
+                    }
+                    sum = X::widen(x[u]);
+                    if (ADD) held = row[u];
+                } else {
+                    sum += X::widen(x[u]);
+                }
+            }
+        }
+    }
+    if (came) came_sum[wave][ld_lane()] = sum;
+    __syncthreads();
+    if (count == 0 || came) return;
+    if (goes_on) {
+        for (int32_t w = wave + 1; begin + w * per < valid && m.keys[begin + w * per] == key_at(run); ++w) sum += came_sum[w][ld_lane()];
+    }
+    write_row<GT, N, ADD>(a, key_at(run), cols, sum, held);
+}
+
 struct Layout {
     int32_t passes, bits, per_tile, tiles;  // one tile: sorted by a workgroup alone
     int32_t chunk, window, chunks;
@@ -662,6 +826,15 @@ Layout layout_of(int64_t T, int64_t V, int32_t d) {
     return l;
 }
 
+// Workgroups that share a block of columns' tokens out.
+int32_t few_shares(int64_t T, int32_t d) {
+    const int32_t blocks = (d + kFewColumns - 1) / kFewColumns, most = static_cast<int32_t>((T + kFewShare - 1) / kFewShare);
+    const int32_t room = kFewGroups / blocks > 1 ? kFewGroups / blocks : 1;
+    return most < room ? most : room;
+}
+
+bool few(int64_t T, int32_t d) { return T > 0 && T <= kFewTokens && d > 0 && T <= few_shares(T, d) * kFewMostShare; }
+
 bool sizes_fit(int64_t T, int64_t V, int32_t d) {
     return T >= 0 && V >= 0 && d >= 0 && d <= LD_MAX_WIDTH && T <= LD_MAX_TOKENS && V < INT32_MAX;
 }
@@ -669,7 +842,7 @@ bool sizes_fit(int64_t T, int64_t V, int32_t d) {
 }  // namespace
 
 extern "C" size_t ld_embed_grad_workspace(int64_t T, int64_t V, int32_t d) {
-    return sizes_fit(T, V, d) ? layout_of(T, V, d).bytes : 0;
+    return sizes_fit(T, V, d) && !few(T, d) ? layout_of(T, V, d).bytes : 0;
 }
 
 extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_t dtype, const void* ids, int32_t id_dtype, int64_t T,
@@ -683,12 +856,28 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     if (!ld_aligned(dout, ld_type_bytes(dtype)) || !ld_aligned(grad, ld_type_bytes(grad_dtype)) ||
         !ld_aligned(ids, id_dtype == LD_I32 ? 4 : 8))
         return LD_ERR_ALIGN;
+    hipStream_t s = static_cast<hipStream_t>(stream);
     const Layout l = layout_of(T, V, d);
+    if (few(T, d)) {
+        const int32_t few_blocks = (d + kFewColumns - 1) / kFewColumns, adding = few_blocks * few_shares(T, d);
+        const int32_t clearing = accumulate ? 0 : static_cast<int32_t>((V + kFewClear - 1) / kFewClear);
+        const int32_t passes = T <= kCounted && V < (1 << (32 - kCountedBits)) - 1 ? 0 : l.passes;
+        const SortArgs sort = {ids, id_dtype == LD_I64, nullptr, nullptr, nullptr, nullptr, nullptr, V, static_cast<int32_t>(T), 0, 0, 0, l.bits};
+        const RowArgs a = {dout, nullptr, nullptr, grad, nullptr, dout_stride, grad_stride, 0, static_cast<int32_t>(T), static_cast<int32_t>(V), d,
+                           0, 0, few_blocks, adding, clearing, 0, scale};
+        ld_begin_call();
+        ld_with_type(dtype, [&](auto type) {
+            ld_with_type(grad_dtype, [&](auto grad_type) {
+                if (accumulate) k_few<type, grad_type, true><<<dim3(adding), dim3(kFewThreads), 0, s>>>(a, sort, passes);
+                else k_few<type, grad_type, false><<<dim3(adding + clearing), dim3(kFewThreads), 0, s>>>(a, sort, passes);
+            });
+        });
+        return ld_launch_status();
+    }
     if (l.bytes > 0 && (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < l.bytes)) return LD_ERR_WORKSPACE;
     const int32_t columns = LD_WAVE * (dtype == LD_F32 ? 4 : 8), blocks = static_cast<int32_t>((static_cast<int64_t>(d) + columns - 1) / columns);
     const int64_t adding = (static_cast<int64_t>(l.chunks) * blocks + kRowWaves - 1) / kRowWaves;
     if (adding + V / kClearRows >= INT32_MAX / kRowWaves) return LD_ERR_RANGE;
-    hipStream_t s = static_cast<hipStream_t>(stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + l.keys), reinterpret_cast<uint32_t*>(ws + l.keys + l.at / 2)};
     uint32_t* at[2] = {reinterpret_cast<uint32_t*>(ws + l.at), reinterpret_cast<uint32_t*>(ws + l.at + l.at / 2)};

@@ -692,10 +692,10 @@ def ld_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, sca
     it, dt, gt = _ids(ids, "ids"), _elem(dout, "dout"), _elem(grad, "grad")
     dp, _, ds = _rows(dout, "dout", None)
     gp, V, gs = _rows(grad, "grad", written=True)
-    if workspace is None:
-        workspace = _scratch(lib.ld_embed_grad_workspace(T, V, d), grad.device, stream)
+    if workspace is None and (need := lib.ld_embed_grad_workspace(T, V, d)) > 0:
+        workspace = _scratch(need, grad.device, stream)
     st = lib.ld_embed_grad(dp, ds, dt, ids.data_ptr(), it, T, d, scale, gp, V, gs, gt, int(accumulate),
-                           _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+                           _dev(workspace, torch.uint8, "workspace"), workspace.numel() if workspace is not None else 0, _stream(stream))
     _check("ld_embed_grad", st)
 
 

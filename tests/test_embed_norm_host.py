@@ -76,12 +76,12 @@ def test_lookup_refusals():
 
 def test_embed_grad_refusals():
     lib = ld.load()
-    wsb = lib.ld_embed_grad_workspace(8, 100, 64)
-    assert wsb > 0
+    wsb = lib.ld_embed_grad_workspace(2000, 100, 64)
+    assert wsb > 0 and lib.ld_embed_grad_workspace(8, 100, 64) == 0  # few tokens are done with in shared memory
     for bad in ((-1, 100, 64), (8, -1, 64), (8, 100, -1), (8, 100, (1 << 20) + 1), ((1 << 24) + 1, 100, 64), (8, 2 ** 31 - 1, 64)):
         assert lib.ld_embed_grad_workspace(*bad) == 0
 
-    def call(dout=FAKE, ds=64, dtype=1, ids=FAKE, it=1, T=8, d=64, grad=FAKE, rows=100, gs=64, gt=0, acc=0, ws=FAKE, wsb=wsb):
+    def call(dout=FAKE, ds=64, dtype=1, ids=FAKE, it=1, T=2000, d=64, grad=FAKE, rows=100, gs=64, gt=0, acc=0, ws=FAKE, wsb=wsb):
         return lib.ld_embed_grad(V(dout), ds, dtype, V(ids), it, T, d, F(1.0), V(grad), rows, gs, gt, acc, V(ws), wsb, None)
 
     assert call(dout=0) == NULL and call(ids=0) == NULL and call(grad=0) == NULL

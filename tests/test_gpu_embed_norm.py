@@ -173,6 +173,13 @@ def test_embed_grad(T, V, d, kind):
     check_grad(T, V, d, kind, scale=0.75 if d % 2 else 1.0)
 
 
+@pytest.mark.parametrize("kind", ["uniform", "outside", "one", "two", "heavy"])
+@pytest.mark.parametrize("T,V,d", [(7, 200, 300), (31, 9, 129), (255, 40, 260), (256, 50257, 131), (257, 40, 130), (512, 300, 1), (700, 20, 128),
+                                   (1023, 90, 515), (1024, 70, 2), (129, 30, 33000), (200, 20_000_000, 2), (1024, 20_000_000, 1)])
+def test_embed_grad_of_few_tokens(T, V, d, kind):
+    check_grad(T, V, d, kind, BF16 if d % 2 else F32, F32, scale=1.25, id_dtype=torch.int32, seed=3)
+
+
 @pytest.mark.parametrize("dtype,grad_dtype", [(a, b) for a in (F32, BF16, F16) for b in (F32, BF16, F16)])
 @pytest.mark.parametrize("T,V,d,kind", [(300, 90, 129, "heavy"), (2500, 1000, 264, "outside"), (129, 40, 1001, "uniform")])
 def test_embed_grad_types(T, V, d, kind, dtype, grad_dtype):
@@ -427,7 +434,7 @@ def test_what_the_binding_refuses_on_the_gpu():
         with pytest.raises((TypeError, ValueError)):
             bad()
     for bad in (lambda: ld.ld_clip_grad_norm([t], -1.0), lambda: ld.ld_clip_grad_norm([t], math.nan),
-                lambda: ld.ld_embed_grad(t[:4], ids, t, workspace=torch.zeros(256, dtype=torch.uint8, device=DEV))):
+                lambda: ld.ld_embed_grad(t.new_zeros(2000, 8), ids.new_zeros(2000), t, workspace=torch.zeros(256, dtype=torch.uint8, device=DEV))):
         with pytest.raises(ld.LowDiffError):
             bad()
     assert not t.any()
