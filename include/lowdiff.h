@@ -447,7 +447,9 @@ ld_status ld_combine_sparse_strategy(const int32_t* const* idx, const float* con
  *   dtype      LD_F32, LD_BF16 or LD_F16
  *   sumsq      dev, one double, 8-byte aligned
  *   norm       dev, one float, or NULL
- *   workspace  dev, 256-byte aligned, ld_grad_norm_workspace() bytes
+ *   workspace  dev, 256-byte aligned, ld_grad_norm_workspace() bytes; for
+ *              ld_clip_grad_norm ld_clip_grad_norm_workspace() bytes (0 for few
+ *              elements: then it may be NULL)
  *
  * ld_clip_grads - scales the tensors down to a norm of max_norm:
  *   out[t][i] = round(fl32(grad[t][i] * f)),  f = fl32(max_norm / sqrt(*sumsq)) where
@@ -464,6 +466,7 @@ ld_status ld_combine_sparse_strategy(const int32_t* const* idx, const float* con
  */
 #define LD_MAX_TENSORS (1 << 20)
 size_t    ld_grad_norm_workspace(int32_t n_tensors);
+size_t    ld_clip_grad_norm_workspace(int32_t n_tensors, const int64_t* n_elems /* host */);
 ld_status ld_grad_norm(const void* const* grad, const int64_t* n_elems, int32_t n_tensors, int32_t dtype,
                        int32_t accumulate, double* sumsq, float* norm /* may be NULL */,
                        void* workspace, size_t workspace_bytes, ld_stream stream);

@@ -130,6 +130,8 @@ def load() -> ctypes.CDLL:
     lib.ld_combine_sparse_strategy.restype = i32
     lib.ld_grad_norm_workspace.argtypes = [i32]
     lib.ld_grad_norm_workspace.restype = sz
+    lib.ld_clip_grad_norm_workspace.argtypes = [i32, vp]
+    lib.ld_clip_grad_norm_workspace.restype = sz
     lib.ld_grad_norm.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
     lib.ld_grad_norm.restype = i32
     lib.ld_clip_grads.argtypes = [vp, vp, vp, i32, i32, i32, vp, f32, vp]
@@ -611,10 +613,10 @@ def ld_clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, outs: Opti
     gp, op, sizes, gt, ot = (got[0].checked("grads"), got[1].checked("outs"), got[0].sizes, got[2], got[3]) if got else (None, None, None, 0, 0)
     if norm.numel() < 1:
         raise ValueError("norm needs an element")
-    if workspace is None:
-        workspace = _scratch(lib.ld_grad_norm_workspace(len(grads)), dev, stream)
+    if workspace is None and (need := lib.ld_clip_grad_norm_workspace(len(grads), sizes)) > 0:
+        workspace = _scratch(need, dev, stream)
     st = lib.ld_clip_grad_norm(gp, op, sizes, len(grads), gt, ot, max_norm, _dev(norm, torch.float32, "norm"),
-                               _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+                               _dev(workspace, torch.uint8, "workspace"), workspace.numel() if workspace is not None else 0, _stream(stream))
     _check("ld_clip_grad_norm", st)
     return norm
 

@@ -54,7 +54,11 @@ def test_clip_refusals():
     assert both(n=np.array([-5, 1], np.int64)) == RANGE
     assert both(odtype=1, o=(V * 2)(FAKE, FAKE + 1)) == ALIGN and both(g=(V * 2)(FAKE + 1, FAKE)) == ALIGN
     assert lib.ld_clip_grads(two, two, _p(n), 2, 0, 0, V(FAKE + 4), F(1.0), None) == ALIGN
-    assert lib.ld_clip_grad_norm(two, two, _p(n), 2, 0, 0, F(1.0), V(FAKE), V(FAKE), wsb - 1, None) == WORKSPACE
+    assert lib.ld_clip_grad_norm_workspace(2, _p(n)) == 0  # few elements are done with in one launch
+    n = np.array([10, 200000], np.int64)
+    assert lib.ld_clip_grad_norm_workspace(2, _p(n)) == wsb and lib.ld_clip_grad_norm_workspace(-1, _p(n)) == 0
+    for bad in ((FAKE, wsb - 1), (0, wsb), (FAKE + 16, wsb)):
+        assert lib.ld_clip_grad_norm(two, two, _p(n), 2, 0, 0, F(1.0), V(FAKE), V(bad[0]), bad[1], None) == WORKSPACE
     assert lib.ld_clip_grads(None, None, None, 0, 0, 0, V(FAKE), F(1.0), None) == 0  # nothing to do
 
 
