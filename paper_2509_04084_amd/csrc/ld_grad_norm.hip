@@ -20,7 +20,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;                 // vectors per thread and piece
 constexpr int kTensorGroup = 16;
-constexpr int kTensorGroups = 11;
 constexpr int kNormGrid = 2048;            // workgroups of a launch, each with a partial sum
 // Workgroups of a launch that clips in place, where all may find that nothing is to be done: GPT-2 XL under the limit 494 us in all, clipping
 // 1048; with one for every piece, as out of place, 520 and 989, with 2048 483 and 1122.
@@ -28,26 +27,28 @@ constexpr int kInPlaceGrid = 16384;
 constexpr int64_t kAloneElems = 32768;     // up to here one workgroup does the whole call
 constexpr int kAloneThreads = 1024;
 
-// The tensors of a launch, in its arguments: up to GROUPS groups of 16. A tensor is cut into pieces, the last one ragged.
-template <int GROUPS>
+// The tensors of a launch, in its arguments: up to GROUPS groups of 16, with DST where each goes to. A tensor is cut into pieces, the
+// last one ragged.
+template <int GROUPS, bool DST>
 struct TensorBatch {
     static constexpr int kMost = GROUPS * kTensorGroup;
+    static constexpr bool kDst = DST;
     int32_t first_of_group[kTensorGroup];  // [0]: all pieces; then every 16th of first_piece
     int32_t first_piece[kMost + 1];        // entries past the last tensor: all pieces
-    struct Tensor {
-        const void* src;
-        void* dst;
-    } tensor[kMost];
+    const void* src[kMost];
+    void* dst[DST ? kMost : 1];
     int16_t last[kMost];                   // elements of a tensor's last piece
 };
+typedef TensorBatch<16, false> SummedTensors;
+typedef TensorBatch<11, true> ClippedTensors;
 // Host time of a launch with 4 KB of arguments 4.6 us, with 400 bytes 4.2
-typedef TensorBatch<1> FewTensors;
-typedef TensorBatch<kTensorGroups> ManyTensors;
-static_assert(sizeof(ManyTensors) <= 4000, "the arguments of a kernel must fit 4 KB");
+typedef TensorBatch<1, false> FewSummed;
+typedef TensorBatch<1, true> FewClipped;
+static_assert(sizeof(SummedTensors) <= 4000 && sizeof(ClippedTensors) <= 4000, "the arguments of a kernel must fit 4 KB");
 
 // The tensor that a piece belongs to: two reads of 16 consecutive entries each.
-template <int GROUPS>
-__device__ __forceinline__ int tensor_of(const TensorBatch<GROUPS>& b, int32_t piece) {
+template <int GROUPS, bool DST>
+__device__ __forceinline__ int tensor_of(const TensorBatch<GROUPS, DST>& b, int32_t piece) {
     int group = 0, t = 0;
     if (GROUPS > 1) {
 #pragma unroll
@@ -92,7 +93,7 @@ template <int DT, int N, int THREADS, typename B>
 __device__ __forceinline__ double squares(const B& b, int32_t p, int32_t me, double sum) {
     typedef LdVec<DT, N> V;
     const Piece at = piece_of<N>(b, p);
-    const typename V::elem* src = static_cast<const typename V::elem*>(b.tensor[at.tensor].src) + at.first;
+    const typename V::elem* src = static_cast<const typename V::elem*>(b.src[at.tensor]) + at.first;
 #pragma unroll
     for (int u = 0; u < piece_elems<N>() / N / THREADS; ++u) {
         const int32_t i = (u * THREADS + me) * N;
@@ -117,8 +118,8 @@ __device__ __forceinline__ void scale_piece(const B& b, int32_t p, int32_t me, f
     typedef LdVec<DT, N> V;
     typedef LdVec<OT, N> O;
     const Piece at = piece_of<N>(b, p);
-    const typename V::elem* src = static_cast<const typename V::elem*>(b.tensor[at.tensor].src) + at.first;
-    typename O::elem* dst = static_cast<typename O::elem*>(b.tensor[at.tensor].dst) + at.first;
+    const typename V::elem* src = static_cast<const typename V::elem*>(b.src[at.tensor]) + at.first;
+    typename O::elem* dst = static_cast<typename O::elem*>(b.dst[at.tensor]) + at.first;
     if (at.have == piece_elems<N>()) {
         const typename V::type* v = reinterpret_cast<const typename V::type*>(src) + me;
         typename O::type* o = reinterpret_cast<typename O::type*>(dst) + me;
@@ -204,26 +205,41 @@ __global__ __launch_bounds__(kAloneThreads) void k_clip_alone(B b, float max_nor
     for (int32_t p = wave; p < b.first_of_group[0]; p += waves) scale_piece<DT, OT, N, LD_WAVE>(b, p, ld_lane(), factor);
 }
 
-// Tensors [t, ...) of the lists as a launch takes them, in pieces of `piece` elements; t moves behind them.
+// A call's lists.
+struct Lists {
+    const void* const* src;
+    void* const* dst;  // NULL: none
+    const int64_t* n_elems;
+    int32_t n_tensors, src_type, dst_type;
+};
+
+// Tensors [t, ...) of the lists as a launch takes them, in pieces of `piece` elements; t moves behind them. With `join` tensors that
+// lie one behind the other, and go so, are one to it: the 420 parts of a flat gradient of 5 M elements are clipped in one launch, not three.
 template <typename B>
-void next_batch(B& b, const void* const* src, void* const* dst, const int64_t* n_elems, int32_t n_tensors, int32_t piece,
-                int32_t& t) {
+void next_batch(B& b, const Lists& l, int32_t piece, bool join, int32_t& t) {
     int32_t count = 0;
-    int64_t pieces = 0;
-    for (; t < n_tensors && count < B::kMost; ++t) {
-        const int64_t np = (n_elems[t] + piece - 1) / piece;
-        if (np == 0) continue;
-        b.tensor[count] = {src[t], dst ? dst[t] : nullptr};
-        b.first_piece[count] = static_cast<int32_t>(pieces);
-        b.last[count] = static_cast<int16_t>(n_elems[t] - (np - 1) * piece);
-        pieces += np;
-        ++count;
+    int64_t pieces = 0, elems = 0;  // of all tensors taken, and of the last
+    const unsigned char *src_end = nullptr, *dst_end = nullptr;
+    const int64_t src_bytes = ld_type_bytes(l.src_type), dst_bytes = ld_type_bytes(l.dst_type);
+    for (; t < l.n_tensors; ++t) {
+        if (l.n_elems[t] == 0) continue;
+        if (B::kDst && join && count > 0 && l.src[t] == src_end && l.dst[t] == dst_end) {
+            elems += l.n_elems[t];
+        } else {
+            if (count == B::kMost) break;
+            b.src[count] = l.src[t];
+            if (B::kDst) b.dst[count] = l.dst[t];
+            b.first_piece[count] = static_cast<int32_t>(pieces);
+            elems = l.n_elems[t];
+            ++count;
+        }
+        const int64_t of_it = (elems + piece - 1) / piece;
+        pieces = b.first_piece[count - 1] + of_it;
+        b.last[count - 1] = static_cast<int16_t>(elems - (of_it - 1) * piece);
+        src_end = static_cast<const unsigned char*>(l.src[t]) + l.n_elems[t] * src_bytes;
+        if (B::kDst) dst_end = static_cast<const unsigned char*>(l.dst[t]) + l.n_elems[t] * dst_bytes;
     }
     for (int32_t i = count; i <= B::kMost; ++i) b.first_piece[i] = static_cast<int32_t>(pieces);
-    for (int32_t i = count; i < B::kMost; ++i) {
-        b.tensor[i] = {nullptr, nullptr};
-        b.last[i] = 0;
-    }
     b.first_of_group[0] = static_cast<int32_t>(pieces);
     for (int32_t g = 1; g < kTensorGroup; ++g)
         b.first_of_group[g] = g * kTensorGroup < B::kMost ? b.first_piece[g * kTensorGroup] : static_cast<int32_t>(pieces);
@@ -231,39 +247,42 @@ void next_batch(B& b, const void* const* src, void* const* dst, const int64_t* n
 
 constexpr int64_t kMostElems = static_cast<int64_t>(1) << 41;  // of all tensors: 2^29 pieces of 4096, and one more a tensor
 
-ld_status check_lists(const void* const* grad, void* const* out, bool with_out, const int64_t* n_elems, int32_t n_tensors,
-                      int32_t dtype, int32_t out_dtype) {
-    if (n_tensors < 0 || n_tensors > LD_MAX_TENSORS || !ld_known_type(dtype) || !ld_known_type(out_dtype)) return LD_ERR_RANGE;
-    if (n_tensors > 0 && (!grad || !n_elems || (with_out && !out))) return LD_ERR_NULL;
+ld_status check_lists(const Lists& l, bool with_dst) {
+    if (l.n_tensors < 0 || l.n_tensors > LD_MAX_TENSORS || !ld_known_type(l.src_type) || !ld_known_type(l.dst_type)) return LD_ERR_RANGE;
+    if (l.n_tensors > 0 && (!l.src || !l.n_elems || (with_dst && !l.dst))) return LD_ERR_NULL;
     int64_t total = 0;
-    for (int32_t t = 0; t < n_tensors; ++t) {
-        if (n_elems[t] < 0 || n_elems[t] > kMostElems - total) return LD_ERR_RANGE;
-        total += n_elems[t];
-        if (n_elems[t] > 0 && (!grad[t] || (with_out && !out[t]))) return LD_ERR_NULL;
-        if (!ld_aligned(grad[t], ld_type_bytes(dtype)) || (with_out && !ld_aligned(out[t], ld_type_bytes(out_dtype)))) return LD_ERR_ALIGN;
+    for (int32_t t = 0; t < l.n_tensors; ++t) {
+        if (l.n_elems[t] < 0 || l.n_elems[t] > kMostElems - total) return LD_ERR_RANGE;
+        total += l.n_elems[t];
+        if (l.n_elems[t] > 0 && (!l.src[t] || (with_dst && !l.dst[t]))) return LD_ERR_NULL;
+        if (!ld_aligned(l.src[t], ld_type_bytes(l.src_type)) || (with_dst && !ld_aligned(l.dst[t], ld_type_bytes(l.dst_type)))) return LD_ERR_ALIGN;
     }
     return LD_OK;
 }
 
 // Partial sums of all launches, and behind them the sum of squares.
 size_t partials_of(int32_t n_tensors) {
-    return static_cast<size_t>((n_tensors + ManyTensors::kMost - 1) / ManyTensors::kMost) * kNormGrid;
+    return static_cast<size_t>((n_tensors + SummedTensors::kMost - 1) / SummedTensors::kMost) * kNormGrid;
 }
 
-// Enqueues the partial sums; `count` of them are left in `part`.
+// Enqueues the partial sums; `count` of them are left in `part`. Every tensor by itself, so that the sum's order is that of the sizes.
 template <typename B>
-ld_status sum_squares(const void* const* grad, const int64_t* n_elems, int32_t n_tensors, int32_t dtype, double* part, int32_t& count, hipStream_t s) {
+ld_status sum_squares(const Lists& l, double* part, int32_t& count, hipStream_t s) {
     count = 0;
-    for (int32_t t = 0; t < n_tensors;) {
+    for (int32_t t = 0; t < l.n_tensors;) {
         B b;
-        next_batch(b, grad, nullptr, n_elems, n_tensors, dtype == LD_F32 ? piece_elems<4>() : piece_elems<8>(), t);
+        next_batch(b, l, l.src_type == LD_F32 ? piece_elems<4>() : piece_elems<8>(), false, t);
         if (b.first_of_group[0] == 0) continue;
         const int32_t grid = b.first_of_group[0] < kNormGrid ? b.first_of_group[0] : kNormGrid;
-        ld_with_type(dtype, [&](auto type) { k_sum_squares<type, B><<<dim3(grid), dim3(kThreads), 0, s>>>(b, part + count); });
+        ld_with_type(l.src_type, [&](auto type) { k_sum_squares<type, B><<<dim3(grid), dim3(kThreads), 0, s>>>(b, part + count); });
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
         count += grid;
     }
     return LD_OK;
+}
+
+ld_status sum_squares(const Lists& l, double* part, int32_t& count, hipStream_t s) {
+    return l.n_tensors <= FewSummed::kMost ? sum_squares<FewSummed>(l, part, count, s) : sum_squares<SummedTensors>(l, part, count, s);
 }
 
 ld_status finish(const double* part, int32_t count, int32_t accumulate, double* sumsq, float* norm, hipStream_t s) {
@@ -273,20 +292,19 @@ ld_status finish(const double* part, int32_t count, int32_t accumulate, double* 
 
 // Enqueues the scaling by `count` partial sums; with `alone` the sums as well, the call being small.
 template <typename B>
-ld_status clip(const void* const* grad, void* const* out, const int64_t* n_elems, int32_t n_tensors, int32_t dtype, int32_t out_dtype,
-               const double* part, int32_t count, float max_norm, float* norm, bool alone, hipStream_t s) {
-    const int32_t piece = dtype == LD_F32 || out_dtype == LD_F32 ? piece_elems<4>() : piece_elems<8>();
-    for (int32_t t = 0; t < n_tensors;) {
+ld_status clip(const Lists& l, const double* part, int32_t count, float max_norm, float* norm, bool alone, hipStream_t s) {
+    const int32_t piece = l.src_type == LD_F32 || l.dst_type == LD_F32 ? piece_elems<4>() : piece_elems<8>();
+    for (int32_t t = 0; t < l.n_tensors;) {
         const int32_t from = t;
         B b;
-        next_batch(b, grad, out, n_elems, n_tensors, piece, t);
+        next_batch(b, l, piece, !alone, t);
         const int32_t pieces = b.first_of_group[0];
         if (pieces == 0 && !alone) continue;
-        int32_t in_place = dtype == out_dtype;
-        for (int32_t i = from; i < t; ++i) in_place &= n_elems[i] == 0 || grad[i] == out[i];
+        int32_t in_place = l.src_type == l.dst_type;
+        for (int32_t i = from; i < t; ++i) in_place &= l.n_elems[i] == 0 || l.src[i] == l.dst[i];
         const dim3 grid(in_place && pieces > kInPlaceGrid ? kInPlaceGrid : pieces);
-        ld_with_type(dtype, [&](auto type) {
-            ld_with_type(out_dtype, [&](auto out_type) {
+        ld_with_type(l.src_type, [&](auto type) {
+            ld_with_type(l.dst_type, [&](auto out_type) {
                 if (alone) k_clip_alone<type, out_type, B><<<dim3(1), dim3(kAloneThreads), 0, s>>>(b, max_norm, in_place, norm);
                 else k_clip<type, out_type, B><<<grid, dim3(kThreads), 0, s>>>(b, part, count, max_norm, in_place, norm);
             });
@@ -296,14 +314,14 @@ ld_status clip(const void* const* grad, void* const* out, const int64_t* n_elems
     return LD_OK;
 }
 
-// Calls f with a pointer, to nothing, of the type of batch that a call of n_tensors takes.
-template <typename F>
-ld_status with_batch(int32_t n_tensors, F f) {
-    return n_tensors <= FewTensors::kMost ? f(static_cast<FewTensors*>(nullptr)) : f(static_cast<ManyTensors*>(nullptr));
+ld_status clip(const Lists& l, const double* part, int32_t count, float max_norm, float* norm, bool alone, hipStream_t s) {
+    return l.n_tensors <= FewClipped::kMost ? clip<FewClipped>(l, part, count, max_norm, norm, alone, s)
+                                            : clip<ClippedTensors>(l, part, count, max_norm, norm, alone, s);
 }
 
+// Whether one workgroup does a call.
 bool done_alone(int32_t n_tensors, const int64_t* n_elems) {
-    if (n_tensors == 0 || n_tensors > ManyTensors::kMost) return false;
+    if (n_tensors <= 0 || n_tensors > ClippedTensors::kMost) return false;
     int64_t total = 0;
     for (int32_t t = 0; t < n_tensors; ++t) {
         if (n_elems[t] < 0 || n_elems[t] > kAloneElems - total) return false;
@@ -320,12 +338,13 @@ extern "C" size_t ld_grad_norm_workspace(int32_t n_tensors) {
 }
 
 extern "C" size_t ld_clip_grad_norm_workspace(int32_t n_tensors, const int64_t* n_elems) {
-    return n_elems && n_tensors >= 0 && done_alone(n_tensors, n_elems) ? 0 : ld_grad_norm_workspace(n_tensors);
+    return n_elems && done_alone(n_tensors, n_elems) ? 0 : ld_grad_norm_workspace(n_tensors);
 }
 
 extern "C" ld_status ld_grad_norm(const void* const* grad, const int64_t* n_elems, int32_t n_tensors, int32_t dtype, int32_t accumulate,
                                   double* sumsq, float* norm, void* workspace, size_t workspace_bytes, ld_stream stream) {
-    const ld_status st = check_lists(grad, nullptr, false, n_elems, n_tensors, dtype, dtype);
+    const Lists l = {grad, nullptr, n_elems, n_tensors, dtype, dtype};
+    ld_status st = check_lists(l, false);
     if (st != LD_OK) return st;
     if (!sumsq) return LD_ERR_NULL;
     if (!ld_aligned(sumsq, 8) || !ld_aligned(norm, 4)) return LD_ERR_ALIGN;
@@ -334,28 +353,27 @@ extern "C" ld_status ld_grad_norm(const void* const* grad, const int64_t* n_elem
     hipStream_t s = static_cast<hipStream_t>(stream);
     double* part = static_cast<double*>(workspace);
     int32_t count;
-    const ld_status summed =
-        with_batch(n_tensors, [&](auto* b) { return sum_squares<std::remove_pointer_t<decltype(b)>>(grad, n_elems, n_tensors, dtype, part, count, s); });
-    return summed != LD_OK ? summed : finish(part, count, accumulate, sumsq, norm, s);
+    st = sum_squares(l, part, count, s);
+    return st != LD_OK ? st : finish(part, count, accumulate, sumsq, norm, s);
 }
 
 extern "C" ld_status ld_clip_grads(const void* const* grad, void* const* out, const int64_t* n_elems, int32_t n_tensors, int32_t dtype,
                                    int32_t out_dtype, const double* sumsq, float max_norm, ld_stream stream) {
-    const ld_status st = check_lists(grad, out, true, n_elems, n_tensors, dtype, out_dtype);
+    const Lists l = {grad, out, n_elems, n_tensors, dtype, out_dtype};
+    const ld_status st = check_lists(l, true);
     if (st != LD_OK) return st;
     if (!(max_norm >= 0.0f)) return LD_ERR_RANGE;
     if (!sumsq) return LD_ERR_NULL;
     if (!ld_aligned(sumsq, 8)) return LD_ERR_ALIGN;
     ld_begin_call();
-    return with_batch(n_tensors, [&](auto* b) {
-        return clip<std::remove_pointer_t<decltype(b)>>(grad, out, n_elems, n_tensors, dtype, out_dtype, sumsq, 1, max_norm, nullptr, false, static_cast<hipStream_t>(stream));
-    });
+    return clip(l, sumsq, 1, max_norm, nullptr, false, static_cast<hipStream_t>(stream));
 }
 
 extern "C" ld_status ld_clip_grad_norm(const void* const* grad, void* const* out, const int64_t* n_elems, int32_t n_tensors, int32_t dtype,
                                        int32_t out_dtype, float max_norm, float* norm, void* workspace, size_t workspace_bytes,
                                        ld_stream stream) {
-    const ld_status st = check_lists(grad, out, true, n_elems, n_tensors, dtype, out_dtype);
+    const Lists l = {grad, out, n_elems, n_tensors, dtype, out_dtype};
+    ld_status st = check_lists(l, true);
     if (st != LD_OK) return st;
     if (!(max_norm >= 0.0f)) return LD_ERR_RANGE;
     if (!norm) return LD_ERR_NULL;
@@ -364,20 +382,14 @@ extern "C" ld_status ld_clip_grad_norm(const void* const* grad, void* const* out
     if (!alone && (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < ld_grad_norm_workspace(n_tensors))) return LD_ERR_WORKSPACE;
     ld_begin_call();
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (alone) return clip(l, nullptr, 0, max_norm, norm, true, s);
     double* part = static_cast<double*>(workspace);
-    return with_batch(n_tensors, [&](auto* b) {
-        typedef std::remove_pointer_t<decltype(b)> B;
-        const auto scaled = [&](const double* sums, int32_t count, float* to) {
-            return clip<B>(grad, out, n_elems, n_tensors, dtype, out_dtype, sums, count, max_norm, to, alone, s);
-        };
-        if (alone) return scaled(nullptr, 0, norm);
-        int32_t count;
-        ld_status status = sum_squares<B>(grad, n_elems, n_tensors, dtype, part, count, s);
-        if (status != LD_OK) return status;
-        // up to a piece a workgroup, the partial sums are so few that whoever clips adds them up: a launch less (1 M elements 10.4 -> 9.0 us)
-        if (count > 0 && count < kNormGrid) return scaled(part, count, norm);
-        double* sumsq = part + partials_of(n_tensors);
-        status = finish(part, count, 0, sumsq, norm, s);
-        return status != LD_OK ? status : scaled(sumsq, 1, nullptr);
-    });
+    int32_t count;
+    st = sum_squares(l, part, count, s);
+    if (st != LD_OK) return st;
+    // up to a piece a workgroup, the partial sums are so few that whoever clips adds them up: a launch less (1 M elements 10.4 -> 9.0 us)
+    if (count > 0 && count < kNormGrid) return clip(l, part, count, max_norm, norm, false, s);
+    double* sumsq = part + partials_of(n_tensors);
+    st = finish(part, count, 0, sumsq, norm, s);
+    return st != LD_OK ? st : clip(l, sumsq, 1, max_norm, nullptr, false, s);
 }

@@ -353,6 +353,35 @@ def test_clip_of_views_at_any_alignment():
         assert bool((room[:5] == 3).all()) and bool((room[5 + at:] == 3).all())
 
 
+@pytest.mark.parametrize("dtype,out_dtype", [(F32, F32), (BF16, F32), (F16, BF16)])
+def test_clip_of_neighbours(dtype, out_dtype):
+    """Parts of one buffer, some apart, some that go elsewhere than behind the one before, some empty."""
+    g = gen(12)
+    sizes = [int(n) for n in torch.randint(0, 900, (700,), generator=g)] + [40000, 3, 0, 17]
+    src = normal(g, (sum(sizes) + 10 * len(sizes),), 1.0, dtype).to(DEV)
+    dst = torch.full((sum(sizes) + 10 * len(sizes),), 7.0, dtype=out_dtype, device=DEV)
+    parts, outs, at, to = [], [], 0, 0
+    for i, n in enumerate(sizes):
+        at += i % 50 == 49   # a gap on one side, on the other, or on both, now and then
+        to += 3 * (i % 40 == 39)
+        parts.append(src[at:at + n])
+        outs.append(dst[to:to + n])
+        at, to = at + n, to + n
+    outs[100], outs[101] = outs[101], outs[100]
+    parts[100], parts[101] = parts[101], parts[100]
+    norm, want = clip64([x.cpu() for x in parts], 5.0, dtype)
+    got = ld.ld_clip_grad_norm(parts, 5.0, outs)
+    assert abs(float(got) - norm) <= U * (1 + 2.0 ** -10) * norm
+    close(torch.cat(outs), torch.cat(want), 2 * U * torch.cat(want).abs(), out_dtype, "neighbours")
+    written = torch.zeros(dst.numel(), dtype=torch.bool, device=DEV)
+    for o in outs:
+        first = (o.data_ptr() - dst.data_ptr()) // dst.element_size()
+        written[first:first + o.numel()] = True
+    assert bool((dst[~written] == 7).all())
+    apart = [x.clone() for x in parts]
+    assert same_bits(ld.ld_clip_grad_norm(apart, 5.0), got)  # the order of the sum is that of the sizes, wherever the tensors lie
+
+
 def test_norms_that_32_bits_do_not_hold():
     big = torch.full((100,), 3e38, device=DEV)
     assert math.isinf(float(ld.ld_clip_grad_norm([big], 1e10)))     # 3e39: finite, but not in 32 bits; clipped all the same
