@@ -513,6 +513,7 @@ ld_status ld_embed_lookup(const void* table, int64_t V, int64_t table_stride,
  *   grad       dev [V] rows of d elements of `grad_dtype`, grad_stride >= d apart; overlaps
  *              neither dout nor ids
  *   T          0 <= T <= LD_MAX_TOKENS;  V  0 <= V < 2^31 - 1;  0 <= d <= LD_MAX_WIDTH
+ *              (T d beyond any GPU's memory, as a broadcast dout can have it, is LD_ERR_RANGE)
  *   workspace  dev, 256-byte aligned, ld_embed_grad_workspace() bytes (0 for few
  *              tokens: then it may be NULL)
  * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_WORKSPACE, LD_ERR_HIP.

@@ -109,18 +109,23 @@ extern "C" ld_status ld_embed_lookup(const void* table, int64_t V, int64_t table
     while (lanes_log2 < 8 && (unroll << lanes_log2) < vectors) ++lanes_log2;
     // few tokens: fewer vectors a thread, so that more of the chip loads at once
     while (lanes_log2 < 8 && (1 << lanes_log2) < vectors && (T << lanes_log2) < 256 * 1024) ++lanes_log2;
-    const int64_t per = kThreads >> lanes_log2, blocks = (T + per - 1) / per;
-    if (blocks > INT32_MAX) return LD_ERR_RANGE;
-    const LookupArgs a = {table, pos_table, ids, positions, out, V, P, T, table_stride, pos_stride, out_stride, d, scale, lanes_log2,
-                          id_dtype == LD_I64};
-    ld_begin_call();
-    const dim3 grid(static_cast<uint32_t>(blocks));
+    const int64_t per = kThreads >> lanes_log2, most = per << 23;  // tokens of a launch, which has fewer than 2^32 threads
     hipStream_t st = static_cast<hipStream_t>(stream);
-    ld_with_type(dtype, [&](auto type) {
-        ld_with_type(out_dtype, [&](auto out_type) {
-            if (streamed) k_lookup<type, out_type, true><<<grid, dim3(kThreads), 0, st>>>(a);
-            else k_lookup<type, out_type, false><<<grid, dim3(kThreads), 0, st>>>(a);
+    ld_begin_call();
+    for (int64_t t = 0; t < T; t += most) {
+        const int64_t tokens = T - t < most ? T - t : most;
+        const LookupArgs a = {table, pos_table, static_cast<const char*>(ids) + t * id_bytes,
+                              positions ? static_cast<const char*>(positions) + t * id_bytes : nullptr,
+                              static_cast<char*>(out) + t * out_stride * ld_type_bytes(out_dtype), V, P, tokens, table_stride, pos_stride,
+                              out_stride, d, scale, lanes_log2, id_dtype == LD_I64};
+        const dim3 grid(static_cast<uint32_t>((tokens + per - 1) / per));
+        ld_with_type(dtype, [&](auto type) {
+            ld_with_type(out_dtype, [&](auto out_type) {
+                if (streamed) k_lookup<type, out_type, true><<<grid, dim3(kThreads), 0, st>>>(a);
+                else k_lookup<type, out_type, false><<<grid, dim3(kThreads), 0, st>>>(a);
+            });
         });
-    });
-    return ld_launch_status();
+        if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
+    }
+    return LD_OK;
 }

@@ -435,25 +435,30 @@ __device__ __forceinline__ void write_row(const RowArgs& a, uint32_t v, Columns 
     store_columns<GT, N, true>(grad_row<GT>(a, v), c, LdVec<GT, N>::narrow(sum));
 }
 
+// Clears the rows that no token names, kClearRows at a time.
 template <int GT>
-__device__ void clear_rows(const RowArgs& a, int32_t first) {
+__device__ void clear_rows(const RowArgs& a, int32_t group) {
     constexpr int N = GT == LD_F32 ? 4 : 8;
     __shared__ uint32_t named;
-    if (threadIdx.x < LD_WAVE) {
-        const int32_t v = first + static_cast<int32_t>(threadIdx.x);
-        bool is = false;
-        if (threadIdx.x < kClearRows && v < a.V) {
-            const int32_t i = lower_bound(a.keys, a.T, v);
-            is = i < a.T && a.keys[i] == static_cast<uint32_t>(v);
+    for (int32_t left = a.V - a.clear_from - group * kClearRows; left > 0; left -= a.clearing * kClearRows) {
+        const int32_t first = a.V - left, rows = left < kClearRows ? left : kClearRows;
+        if (threadIdx.x < LD_WAVE) {
+            bool is = false;
+            if (static_cast<int32_t>(threadIdx.x) < rows) {
+                const uint32_t v = first + threadIdx.x;
+                const int32_t i = lower_bound(a.keys, a.T, v);
+                is = i < a.T && a.keys[i] == v;
+            }
+            const uint64_t all = __ballot(is);
+            if (threadIdx.x == 0) named = static_cast<uint32_t>(all);
         }
-        const uint64_t all = __ballot(is);
-        if (threadIdx.x == 0) named = static_cast<uint32_t>(all);
-    }
-    __syncthreads();
-    for (int32_t r = threadIdx.x / LD_WAVE; r < kClearRows && first + r < a.V; r += kRowWaves) {
-        if (named >> r & 1) continue;
-        typename LdElem<GT>::type* row = static_cast<typename LdElem<GT>::type*>(a.grad) + static_cast<int64_t>(first + r) * a.grad_stride;
-        for (int32_t l = ld_lane(); l * N < a.d; l += LD_WAVE) store_columns<GT, N, true>(row, columns_of<N>(l, a.d), typename LdVec<GT, N>::type(0));
+        __syncthreads();
+        for (int32_t r = threadIdx.x / LD_WAVE; r < rows; r += kRowWaves) {
+            if (named >> r & 1) continue;
+            for (int32_t l = ld_lane(); l * N < a.d; l += LD_WAVE)
+                store_columns<GT, N, true>(grad_row<GT>(a, first + r), columns_of<N>(l, a.d), typename LdVec<GT, N>::type(0));
+        }
+        __syncthreads();
     }
 }
 
@@ -493,7 +498,7 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
         const int64_t all = a.adding + a.clearing;
         const int32_t before = static_cast<int32_t>(static_cast<int64_t>(block) * a.clearing / all);
         if (static_cast<int32_t>(static_cast<int64_t>(block + 1) * a.clearing / all) > before) {
-            clear_rows<GT>(a, a.clear_from + before * kClearRows);
+            clear_rows<GT>(a, before);
             return;
         }
         block -= before;
@@ -696,21 +701,26 @@ __device__ __forceinline__ void count_in_shared(const SortArgs& a, SortShared<1>
     __syncthreads();
 }
 
+// Clears the rows that none of few tokens names, kFewClear at a time.
 template <int GT>
-__device__ void clear_unnamed(const RowArgs& a, const SortArgs& s, int32_t first) {
+__device__ void clear_unnamed(const RowArgs& a, const SortArgs& s, int32_t group) {
     constexpr int N = GT == LD_F32 ? 4 : 8;
     __shared__ unsigned long long named;
-    if (threadIdx.x == 0) named = 0;
-    __syncthreads();
-    for (int32_t i = threadIdx.x; i < a.T; i += kFewThreads) {
-        const uint32_t r = key_of(s, i) - static_cast<uint32_t>(first);  // of an id before the first: a large number
-        if (r < kFewClear) atomicOr(&named, 1ull << r);
-    }
-    __syncthreads();
-    for (int32_t r = threadIdx.x / LD_WAVE; r < kFewClear && first + r < a.V; r += kFewWaves) {
-        if (named >> r & 1) continue;
-        for (int32_t l = ld_lane(); l * N < a.d; l += LD_WAVE)
-            store_columns<GT, N, true>(grad_row<GT>(a, first + r), columns_of<N>(l, a.d), typename LdVec<GT, N>::type(0));
+    for (int32_t left = a.V - group * kFewClear; left > 0; left -= a.clearing * kFewClear) {
+        const int32_t first = a.V - left, rows = left < kFewClear ? left : kFewClear;
+        if (threadIdx.x == 0) named = 0;
+        __syncthreads();
+        for (int32_t i = threadIdx.x; i < a.T; i += kFewThreads) {
+            const uint32_t r = key_of(s, i) - static_cast<uint32_t>(first);  // of an id before the first: a large number
+            if (r < kFewClear) atomicOr(&named, 1ull << r);
+        }
+        __syncthreads();
+        for (int32_t r = threadIdx.x / LD_WAVE; r < rows; r += kFewWaves) {
+            if (named >> r & 1) continue;
+            for (int32_t l = ld_lane(); l * N < a.d; l += LD_WAVE)
+                store_columns<GT, N, true>(grad_row<GT>(a, first + r), columns_of<N>(l, a.d), typename LdVec<GT, N>::type(0));
+        }
+        __syncthreads();
     }
 }
 
@@ -723,7 +733,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few(RowArgs a, SortArgs s, int3
     __shared__ typename X::wide came_sum[kFewWaves][LD_WAVE];
     __shared__ int32_t shared_valid;
     if (static_cast<int32_t>(blockIdx.x) >= a.adding) {
-        clear_unnamed<GT>(a, s, (static_cast<int32_t>(blockIdx.x) - a.adding) * kFewClear);
+        clear_unnamed<GT>(a, s, static_cast<int32_t>(blockIdx.x) - a.adding);
         return;
     }
     if (threadIdx.x == 0) shared_valid = 0;
@@ -840,6 +850,10 @@ int32_t few_shares(int64_t T, int32_t d) {
 
 bool few(int64_t T, int32_t d) { return T > 0 && T <= kFewTokens && d > 0 && T <= few_shares(T, d) * kFewMostShare; }
 
+constexpr int32_t kMostBlocks = (1 << 24) - 1;  // of 256 threads: a launch has fewer than 2^32
+
+int32_t at_most(int64_t n, int32_t most) { return n < most ? static_cast<int32_t>(n) : most; }
+
 bool sizes_fit(int64_t T, int64_t V, int32_t d) {
     return T >= 0 && V >= 0 && d >= 0 && d <= LD_MAX_WIDTH && T <= LD_MAX_TOKENS && V < INT32_MAX;
 }
@@ -865,7 +879,7 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     const Layout l = layout_of(T, V, d);
     if (few(T, d)) {
         const int32_t few_blocks = (d + kFewColumns - 1) / kFewColumns, adding = few_blocks * few_shares(T, d);
-        const int32_t clearing = accumulate ? 0 : static_cast<int32_t>((V + kFewClear - 1) / kFewClear);
+        const int32_t clearing = accumulate ? 0 : at_most((V + kFewClear - 1) / kFewClear, kMostBlocks / 4);
         const int32_t passes = T <= kCounted && V < (1 << (32 - kCountedBits)) - 1 ? 0 : l.passes;
         const SortArgs sort = {ids, id_dtype == LD_I64, nullptr, nullptr, nullptr, nullptr, nullptr, V, static_cast<int32_t>(T), 0, 0, 0, l.bits};
         const RowArgs a = {dout, nullptr, nullptr, grad, nullptr, dout_stride, grad_stride, 0, static_cast<int32_t>(T), static_cast<int32_t>(V), d,
@@ -882,7 +896,7 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     if (l.bytes > 0 && (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < l.bytes)) return LD_ERR_WORKSPACE;
     const int32_t columns = LD_WAVE * (dtype == LD_F32 ? 4 : 8), blocks = static_cast<int32_t>((static_cast<int64_t>(d) + columns - 1) / columns);
     const int64_t adding = (static_cast<int64_t>(l.chunks) * blocks + kRowWaves - 1) / kRowWaves;
-    if (adding + V / kClearRows >= INT32_MAX / kRowWaves) return LD_ERR_RANGE;
+    if (adding > kMostBlocks / 2) return LD_ERR_RANGE;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + l.keys), reinterpret_cast<uint32_t*>(ws + l.keys + l.at / 2)};
     uint32_t* at[2] = {reinterpret_cast<uint32_t*>(ws + l.at), reinterpret_cast<uint32_t*>(ws + l.at + l.at / 2)};
@@ -921,10 +935,10 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
         sort.at_in = at[last];
     }
     clear.from += clear.rows;
-    const int64_t clearing = accumulate ? 0 : (V - clear.from + kClearRows - 1) / kClearRows;
+    const int32_t clearing = accumulate ? 0 : at_most((V - clear.from + kClearRows - 1) / kClearRows, kMostBlocks / 2);
     const RowArgs a = {dout, keys[last], at[last], grad, reinterpret_cast<float*>(ws + l.part), dout_stride, grad_stride, l.part_stride,
                        static_cast<int32_t>(T), static_cast<int32_t>(V), d, l.chunk, l.window, blocks, static_cast<int32_t>(adding),
-                       static_cast<int32_t>(clearing), clear.from, scale};
+                       clearing, clear.from, scale};
     const dim3 grid(static_cast<uint32_t>(adding + clearing));
     const bool streamed = T * static_cast<int64_t>(d) * ld_type_bytes(dtype) > kStreamed;
     ld_with_type(dtype, [&](auto type) {

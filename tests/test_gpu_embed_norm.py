@@ -283,6 +283,24 @@ def test_tables_and_gradients_of_more_than_2_31_elements():
     assert bool((grad[1] == 1).all()) and bool((grad[2] == 2).all()) and not grad[0].any()
 
 
+def test_more_rows_than_a_launch_has_threads_for():
+    V = 70_000_001
+    for T in (3, 2000, 5000):
+        grad = torch.full((V, 1), 5.0, dtype=BF16, device=DEV)
+        ids = torch.arange(T, device=DEV) * (V // T)
+        ids[-1] = V - 1
+        ld.ld_embed_grad(torch.ones(T, 1, device=DEV), ids, grad, 3.0)
+        assert float(grad.float().sum()) == 3.0 * T and bool((grad[ids] == 3).all())
+
+
+def test_lookup_of_more_tokens_than_a_launch_takes():
+    table = torch.arange(300.0, device=DEV)[:, None].to(F16)
+    ids = torch.arange(2_200_000_000, device=DEV, dtype=torch.int32).remainder_(300)
+    out = ld.ld_embed_lookup(table, ids, 2.0)
+    for a in (0, 2_147_480_000, 2_199_990_000):
+        assert torch.equal(out[a:a + 10_000, 0], 2.0 * ids[a:a + 10_000].to(F16))
+
+
 # --------------------------------------------------------------------------------------- norm, clipping
 
 def clip64(parts, max_norm, dtype):
