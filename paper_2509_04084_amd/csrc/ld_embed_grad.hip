@@ -376,7 +376,7 @@ constexpr int kClearRows = 4;     // rows that a clearing workgroup looks after 
 constexpr int64_t kStreamed = 256 << 20;
 constexpr int kJoinWaves = 8;     // chunks of a joining workgroup
 constexpr int kJoinAlone = 8;     // partial sums that a wave adds up by itself
-constexpr int kJoinAhead = 16;    // else partial sums that each of the waves loads before it adds the first (8: 16384 tokens of one id 83 us instead of 63)
+constexpr int kJoinAhead = 8;     // partial sums that a wave loads before it adds the first (16: Llama's width 200 us instead of 196, 16384 tokens of one id 75 of 83)
 
 struct RowArgs {
     const void* dout;
@@ -582,18 +582,17 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
 }
 
 // Partial sums from, from + step, ... up to last of a long run that begins in chunk `first`.
-template <int AHEAD>
 __device__ __forceinline__ ld_f32x4 sum_parts(const RowArgs& a, Columns cols, int32_t first, int32_t from, int32_t last, int32_t step) {
     ld_f32x4 sum = ld_f32x4(0.0f);
-    for (int32_t j = from; j <= last; j += step * AHEAD) {
-        ld_f32x4 x[AHEAD];
+    for (int32_t j = from; j <= last; j += step * kJoinAhead) {
+        ld_f32x4 x[kJoinAhead];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
+        for (int u = 0; u < kJoinAhead; ++u) {
             const int64_t k = static_cast<int64_t>(j) + u * step;
             x[u] = k <= last ? load_columns<LD_F32, 4, false>(a.part + (2 * k + (k == first)) * a.part_stride, cols) : ld_f32x4(0.0f);
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) sum += x[u];
+        for (int u = 0; u < kJoinAhead; ++u) sum += x[u];
     }
     return sum;
 }
@@ -630,13 +629,13 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
     if (last >= 0 && alone) {
         typename LdVec<GT, N>::type held = typename LdVec<GT, N>::type(0);
         if (ADD) held = load_columns<GT, N, false>(grad_row<GT>(a, run), cols);
-        const ld_f32x4 sum = sum_parts<kJoinAlone>(a, cols, c, c, last, 1);
+        const ld_f32x4 sum = sum_parts(a, cols, c, c, last, 1);
         write_row<GT, N, ADD>(a, run, cols, sum, held);
     }
     for (int32_t w = 0; w < kJoinWaves; ++w) {
         const int32_t to = shared_last[w];
         if (to < 0) continue;
-        sh[wave][ld_lane()] = sum_parts<kJoinAhead>(a, cols, c0 + w, c0 + w + wave, to, kJoinWaves);
+        sh[wave][ld_lane()] = sum_parts(a, cols, c0 + w, c0 + w + wave, to, kJoinWaves);
         __syncthreads();
         if (wave == 0) {
             ld_f32x4 sum = sh[0][ld_lane()];
