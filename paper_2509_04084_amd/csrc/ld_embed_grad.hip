@@ -7,13 +7,18 @@
 // feedback and a recovery that replays differentials need it.
 //
 // Bound by memory where there are many tokens or rows to clear (16384 tokens of GPT-2 XL, 375 MB, 81 us; 65536 at Llama's width, 800 MB,
-// 195 us, of which the sum of the rows 157 at 5.2 TB/s), else by what waits on one another: the sort's launches of 4 to 8 us each (16384
-// tokens of GPT-2 XL's positions, 59 MB, 28 us), the two or three reads between an id and its row.
+// 194 us, of which the sum of the rows 157 at 5.2 TB/s), else by what waits on one another: the sort's launches of 4 to 8 us each (16384
+// tokens of GPT-2 XL's positions, 59 MB, 27 us), the two or three reads between an id and its row.
 #include <type_traits>
 
 #include "ld_elem.h"
 
 namespace {
+
+// A lane's value, in every lane.
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int32_t lane) {
+    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), lane));
+}
 
 // The columns of a lane: N from `column` on, of which the last `own` are its own. In the row's last vector, which ends with the
 // row, the first are the lane's before (their sums are made twice and written once); in rows of fewer than N columns they are none.
@@ -79,7 +84,8 @@ constexpr int64_t kHidden = 32 << 20;
 __device__ __forceinline__ bool cleared(const Clearing& c, int32_t own_blocks) {
     const int32_t block = static_cast<int32_t>(blockIdx.x) - own_blocks;
     if (block < 0) return false;
-    const int32_t per = blockDim.x / LD_WAVE, wave = block * per + threadIdx.x / LD_WAVE, waves = (static_cast<int32_t>(gridDim.x) - own_blocks) * per;
+    const int32_t per = blockDim.x / LD_WAVE, wave = block * per + threadIdx.x / LD_WAVE;
+    const int32_t waves = (static_cast<int32_t>(gridDim.x) - own_blocks) * per;
     if (c.wide) clear_span<LD_F32>(c, wave, waves);
     else clear_span<LD_BF16>(c, wave, waves);
     return true;
@@ -110,6 +116,13 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs& a, int32_t i) {
     if (!a.ids) return a.keys_in[i];
     const int64_t id = a.wide_ids ? static_cast<const int64_t*>(a.ids)[i] : static_cast<const int32_t*>(a.ids)[i];
     return static_cast<uint32_t>(id >= 0 && id < a.V ? id : a.V);
+}
+
+// A wave's counts cleared, 16 bytes a lane.
+__device__ __forceinline__ void clear_counts(uint16_t* seen, int32_t bins) {
+    for (int32_t i = 8 * ld_lane(); i < bins; i += 8 * LD_WAVE) __builtin_memset(__builtin_assume_aligned(seen + i, 16), 0, 16);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 // The token's place among those of its digit that its wave has had, `seen` (a count for each digit) being moved on.
@@ -155,7 +168,7 @@ template <int ROUNDS>
 struct SortShared {
     uint32_t keys[ROUNDS * kSortThreads];
     uint16_t tokens[ROUNDS * kSortThreads];
-    uint16_t seen[kSortWaves][kAloneBins];
+    __attribute__((aligned(16))) uint16_t seen[kSortWaves][kAloneBins];
     uint32_t first[kAloneBins], sh[kSortWaves];
 };
 
@@ -172,9 +185,7 @@ __device__ __forceinline__ void sort_in_shared(const SortArgs& a, int32_t passes
     }
     for (int32_t p = 0; p < passes; ++p) {
         const int32_t shift = p * a.bits;
-        for (int32_t i = ld_lane(); i < bins; i += LD_WAVE) m.seen[wave][i] = 0;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        clear_counts(m.seen[wave], bins);
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r)
             rank[r] = rank_in_wave((key[r] >> shift) & (bins - 1), base + r * LD_WAVE < a.T, a.bits, m.seen[wave]);
@@ -258,7 +269,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_count(SortArgs a, Clearin
 __global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a, Clearing c) {
     constexpr int kPer = kBins / kSortThreads, kLoads = 8;
     __shared__ uint32_t first[kBins];                // where this tile's next tokens of a digit go
-    __shared__ uint16_t seen[kSortWaves][kBins];
+    __shared__ __attribute__((aligned(16))) uint16_t seen[kSortWaves][kBins];
     __shared__ uint32_t part_before[kBins], part_all[kBins], sh[kSortWaves];
     const int32_t bins = 1 << a.bits, wave = threadIdx.x / LD_WAVE;
     const uint32_t mask = bins - 1;
@@ -318,9 +329,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a, Clearing
             key[r] = i < a.T ? key_of(a, i) : 0;
             at[r] = i < a.T && a.at_in ? a.at_in[i] : static_cast<uint32_t>(i);
         }
-        for (int32_t i = ld_lane(); i < bins; i += LD_WAVE) seen[wave][i] = 0;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        clear_counts(seen[wave], bins);
 #pragma unroll
         for (int r = 0; r < kSortRounds; ++r) rank[r] = rank_in_wave((key[r] >> a.shift) & mask, base + r * LD_WAVE < a.T, a.bits, seen[wave]);
         __syncthreads();
@@ -361,8 +370,8 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_move(SortArgs a, Clearing
 
 // The sorted tokens are cut into chunks of 4 to 32, a wave for each chunk and block of columns. It adds up, one after the other,
 // the runs of equal ids that begin in its chunk, to their ends where it can see them (in a window of 16 to 64 tokens from the
-// chunk's first on), and writes their rows. A run that goes on further is long: every chunk that it touches leaves a partial sum, and k_join adds those
-// up. Rows that no token names are cleared by workgroups of the same launch.
+// chunk's first on), and writes their rows. A run that goes on further is long: every chunk that it touches leaves a partial sum,
+// and k_join adds those up. Rows that no token names are cleared by workgroups of the same launch.
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / LD_WAVE;
 // Tokens whose rows a wave loads before it adds the first; where sums are added to what is there, the rows of grad that they end in with
@@ -376,7 +385,8 @@ constexpr int kClearRows = 4;     // rows that a clearing workgroup looks after 
 constexpr int64_t kStreamed = 256 << 20;
 constexpr int kJoinWaves = 8;     // chunks of a joining workgroup
 constexpr int kJoinAlone = 8;     // partial sums that a wave adds up by itself
-constexpr int kJoinAhead = 8;     // partial sums that a wave loads before it adds the first (16: Llama's width 200 us instead of 196, 16384 tokens of one id 75 of 83)
+// Partial sums that a wave loads before it adds the first. 16: Llama's width 200 us instead of 196, 16384 tokens of one id 75 instead of 83.
+constexpr int kJoinAhead = 8;
 
 struct RowArgs {
     const void* dout;
@@ -428,7 +438,8 @@ __device__ __forceinline__ typename LdElem<GT>::type* grad_row(const RowArgs& a,
 
 // A finished sum to its row, added to what the row held where ADD.
 template <int GT, int N, bool ADD>
-__device__ __forceinline__ void write_row(const RowArgs& a, uint32_t v, Columns c, typename LdVec<GT, N>::wide sum, typename LdVec<GT, N>::type held) {
+__device__ __forceinline__ void write_row(const RowArgs& a, uint32_t v, Columns c, typename LdVec<GT, N>::wide sum,
+                                          typename LdVec<GT, N>::type held) {
     const typename LdVec<GT, N>::wide old = LdVec<GT, N>::widen(held);
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] = ADD ? __fmaf_rn(a.scale, sum[e], old[e]) : a.scale * sum[e];
@@ -477,8 +488,9 @@ __device__ __forceinline__ Runs runs_of(const RowArgs& a, int32_t from) {
     const int32_t i = from + ld_lane(), b = i - LD_WAVE;
     r.key = i < a.T ? a.keys[i] : UINT32_MAX;
     const uint32_t before = b >= 0 ? a.keys[b] : UINT32_MAX;
-    const uint32_t last = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(before), LD_WAVE - 1));
-    const uint32_t below = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(last), static_cast<int>(r.key), kShr1, 0xf, 0xf, false));
+    const uint32_t last = lane_of(before, LD_WAVE - 1);
+    const uint32_t below = static_cast<uint32_t>(
+        __builtin_amdgcn_update_dpp(static_cast<int>(last), static_cast<int>(r.key), kShr1, 0xf, 0xf, false));
     const uint32_t below_before = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(before), kShr1, 0xf, 0xf, false));
     r.own = (1ull << a.chunk) - 1;
     r.heads = __ballot(r.key != below && ld_lane() < a.window);
@@ -529,9 +541,9 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
     typename X::wide sum = typename X::wide(0.0f);
     int32_t run = i;  // where the run being added up begins
     typename G::type held = typename G::type(0);  // its row of grad, where that is added to
-    const auto key_at = [&](int32_t j) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), j)); };
+    const auto key_at = [&](int32_t j) { return lane_of(r.key, j); };
     const auto load = [&](int32_t j) {
-        return load_columns<DT, N, STREAM>(dout + static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), j)) * a.dout_stride, cols);
+        return load_columns<DT, N, STREAM>(dout + lane_of(at, j) * a.dout_stride, cols);
     };
     const auto begins = [&](int32_t j) { return (r.heads >> j & 1) != 0; };
     const auto add = [&](int32_t j, typename X::type x, typename G::type row) {
@@ -615,7 +627,7 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
         if (own != 0 && (r.heads & ~r.own) == 0) {
             const int32_t first = LD_WAVE - 1 - __builtin_clzll(own);
             if (first < r.valid) {
-                run = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.key), first));
+                run = lane_of(r.key, first);
                 last = (wave_lower_bound(a.keys, a.T, run + 1) - 1) / a.chunk;
             }
         }
@@ -666,8 +678,10 @@ constexpr int kFewClear = 64;       // rows of a clearing workgroup
 constexpr int kFewShare = 32;
 constexpr int kFewMostShare = 128;
 constexpr int kFewGroups = 256;
-constexpr int kCountedBits = 8;     // up to so many tokens (their bits) a token's place is found by counting those that go before it: 8 tokens
-constexpr int kCounted = 1 << kCountedBits;  // 5.5 us instead of 8.1, 256 8.5 instead of 9.9 (512 11.8 instead of 10.5)
+// Up to 256 tokens a token's place is found by counting those that go before it: 8 tokens 5.5 us instead of 8.1, 256 8.5 instead of 9.9 (512
+// would be 11.8 instead of 10.5).
+constexpr int kCountedBits = 8;
+constexpr int kCounted = 1 << kCountedBits;
 
 // Sorts tokens of keys below 2^24 - 1, like sort_in_shared.
 __device__ __forceinline__ void count_in_shared(const SortArgs& a, SortShared<1>& m) {
@@ -740,7 +754,8 @@ __global__ __launch_bounds__(kFewThreads) void k_few(RowArgs a, SortArgs s, int3
     else sort_in_shared<1>(s, passes, m);
     {
         const int32_t i = threadIdx.x;
-        if (i < a.T && m.keys[i] < static_cast<uint32_t>(a.V) && (i + 1 == a.T || m.keys[i + 1] >= static_cast<uint32_t>(a.V))) shared_valid = i + 1;
+        const uint32_t none = a.V;
+        if (i < a.T && m.keys[i] < none && (i + 1 == a.T || m.keys[i + 1] >= none)) shared_valid = i + 1;
     }
     __syncthreads();
     // the workgroups of a block of columns share the tokens out from one run's beginning to another's
@@ -764,7 +779,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few(RowArgs a, SortArgs s, int3
     const uint32_t before = mine && from + ld_lane() > 0 ? m.keys[from + ld_lane() - 1] : UINT32_MAX;
     const uint64_t heads = __ballot(mine && key != before);
     const bool goes_on = count > 0 && from + count < end && m.keys[from + count] == m.keys[from + count - 1];
-    const auto key_at = [&](int32_t j) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key), j)); };
+    const auto key_at = [&](int32_t j) { return lane_of(key, j); };
     const typename X::elem* dout = static_cast<const typename X::elem*>(a.dout);
     typename X::wide sum = typename X::wide(0.0f);
     typename G::type held = typename G::type(0);
@@ -776,7 +791,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few(RowArgs a, SortArgs s, int3
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (i + u < count) {
-                x[u] = load_columns<DT, N, false>(dout + static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), i + u)) * a.dout_stride, cols);
+                x[u] = load_columns<DT, N, false>(dout + lane_of(at, i + u) * a.dout_stride, cols);
                 if (ADD && (heads >> (i + u) & 1)) row[u] = load_columns<GT, N, false>(grad_row<GT>(a, key_at(i + u)), cols);
             }
         }

@@ -211,8 +211,16 @@ class _Table:
 def _one_device(first: torch.Tensor, others: Sequence, *tables: _Table) -> None:
     """_same_device over single tensors and the tensors of tables."""
     at = first.get_device()
-    if at >= 0 and all(t is None or t.get_device() == at for t in others) and all(b.device == at or not b.sizes for b in tables):
-        return
+    if at >= 0:
+        for t in others:
+            if t is not None and t.get_device() != at:
+                break
+        else:
+            for b in tables:
+                if b.sizes and b.device != at:
+                    break
+            else:
+                return
     _same_device(first, *others, *(t for b in tables for t in b.tensors))
 
 
