@@ -77,7 +77,8 @@ __device__ __forceinline__ void clear_span(const Clearing& c, int32_t wave, int3
 
 // Bytes that a launch of the sort clears: about what is written in its time. GPT-2 XL's 16 K tokens without it 97.7 us, with 16 MB 89.5,
 // 32 MB 86.8, 48 MB 88.8. Rows that tokens name are written twice so: at Llama's width 65 K tokens of 32 K rows 182 and 192 us; it is done
-// where there are fewer tokens than rows.
+// where there are fewer tokens than rows. The launch that sorts 2049 to 4096 tokens alone takes as long as two: 4096 tokens of GPT-2 XL with 32 MB
+// 78 us, with 64 MB 72 (2048 tokens 70 either way).
 constexpr int64_t kHidden = 32 << 20;
 
 // Whether a workgroup is one of those, its work then done.
@@ -918,7 +919,8 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     SortArgs sort = {ids, id_dtype == LD_I64, nullptr, nullptr, keys[0], at[0], reinterpret_cast<uint32_t*>(ws + l.counts), V,
                      static_cast<int32_t>(T), l.tiles, l.per_tile, 0, l.bits};
     Clearing clear = {grad, grad_stride, d, ld_type_bytes(grad_dtype) == 4, 0, 0};
-    const int64_t hidden = accumulate || T > V ? 0 : kHidden / (static_cast<int64_t>(d) * ld_type_bytes(grad_dtype));  // rows a launch
+    const int64_t hidden_bytes = accumulate || T > V ? 0 : l.tiles == 1 && T > 2 * kSortThreads ? 2 * kHidden : kHidden;
+    const int64_t hidden = hidden_bytes / (static_cast<int64_t>(d) * ld_type_bytes(grad_dtype));  // rows a launch
     const auto blocks_of = [&](int32_t own) {  // of a launch that clears the next rows as well
         clear.from += clear.rows;
         clear.rows = static_cast<int32_t>(V - clear.from < hidden ? V - clear.from : hidden);
