@@ -194,6 +194,24 @@ def test_embed_grad_of_many_tokens(T, V, d, kind):
     check_grad(T, V, d, kind, BF16, F32, seed=5)
 
 
+@pytest.mark.parametrize("length", [2, 3, 15, 16, 17, 31, 32, 33, 63, 64, 65, 130])
+@pytest.mark.parametrize("T,d", [(200, 5), (900, 300), (1500, 600), (5000, 1100), (20000, 1100), (70000, 2100)])
+def test_embed_grad_of_runs_of_every_length(T, d, length):
+    """Whole numbers, so that every order of adding gives the same: ids that are each named as often, from some offset on."""
+    print(f"[embed_grad] T={T} d={d} runs of {length}", flush=True)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T + length)
+    for offset in (0, 7):
+        ids = ((torch.arange(T, device=DEV) + offset) // length)[torch.randperm(T, device=DEV, generator=g)]
+        V = (T + offset) // length + 2
+        x = torch.randint(-2, 3, (T, d), device=DEV, generator=g).to(BF16)
+        want = torch.zeros(V, d, device=DEV).index_add_(0, ids, x.float())
+        for accumulate in (False, True):
+            grad = torch.full((V, d), 4.0, device=DEV)
+            ld.ld_embed_grad(x, ids, grad, accumulate=accumulate)
+            assert torch.equal(grad, want + 4.0 if accumulate else want), (offset, accumulate)
+
+
 def test_embed_grad_of_nothing():
     grad = torch.ones(5, 7, device=DEV)
     none, x = torch.zeros(0, dtype=torch.int64, device=DEV), torch.zeros(0, 7, device=DEV)
