@@ -21,7 +21,8 @@ __device__ __forceinline__ uint32_t lane_of(uint32_t x, int32_t lane) {
 }
 
 // The columns of a lane: N from `column` on, of which the last `own` are its own. In the row's last vector, which ends with the
-// row, the first are the lane's before (their sums are made twice and written once); in rows of fewer than N columns they are none.
+// row, the first are the lane's before (their sums are made twice and written once). Rows have N columns at least, but where they are
+// only cleared.
 struct Columns {
     int32_t column, own;
 };
@@ -34,15 +35,8 @@ __device__ __forceinline__ Columns columns_of(int32_t vector, int32_t d) {
 
 template <int DT, int N, bool STREAM>
 __device__ __forceinline__ typename LdVec<DT, N>::type load_columns(const typename LdElem<DT>::type* row, Columns c) {
-    if (c.column >= 0) {
-        const typename LdVec<DT, N>::type* p = reinterpret_cast<const typename LdVec<DT, N>::type*>(row + c.column);
-        return STREAM ? __builtin_nontemporal_load(p) : *p;
-    }
-    typename LdVec<DT, N>::type x = typename LdVec<DT, N>::type(0);
-#pragma unroll
-    for (int e = 1; e < N; ++e)
-        if (e + c.column >= 0) x[e] = row[e + c.column];
-    return x;
+    const typename LdVec<DT, N>::type* p = reinterpret_cast<const typename LdVec<DT, N>::type*>(row + c.column);
+    return STREAM ? __builtin_nontemporal_load(p) : *p;
 }
 
 template <int DT, int N, bool STREAM>
@@ -501,9 +495,8 @@ __device__ __forceinline__ Runs runs_of(const RowArgs& a, int32_t from) {
     return r;
 }
 
-template <int DT, int GT, bool STREAM, bool ADD>
+template <int DT, int GT, int N, bool STREAM, bool ADD>
 __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
-    constexpr int N = DT == LD_F32 ? 4 : 8;
     typedef LdVec<DT, N> X;
     typedef LdVec<GT, N> G;
     int32_t block = blockIdx.x;
@@ -595,14 +588,16 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
 }
 
 // Partial sums from, from + step, ... up to last of a long run that begins in chunk `first`.
-__device__ __forceinline__ ld_f32x4 sum_parts(const RowArgs& a, Columns cols, int32_t first, int32_t from, int32_t last, int32_t step) {
-    ld_f32x4 sum = ld_f32x4(0.0f);
+template <int N>
+__device__ __forceinline__ typename LdVec<LD_F32, N>::wide sum_parts(const RowArgs& a, Columns cols, int32_t first, int32_t from, int32_t last, int32_t step) {
+    typedef typename LdVec<LD_F32, N>::wide Sum;
+    Sum sum = Sum(0.0f);
     for (int32_t j = from; j <= last; j += step * kJoinAhead) {
-        ld_f32x4 x[kJoinAhead];
+        Sum x[kJoinAhead];
 #pragma unroll
         for (int u = 0; u < kJoinAhead; ++u) {
             const int64_t k = static_cast<int64_t>(j) + u * step;
-            x[u] = k <= last ? load_columns<LD_F32, 4, false>(a.part + (2 * k + (k == first)) * a.part_stride, cols) : ld_f32x4(0.0f);
+            x[u] = k <= last ? load_columns<LD_F32, N, false>(a.part + (2 * k + (k == first)) * a.part_stride, cols) : Sum(0.0f);
         }
 #pragma unroll
         for (int u = 0; u < kJoinAhead; ++u) sum += x[u];
@@ -611,11 +606,11 @@ __device__ __forceinline__ ld_f32x4 sum_parts(const RowArgs& a, Columns cols, in
 }
 
 // Adds up the partial sums of long runs, each from the chunk that it begins in to the one that it ends in, in their order. A wave
-// looks at a chunk, with 256 columns; what it would be long busy with is shared by the workgroup's waves, which take partial sums in turn.
-template <int GT, bool ADD>
+// looks at a chunk, with 64 N columns; what it would be long busy with is shared by the workgroup's waves, which take partial sums in turn.
+template <int GT, int N, bool ADD>
 __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_t chunks) {
-    constexpr int N = 4;
-    __shared__ ld_f32x4 sh[kJoinWaves][LD_WAVE];
+    typedef typename LdVec<LD_F32, N>::wide Sum;
+    __shared__ Sum sh[kJoinWaves][LD_WAVE];
     __shared__ int32_t shared_last[kJoinWaves];
     __shared__ uint32_t shared_run[kJoinWaves];
     const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LD_WAVE), c0 = blockIdx.x * kJoinWaves, c = c0 + wave;
@@ -642,16 +637,16 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
     if (last >= 0 && alone) {
         typename LdVec<GT, N>::type held = typename LdVec<GT, N>::type(0);
         if (ADD) held = load_columns<GT, N, false>(grad_row<GT>(a, run), cols);
-        const ld_f32x4 sum = sum_parts(a, cols, c, c, last, 1);
+        const Sum sum = sum_parts<N>(a, cols, c, c, last, 1);
         write_row<GT, N, ADD>(a, run, cols, sum, held);
     }
     for (int32_t w = 0; w < kJoinWaves; ++w) {
         const int32_t to = shared_last[w];
         if (to < 0) continue;
-        sh[wave][ld_lane()] = sum_parts(a, cols, c0 + w, c0 + w + wave, to, kJoinWaves);
+        sh[wave][ld_lane()] = sum_parts<N>(a, cols, c0 + w, c0 + w + wave, to, kJoinWaves);
         __syncthreads();
         if (wave == 0) {
-            ld_f32x4 sum = sh[0][ld_lane()];
+            Sum sum = sh[0][ld_lane()];
 #pragma unroll
             for (int i = 1; i < kJoinWaves; ++i) sum += sh[i][ld_lane()];
             typename LdVec<GT, N>::type held = typename LdVec<GT, N>::type(0);
@@ -738,9 +733,8 @@ __device__ void clear_unnamed(const RowArgs& a, const SortArgs& s, int32_t group
     }
 }
 
-template <int DT, int GT, bool ADD>
+template <int DT, int GT, int N, bool ADD>
 __global__ __launch_bounds__(kFewThreads) void k_few(RowArgs a, SortArgs s, int32_t passes) {
-    constexpr int N = kFewVector;
     typedef LdVec<DT, N> X;
     typedef LdVec<GT, N> G;
     __shared__ SortShared<1> m;
@@ -865,6 +859,13 @@ int32_t few_shares(int64_t T, int32_t d) {
 
 bool few(int64_t T, int32_t d) { return T > 0 && T <= kFewTokens && d > 0 && T <= few_shares(T, d) * kFewMostShare; }
 
+// Calls f with the columns of a lane: N, or one where a row has fewer (a block of 64 columns then holds it).
+template <int N, typename F>
+void with_vector(int32_t d, F f) {
+    if (d >= N) f(std::integral_constant<int, N>());
+    else f(std::integral_constant<int, 1>());
+}
+
 constexpr int32_t kMostBlocks = (1 << 24) - 1;  // of 256 threads: a launch has fewer than 2^32
 
 int32_t at_most(int64_t n, int32_t most) { return n < most ? static_cast<int32_t>(n) : most; }
@@ -902,8 +903,11 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
         ld_begin_call();
         ld_with_type(dtype, [&](auto type) {
             ld_with_type(grad_dtype, [&](auto grad_type) {
-                if (accumulate) k_few<type, grad_type, true><<<dim3(adding), dim3(kFewThreads), 0, s>>>(a, sort, passes);
-                else k_few<type, grad_type, false><<<dim3(adding + clearing), dim3(kFewThreads), 0, s>>>(a, sort, passes);
+                const dim3 grid(adding + clearing), threads(kFewThreads);
+                with_vector<kFewVector>(d, [&](auto n) {
+                    if (accumulate) k_few<type, grad_type, n, true><<<grid, threads, 0, s>>>(a, sort, passes);
+                    else k_few<type, grad_type, n, false><<<grid, threads, 0, s>>>(a, sort, passes);
+                });
             });
         });
         return ld_launch_status();
@@ -959,21 +963,26 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     const bool streamed = T * static_cast<int64_t>(d) * ld_type_bytes(dtype) > kStreamed;
     ld_with_type(dtype, [&](auto type) {
         ld_with_type(grad_dtype, [&](auto grad_type) {
-            if (accumulate) {
-                if (streamed) k_rows<type, grad_type, true, true><<<grid, dim3(kRowThreads), 0, s>>>(a);
-                else k_rows<type, grad_type, false, true><<<grid, dim3(kRowThreads), 0, s>>>(a);
-            } else {
-                if (streamed) k_rows<type, grad_type, true, false><<<grid, dim3(kRowThreads), 0, s>>>(a);
-                else k_rows<type, grad_type, false, false><<<grid, dim3(kRowThreads), 0, s>>>(a);
-            }
+            with_vector<type == LD_F32 ? 4 : 8>(d, [&](auto n) {
+                constexpr bool kWide = n > 1;  // narrow rows are never so many bytes that it matters
+                if (accumulate) {
+                    if (streamed) k_rows<type, grad_type, n, kWide, true><<<grid, dim3(kRowThreads), 0, s>>>(a);
+                    else k_rows<type, grad_type, n, false, true><<<grid, dim3(kRowThreads), 0, s>>>(a);
+                } else {
+                    if (streamed) k_rows<type, grad_type, n, kWide, false><<<grid, dim3(kRowThreads), 0, s>>>(a);
+                    else k_rows<type, grad_type, n, false, false><<<grid, dim3(kRowThreads), 0, s>>>(a);
+                }
+            });
         });
     });
     if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
     if (T < l.window) return LD_OK;  // no run is long
     ld_with_type(grad_dtype, [&](auto grad_type) {
         const dim3 joins((l.chunks + kJoinWaves - 1) / kJoinWaves, (d + 4 * LD_WAVE - 1) / (4 * LD_WAVE));
-        if (accumulate) k_join<grad_type, true><<<joins, dim3(kJoinWaves * LD_WAVE), 0, s>>>(a, l.chunks);
-        else k_join<grad_type, false><<<joins, dim3(kJoinWaves * LD_WAVE), 0, s>>>(a, l.chunks);
+        with_vector<4>(d, [&](auto n) {
+            if (accumulate) k_join<grad_type, n, true><<<joins, dim3(kJoinWaves * LD_WAVE), 0, s>>>(a, l.chunks);
+            else k_join<grad_type, n, false><<<joins, dim3(kJoinWaves * LD_WAVE), 0, s>>>(a, l.chunks);
+        });
     });
     return ld_launch_status();
 }

@@ -127,14 +127,18 @@ __device__ __forceinline__ void scale_piece(const B& b, int32_t p, int32_t me, f
     if (at.have == piece_elems<N>()) {
         const typename V::type* v = reinterpret_cast<const typename V::type*>(src) + me;
         typename O::type* o = reinterpret_cast<typename O::type*>(dst) + me;
-        typename V::type x[kVectors];
+#pragma unroll 1
+        for (int u0 = 0; u0 < kVectors; u0 += kUnroll) {
+            typename V::type x[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kVectors; ++u) x[u] = __builtin_nontemporal_load(v + u * THREADS);
+            for (int u = 0; u < kUnroll; ++u) x[u] = __builtin_nontemporal_load(v + (u0 + u) * THREADS);
 #pragma unroll
-        for (int u = 0; u < kVectors; ++u) __builtin_nontemporal_store(O::narrow(V::widen(x[u]) * factor), o + u * THREADS);
+            for (int u = 0; u < kUnroll; ++u)
+                __builtin_nontemporal_store(O::narrow(V::widen(x[u]) * factor), o + (u0 + u) * THREADS);
+        }
         return;
     }
-#pragma unroll
+#pragma unroll kUnroll
     for (int u = 0; u < kVectors; ++u) {
         const int32_t i = (u * THREADS + me) * N;
         if (i + N <= at.have) {
