@@ -495,8 +495,14 @@ __device__ __forceinline__ Runs runs_of(const RowArgs& a, int32_t from) {
     return r;
 }
 
+// Waves of a SIMD that k_rows' registers leave room for. For fp32 gradients four are asked for: the kernel waits for its loads, and
+// 16384 tokens of 1600 columns into 50257 fp32 rows measured 102 us instead of 112 (into 1024 rows 40 and 41, 32768 tokens of 4096
+// columns into bf16 rows 186 and 184). The 16-bit types hold twice the columns a lane: fp16 with accumulation spills at four, 67 us
+// instead of 58, and they keep what the compiler chooses.
+constexpr int row_occupancy(int dt) { return dt == LD_F32 ? 4 : 1; }
+
 template <int DT, int GT, int N, bool STREAM, bool ADD>
-__global__ __launch_bounds__(kRowThreads) void k_rows(RowArgs a) {
+__global__ __launch_bounds__(kRowThreads, row_occupancy(DT)) void k_rows(RowArgs a) {
     typedef LdVec<DT, N> X;
     typedef LdVec<GT, N> G;
     int32_t block = blockIdx.x;
@@ -662,7 +668,7 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
 // All in one launch. Every workgroup sorts all tokens for itself, takes a block of columns and a share of the tokens, from where one
 // run begins to where another does, and deals them out to its waves; a run that goes on in the next wave's tokens is added up in
 // shared memory. Other workgroups clear the rows that no token names. Added to 50257 rows of 1600 columns, as three launches and so:
-// 8 tokens 10.4 and 5.5 us, 64 12.5 and 6.6, 256 14.6 and 8.5, 512 15.2 and 10.5, 1024 17.8 and 11.2; 1024 of one id 19.7 and 27.
+// 8 tokens 10.4 and 5.5 us, 64 12.5 and 6.6, 256 14.6 and 8.5, 512 15.2 and 10.5, 1024 17.8 and 11.2; 1024 of one id 19.7 and 23.
 constexpr int kFewThreads = kSortThreads;
 constexpr int kFewWaves = kFewThreads / LD_WAVE;
 constexpr int kFewTokens = kSortThreads;
