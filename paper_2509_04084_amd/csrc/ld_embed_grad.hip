@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "ld_elem.h"
+#include "ld_grid.h"
 
 namespace {
 
@@ -669,12 +670,11 @@ __global__ __launch_bounds__(kJoinWaves * LD_WAVE) void k_join(RowArgs a, int32_
 // run begins to where another does, and deals them out to its waves; a run that goes on in the next wave's tokens is added up in
 // shared memory. Other workgroups clear the rows that no token names. Added to 50257 rows of 1600 columns, as three launches and so:
 // 8 tokens 10.4 and 5.5 us, 64 12.5 and 6.6, 256 14.6 and 8.5, 512 15.2 and 10.5, 1024 17.8 and 11.2; 1024 of one id 19.7 and 23.
-constexpr int kFewThreads = kSortThreads;
+static_assert(kFewThreads == kSortThreads, "every workgroup sorts");
 constexpr int kFewWaves = kFewThreads / LD_WAVE;
 constexpr int kFewTokens = kSortThreads;
 constexpr int kFewVector = 2;       // columns of a lane: narrow blocks, for more workgroups
 constexpr int kFewColumns = kFewVector * LD_WAVE;
-constexpr int kFewClear = 64;       // rows of a clearing workgroup
 // Tokens of a share at least, and at most: so many that a share is no more than 8 tokens for a wave. Shares of 32, 64 and 128: 1024 tokens of
 // 256 columns 10.9, 11.2, 12.8 us, of 4096 24.9, 16.9, 15.8: no more workgroups than compute units, each sorts.
 constexpr int kFewShare = 32;
@@ -901,7 +901,7 @@ extern "C" ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_
     const Layout l = layout_of(T, V, d);
     if (few(T, d)) {
         const int32_t few_blocks = (d + kFewColumns - 1) / kFewColumns, adding = few_blocks * few_shares(T, d);
-        const int32_t clearing = accumulate ? 0 : at_most((V + kFewClear - 1) / kFewClear, kMostBlocks / 4);
+        const int32_t clearing = accumulate ? 0 : ld_few_clearing(V, adding);
         const int32_t passes = T <= kCounted && V < (1 << (32 - kCountedBits)) - 1 ? 0 : l.passes;
         const SortArgs sort = {ids, id_dtype == LD_I64, nullptr, nullptr, nullptr, nullptr, nullptr, V, static_cast<int32_t>(T), 0, 0, 0, l.bits};
         const RowArgs a = {dout, nullptr, nullptr, grad, nullptr, dout_stride, grad_stride, 0, static_cast<int32_t>(T), static_cast<int32_t>(V), d,

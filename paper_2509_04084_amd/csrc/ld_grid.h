@@ -1,0 +1,17 @@
+// Sizes of launches, apart from their kernels so that host code can be built from it as well: the tests try them at sizes
+// that no test allocates.
+#pragma once
+
+#include <stdint.h>
+
+// Workgroups of `threads` threads that a launch takes beside `others` of the same size, at most `wanted`: a launch has fewer
+// than 2^32 threads in a dimension.
+inline int32_t ld_workgroups(int64_t wanted, int32_t threads, int64_t others = 0) {
+    const int64_t most = ((static_cast<int64_t>(1) << 32) - 1) / threads - others;
+    return static_cast<int32_t>(wanted < most ? wanted : most);
+}
+
+// A few tokens' embedding gradient: the workgroups that clear rows beside the `adding` ones.
+constexpr int32_t kFewThreads = 1024;
+constexpr int32_t kFewClear = 64;  // rows of a clearing workgroup at a time
+inline int32_t ld_few_clearing(int64_t V, int32_t adding) { return ld_workgroups((V + kFewClear - 1) / kFewClear, kFewThreads, adding); }
