@@ -14,16 +14,14 @@
 #include <type_traits>
 
 #include "ld_elem.h"
+#include "ld_grid.h"
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kClipThreads;
 constexpr int kUnroll = 4;                 // vectors per thread and piece
 constexpr int kTensorGroup = 16;
 constexpr int kNormGrid = 2048;            // workgroups of a launch, each with a partial sum
-// Workgroups of a launch that clips in place, where all may find that nothing is to be done: GPT-2 XL under the limit 494 us in all, clipping
-// 1048; with one for every piece, as out of place, 520 and 989, with 2048 483 and 1122.
-constexpr int kInPlaceGrid = 16384;
 // Consecutive pieces that an XCD clips at a time, as for the snapshot: 3.1 GB of one tensor 1491 us in runs of 64, 1494 of 16, 1688 of 4, 1569
 // piece by piece. The sum, in rounds of the same workgroups, is no faster so (490 us; 102 MB 25 instead of 23).
 constexpr uint32_t kXcdRun = 64;
@@ -313,7 +311,7 @@ ld_status clip(const Lists& l, const double* part, int32_t count, float max_norm
         if (pieces == 0 && !alone) continue;
         int32_t in_place = l.src_type == l.dst_type;
         for (int32_t i = from; i < t; ++i) in_place &= l.n_elems[i] == 0 || l.src[i] == l.dst[i];
-        const dim3 grid(in_place && pieces > kInPlaceGrid ? kInPlaceGrid : (pieces + 7) / 8 * 8);
+        const dim3 grid(ld_clip_grid(pieces, in_place != 0));
         ld_with_type(l.src_type, [&](auto type) {
             ld_with_type(l.dst_type, [&](auto out_type) {
                 if (alone) k_clip_alone<type, out_type, B><<<dim3(1), dim3(kAloneThreads), 0, s>>>(b, max_norm, in_place, norm);

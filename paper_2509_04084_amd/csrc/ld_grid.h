@@ -15,3 +15,13 @@ inline int32_t ld_workgroups(int64_t wanted, int32_t threads, int64_t others = 0
 constexpr int32_t kFewThreads = 1024;
 constexpr int32_t kFewClear = 64;  // rows of a clearing workgroup at a time
 inline int32_t ld_few_clearing(int64_t V, int32_t adding) { return ld_workgroups((V + kFewClear - 1) / kFewClear, kFewThreads, adding); }
+
+// Clipping: the workgroups that share `pieces` pieces out, a multiple of 8 (XCDs).
+constexpr int32_t kClipThreads = 256;
+// Workgroups of a launch that clips in place, where all may find that nothing is to be done: GPT-2 XL under the limit 494 us in all, clipping
+// 1048; with one for every piece, as out of place, 520 and 989, with 2048 483 and 1122.
+constexpr int32_t kInPlaceGrid = 16384;
+inline int32_t ld_clip_grid(int32_t pieces, bool in_place) {
+    if (in_place && pieces > kInPlaceGrid) return kInPlaceGrid;
+    return ld_workgroups((static_cast<int64_t>(pieces) + 7) / 8 * 8, kClipThreads) / 8 * 8;
+}

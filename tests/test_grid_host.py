@@ -13,6 +13,7 @@ SHIM = """
 extern "C" {
 int32_t workgroups(int64_t wanted, int32_t threads, int64_t others) { return ld_workgroups(wanted, threads, others); }
 int32_t few_clearing(int64_t V, int32_t adding) { return ld_few_clearing(V, adding); }
+int32_t clip_grid(int32_t pieces, int32_t in_place) { return ld_clip_grid(pieces, in_place != 0); }
 }
 """
 
@@ -45,3 +46,13 @@ def test_rows_cleared_beside_few_tokens(shim):
             got = shim.few_clearing(ctypes.c_int64(V), adding)
             assert 1 <= got <= (V + 63) // 64 and (got + adding) * 1024 < 2 ** 32, (V, adding)
             assert got == (V + 63) // 64 or (got + adding + 1) * 1024 >= 2 ** 32, (V, adding)
+
+
+def test_workgroups_that_clip(shim):
+    """2^41 elements in all are 2^29 pieces, and one more for each tensor: they are shared out where a launch has no workgroup for each."""
+    for pieces in (1, 7, 8, 9, 16384, 16385, 2 ** 24 - 9, 2 ** 24 - 8, 2 ** 24 - 7, 2 ** 24, 2 ** 24 + 1, 2 ** 29 + 2 ** 20):
+        places = (pieces + 7) // 8 * 8
+        out, inside = shim.clip_grid(pieces, 0), shim.clip_grid(pieces, 1)
+        assert out % 8 == 0 and out == min(places, 2 ** 24 - 8) and out * 256 < 2 ** 32, pieces
+        assert inside == (places if pieces <= 16384 else 16384), pieces
+        assert places - 1 + out < 2 ** 31  # a workgroup's pieces, from one to the next
