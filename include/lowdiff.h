@@ -455,7 +455,7 @@ ld_status ld_combine_sparse_strategy(const int32_t* const* idx, const float* con
  *   out[t][i] = round(fl32(grad[t][i] * f)),  f = fl32(max_norm / sqrt(*sumsq)) where
  *   sqrt(*sumsq) > max_norm, else 1
  * A sum that is infinite or NaN scales nothing (f = 1); the caller finds that in the
- * norm.
+ * norm.  A finite sum whose root is beyond fp32 does clip, and *norm is infinite.
  *   out        host array of n_tensors dev pointers to elements of `out_dtype`; each
  *              is the tensor itself (in place; then out_dtype = dtype) or overlaps no
  *              tensor of the call

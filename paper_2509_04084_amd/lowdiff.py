@@ -610,7 +610,7 @@ def ld_grad_norm(grads: Sequence[torch.Tensor], sumsq: Optional[torch.Tensor] = 
 def ld_clip_grads(grads: Sequence[torch.Tensor], sumsq: torch.Tensor, max_norm: float,
                   outs: Optional[Sequence[torch.Tensor]] = None, stream=None) -> None:
     """Scales the tensors by max_norm / sqrt(sumsq) where that root is larger than max_norm: in place, or into
-    `outs` (of one type, which may be another; copied unscaled where the norm is not larger, or not finite)."""
+    `outs` (of one type, which may be another; copied unscaled where the root is not larger, or not finite)."""
     got = _lists(grads, outs)
     if sumsq.numel() < 1:
         raise ValueError("sumsq needs an element")
@@ -626,8 +626,9 @@ def ld_clip_grads(grads: Sequence[torch.Tensor], sumsq: torch.Tensor, max_norm: 
 def ld_clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, outs: Optional[Sequence[torch.Tensor]] = None,
                       norm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
-    """ld_grad_norm and ld_clip_grads in one call. Returns the norm before clipping, a float32[1] on the device; a step
-    whose norm is not finite is left unscaled, and the caller sees it there."""
+    """ld_grad_norm and ld_clip_grads in one call. Returns the norm before clipping, a float32[1] on the device. A step whose
+    sum of squares is not finite (an infinity or NaN among the gradients) is left unscaled, and the norm tells the caller. The sum
+    is 64 bits wide: finite gradients whose norm is only too large for 32 bits are clipped, though the norm reads infinite."""
     lib = load()
     got = _lists(grads, outs)
     dev = grads[0].device if got else norm.device if norm is not None else torch.device("cuda", torch.cuda.current_device())
