@@ -453,7 +453,7 @@ ld_status ld_combine_sparse_strategy(const int32_t* const* idx, const float* con
  *
  * ld_clip_grads - scales the tensors down to a norm of max_norm:
  *   out[t][i] = round(fl32(grad[t][i] * f)),  f = fl32(max_norm / sqrt(*sumsq)) where
- *   sqrt(*sumsq) > max_norm, else 1
+ *   sqrt(*sumsq) > max_norm, else 1  (nothing is added to the divisor)
  * A sum that is infinite or NaN scales nothing (f = 1); the caller finds that in the
  * norm.  A finite sum whose root is beyond fp32 does clip, and *norm is infinite.
  *   out        host array of n_tensors dev pointers to elements of `out_dtype`; each
@@ -488,7 +488,8 @@ ld_status ld_clip_grad_norm(const void* const* grad, void* const* out, const int
  *   pos_table  dev [P] rows of d elements of `dtype`, pos_stride >= 0 apart, or NULL
  *   ids        dev [T] of `id_dtype` (LD_I32 or LD_I64)
  *   positions  dev [T] of `id_dtype`; read only with a pos_table
- *   out        dev [T] rows of d elements of `out_dtype`, out_stride >= d apart
+ *   out        dev [T] rows of d elements of `out_dtype`, out_stride >= d apart; overlaps
+ *              none of the inputs
  *   T, V, P >= 0;  0 <= d <= LD_MAX_WIDTH  (T = 0 or d = 0 enqueues nothing)
  * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_HIP.
  */
@@ -515,7 +516,10 @@ ld_status ld_embed_lookup(const void* table, int64_t V, int64_t table_stride,
  *   T          0 <= T <= LD_MAX_TOKENS;  V  0 <= V < 2^31 - 1;  0 <= d <= LD_MAX_WIDTH
  *              (T d beyond any GPU's memory, as a broadcast dout can have it, is LD_ERR_RANGE)
  *   workspace  dev, 256-byte aligned, ld_embed_grad_workspace() bytes (0 for few
- *              tokens: then it may be NULL)
+ *              tokens: then it may be NULL).  16 T for the sort, and for partial sums of
+ *              rows that many tokens name 2 T d, T d, T d / 2 and T d / 4 bytes: fewer the more
+ *              work there is, the steps being at 8192, 32768 and 262144 tokens of up
+ *              to 512 columns (a half, a quarter .. of the tokens where rows are wider)
  * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_WORKSPACE, LD_ERR_HIP.
  */
 #define LD_MAX_TOKENS (1 << 24)

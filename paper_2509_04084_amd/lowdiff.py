@@ -609,7 +609,8 @@ def ld_grad_norm(grads: Sequence[torch.Tensor], sumsq: Optional[torch.Tensor] = 
 
 def ld_clip_grads(grads: Sequence[torch.Tensor], sumsq: torch.Tensor, max_norm: float,
                   outs: Optional[Sequence[torch.Tensor]] = None, stream=None) -> None:
-    """Scales the tensors by max_norm / sqrt(sumsq) where that root is larger than max_norm: in place, or into
+    """Scales the tensors by max_norm / sqrt(sumsq) where that root is larger than max_norm (by the quotient itself:
+    torch.nn.utils.clip_grad_norm_ adds 1e-6 to the norm and so scales a little further): in place, or into
     `outs` (of one type, which may be another; copied unscaled where the root is not larger, or not finite)."""
     got = _lists(grads, outs)
     if sumsq.numel() < 1:
@@ -675,7 +676,8 @@ def ld_embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, 
                     out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """scale * table[ids] (+ pos_table[positions]) in `out` or a new tensor of shape ids.shape + (d,) and type
     `out_dtype` (the table's unless given). Rows outside their table count as zeros. The tables, and an `out` of two
-    dimensions, may have any row stride."""
+    dimensions, may have any row stride; `out` overlaps none of the inputs. Autograd records nothing, whatever the table's
+    requires_grad: the table's gradient is ld_embed_grad's to make."""
     if (pos_table is None) != (positions is None):
         raise ValueError("pos_table and positions go together")
     d, T = table.shape[-1], ids.numel()
@@ -710,7 +712,8 @@ def ld_embed_grad_workspace(T: int, V: int, d: int) -> int:
 def ld_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
                   workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """The gradient of ld_embed_lookup by its table from that of its output, `dout` (ids.shape + (d,), or [T, d] with any
-    row stride): written to `grad` [V, d], or with `accumulate` added to it. Deterministic."""
+    row stride): written to `grad` [V, d], or with `accumulate` added to it. Deterministic. A workspace that is not given is
+    allocated for the call: ld_embed_grad_workspace bytes, for a small batch about as many as its `dout` has in 16 bits."""
     lib = load()
     T, d = ids.numel(), grad.shape[-1]
     if dout.shape[-1] != d or dout.numel() != T * d:
