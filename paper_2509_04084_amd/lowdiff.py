@@ -224,14 +224,14 @@ def _one_device(first: torch.Tensor, others: Sequence, *tables: _Table) -> None:
     _same_device(first, *others, *(t for b in tables for t in b.tensors))
 
 
-def _empty(shape, dtype, device, stream) -> torch.Tensor:
+def _empty(dtype, device, stream, *shape) -> torch.Tensor:
     """An uninitialised tensor out of the memory that torch's allocator keeps for `stream` (None: the current one). What it keeps for
     another stream may be a block that was just given back and that kernels of that stream, still to run, use."""
     if stream is None or torch.device(device).type != "cuda" or \
             (_current_raw_stream is not None and _current_raw_stream(stream.device_index) == stream.cuda_stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
 
 
 def _record(t: torch.Tensor, *streams) -> torch.Tensor:
@@ -242,18 +242,19 @@ def _record(t: torch.Tensor, *streams) -> torch.Tensor:
     return t
 
 
-def _output(shape, dtype, device, stream) -> torch.Tensor:
+def _output(dtype, device, stream, *shape) -> torch.Tensor:
     """A tensor that a call writes on `stream` and returns. What reads it is taken to run there or on the current stream; once it is
     dropped, its memory is not handed out again before both have passed that point."""
-    t = _empty(shape, dtype, device, stream)
-    return t if stream is None else _record(t, None)
+    if stream is None:
+        return torch.empty(*shape, dtype=dtype, device=device)
+    return _record(_empty(dtype, device, stream, *shape), None)
 
 
 def _scratch(nbytes: int, device, stream, *others) -> torch.Tensor:
     """A temporary the binding allocates itself and drops when the call returns, first written on `stream`. The block belongs to
     that stream, and is marked as in use on the other streams of the call: it is handed out again only behind the call's kernels,
     and holds nothing that others before them still use."""
-    return _record(_empty(max(1, int(nbytes)), torch.uint8, device, stream), *others)
+    return _record(_empty(torch.uint8, device, stream, max(1, int(nbytes))), *others)
 
 
 def _host(a, dtype) -> np.ndarray:
@@ -293,9 +294,9 @@ def ld_compress_topk(grad: torch.Tensor, residual: torch.Tensor, seg_off, seg_k,
     _same_device(grad, residual, out_idx, out_val, workspace)
     K = int(seg_k.astype(np.int64).sum())
     if out_idx is None:
-        out_idx = _output(K, torch.int32, grad.device, stream)
+        out_idx = _output(torch.int32, grad.device, stream, K)
     if out_val is None:
-        out_val = _output(K, torch.float32, grad.device, stream)
+        out_val = _output(torch.float32, grad.device, stream, K)
     if out_idx.numel() < K or out_val.numel() < K:
         raise ValueError("output buffers smaller than sum(seg_k)")
     if workspace is None:
@@ -317,8 +318,8 @@ def ld_compress_topk_paths(workspace: torch.Tensor, seg_off, stream=None) -> Tup
     ld_compress_topk call that used `workspace` took for each segment (see lowdiff.h)."""
     seg_off = _host(seg_off, np.int64)
     n_seg = int(seg_off.shape[0]) - 1
-    paths = _output(max(n_seg, 1), torch.int32, workspace.device, stream)
-    over = _output(max(n_seg, 1), torch.int32, workspace.device, stream)
+    paths = _output(torch.int32, workspace.device, stream, max(n_seg, 1))
+    over = _output(torch.int32, workspace.device, stream, max(n_seg, 1))
     st = load().ld_compress_topk_paths(_dev(workspace, torch.uint8, "workspace"), workspace.numel(), n_seg,
                                        _hp(seg_off), _dev(paths, torch.int32, "paths"),
                                        _dev(over, torch.int32, "overflowed_tiles"), _stream(stream))
@@ -473,7 +474,7 @@ def ld_check_diff(idx: torch.Tensor, val: Optional[torch.Tensor], n: int,
     if val is not None and val.numel() != idx.numel():
         raise ValueError("idx and val differ in length")
     if counts is None:
-        counts = _output(3, torch.int64, idx.device, stream)
+        counts = _output(torch.int64, idx.device, stream, 3)
     if counts.numel() < 3:
         raise ValueError("counts needs 3 elements")
     st = load().ld_check_diff(_dev(idx, torch.int32, "idx"), _dev(val, torch.float32, "val"),
@@ -532,11 +533,11 @@ def ld_combine_sparse(idx: Sequence[torch.Tensor], val: Sequence[torch.Tensor], 
     dev = idx[0].device if N else torch.device("cuda", torch.cuda.current_device())
     total = int(K.sum())
     if out_idx is None:
-        out_idx = _output(total, torch.int32, dev, stream)
+        out_idx = _output(torch.int32, dev, stream, total)
     if out_val is None:
-        out_val = _output(total, torch.float32, dev, stream)
+        out_val = _output(torch.float32, dev, stream, total)
     if out_count is None:
-        out_count = _output(1, torch.int64, dev, stream)
+        out_count = _output(torch.int64, dev, stream, 1)
     cap = min(out_idx.numel(), out_val.numel())
     _one_device(out_idx, (out_val, out_count, workspace), gi, gv)
     ip, vp = gi.checked("idx"), gv.checked("val")
@@ -591,9 +592,9 @@ def ld_grad_norm(grads: Sequence[torch.Tensor], sumsq: Optional[torch.Tensor] = 
     got = _lists(grads, None)
     dev = grads[0].device if got else sumsq.device if sumsq is not None else torch.device("cuda", torch.cuda.current_device())
     if sumsq is None:
-        sumsq = _output(1, torch.float64, dev, stream)
+        sumsq = _output(torch.float64, dev, stream, 1)
     if norm is None:
-        norm = _output(1, torch.float32, dev, stream)
+        norm = _output(torch.float32, dev, stream, 1)
     _one_device(sumsq, (norm, workspace), *(got[:1] if got else ()))
     gp, sizes, gt = (got[0].checked("grads"), got[0].sizes, got[2]) if got else (None, None, 0)
     if sumsq.numel() < 1 or norm.numel() < 1:
@@ -634,7 +635,7 @@ def ld_clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, outs: Opti
     got = _lists(grads, outs)
     dev = grads[0].device if got else norm.device if norm is not None else torch.device("cuda", torch.cuda.current_device())
     if norm is None:
-        norm = _output(1, torch.float32, dev, stream)
+        norm = _output(torch.float32, dev, stream, 1)
     _one_device(norm, (workspace,), *(got[:2] if got else ()))
     gp, op, sizes, gt, ot = (got[0].checked("grads"), got[1].checked("outs"), got[0].sizes, got[2], got[3]) if got else (None, None, None, 0, 0)
     if norm.numel() < 1:
@@ -695,7 +696,7 @@ def ld_embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, 
         _ids(positions, "positions")
         at = positions.data_ptr()
     if out is None:
-        out = _output((*ids.shape, d), out_dtype or table.dtype, table.device, stream)
+        out = _output(out_dtype or table.dtype, table.device, stream, *ids.shape, d)
     elif out.numel() != T * d or out.shape[-1] != d or (out_dtype is not None and out.dtype != out_dtype):
         raise ValueError("out differs in shape or type from what the lookup gives")
     op, _, os_ = _rows(out, "out", None, written=True)

@@ -12,14 +12,14 @@ DEV = "cuda:0"
 @pytest.fixture
 def blocks(monkeypatch):
     """First and last byte of every tensor that the binding allocates."""
-    seen, real = [], ld._empty
+    seen, real = [], torch.empty
 
-    def spy(*args):
-        t = real(*args)
+    def spy(*args, **kw):
+        t = real(*args, **kw)
         seen.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
         return t
 
-    monkeypatch.setattr(ld, "_empty", spy)
+    monkeypatch.setattr(torch, "empty", spy)
     return seen
 
 

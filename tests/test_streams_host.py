@@ -66,12 +66,12 @@ def test_a_temporary_of_two_streams(streams):
 def test_an_output_belongs_to_the_stream_that_writes_it_and_may_be_read_on_the_current_one(streams):
     main, side, third = streams
     for stream in (None, main):
-        t = ld._output(3, torch.float32, "cuda:0", stream)
+        t = ld._output(torch.float32, "cuda:0", stream, 3)
         assert t.owner is main and t.used_on == []
-    t = ld._output((2, 3), torch.float32, "cuda:0", side)
+    t = ld._output(torch.float32, "cuda:0", side, 2, 3)
     assert t.owner is side and t.used_on == [main]
 
 
 def test_host_memory_has_no_stream():
     assert ld._scratch(100, "cpu", Stream(16)).numel() == 100
-    assert ld._output(3, torch.float32, torch.device("cpu"), Stream(16)).shape == (3,)
+    assert ld._output(torch.float32, torch.device("cpu"), Stream(16), 3).shape == (3,)
