@@ -224,11 +224,16 @@ def _one_device(first: torch.Tensor, others: Sequence, *tables: _Table) -> None:
     _same_device(first, *others, *(t for b in tables for t in b.tensors))
 
 
+def _allocates_for(stream, device) -> bool:
+    """Whether memory that torch's allocator gives now is that of `stream` (None: the current one), or no stream's."""
+    return stream is None or torch.device(device).type != "cuda" or \
+        (_current_raw_stream is not None and _current_raw_stream(stream.device_index) == stream.cuda_stream)
+
+
 def _empty(dtype, device, stream, *shape) -> torch.Tensor:
-    """An uninitialised tensor out of the memory that torch's allocator keeps for `stream` (None: the current one). What it keeps for
-    another stream may be a block that was just given back and that kernels of that stream, still to run, use."""
-    if stream is None or torch.device(device).type != "cuda" or \
-            (_current_raw_stream is not None and _current_raw_stream(stream.device_index) == stream.cuda_stream):
+    """An uninitialised tensor out of the memory that torch's allocator keeps for `stream`. What it keeps for another stream may be a
+    block that was just given back and that kernels of that stream, still to run, use."""
+    if _allocates_for(stream, device):
         return torch.empty(*shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(*shape, dtype=dtype, device=device)
@@ -245,7 +250,7 @@ def _record(t: torch.Tensor, *streams) -> torch.Tensor:
 def _output(dtype, device, stream, *shape) -> torch.Tensor:
     """A tensor that a call writes on `stream` and returns. What reads it is taken to run there or on the current stream; once it is
     dropped, its memory is not handed out again before both have passed that point."""
-    if stream is None:
+    if stream is None or _allocates_for(stream, device):
         return torch.empty(*shape, dtype=dtype, device=device)
     return _record(_empty(dtype, device, stream, *shape), None)
 
