@@ -31,7 +31,7 @@ def _short(name: str) -> str:
 
 
 def _ours(name: str) -> bool:
-    return any(tag in name for tag in OURS)
+    return _short(name).split("<")[0].split("::")[-1].startswith(OURS)
 
 
 def trace(db_path: str, everything: bool = False) -> str:
