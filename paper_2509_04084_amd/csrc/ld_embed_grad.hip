@@ -7,7 +7,7 @@
 // feedback and a recovery that replays differentials need it.
 //
 // Bound by memory where there are many tokens or rows to clear (16384 tokens of GPT-2 XL, 375 MB, 81 us; 65536 at Llama's width, 800 MB,
-// 194 us, of which the sum of the rows 157 at 5.2 TB/s), else by what waits on one another: the sort's launches of 4 to 8 us each (16384
+// 191 us, of which the sum of the rows 156 at 5.2 TB/s), else by what waits on one another: the sort's launches of 4 to 11 us each (16384
 // tokens of GPT-2 XL's positions, 59 MB, 27 us), the two or three reads between an id and its row.
 #include <type_traits>
 
