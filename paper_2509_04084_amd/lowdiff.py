@@ -686,11 +686,11 @@ def ld_embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, 
     requires_grad: the table's gradient is ld_embed_grad's to make."""
     if (pos_table is None) != (positions is None):
         raise ValueError("pos_table and positions go together")
-    d, T = table.shape[-1], ids.numel()
+    d, T = table.shape[-1] if table.shape else -1, ids.numel()
     if pos_table is not None:
         if positions.numel() != T or positions.dtype != ids.dtype:
             raise ValueError("positions must be as many as ids, and of their type")
-        if pos_table.shape[-1] != d or pos_table.dtype != table.dtype:
+        if pos_table.shape[-1:] != (d,) or pos_table.dtype != table.dtype:
             raise ValueError("table and pos_table differ in width or type")
     _one_device(table, (ids, pos_table, positions, out))
     code, it = _elem(table, "table"), _ids(ids, "ids")
@@ -702,7 +702,7 @@ def ld_embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, 
         at = positions.data_ptr()
     if out is None:
         out = _output(out_dtype or table.dtype, table.device, stream, *ids.shape, d)
-    elif out.numel() != T * d or out.shape[-1] != d or (out_dtype is not None and out.dtype != out_dtype):
+    elif out.numel() != T * d or out.shape[-1:] != (d,) or (out_dtype is not None and out.dtype != out_dtype):
         raise ValueError("out differs in shape or type from what the lookup gives")
     op, _, os_ = _rows(out, "out", None, written=True)
     st = load().ld_embed_lookup(tp, V, ts, pp, P, ps, code, ids.data_ptr(), at, it, T, d, scale, op, os_, _elem(out, "out"),
@@ -721,8 +721,8 @@ def ld_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, sca
     row stride): written to `grad` [V, d], or with `accumulate` added to it. Deterministic. A workspace that is not given is
     allocated for the call: ld_embed_grad_workspace bytes, for a small batch about as many as its `dout` has in 16 bits."""
     lib = load()
-    T, d = ids.numel(), grad.shape[-1]
-    if dout.shape[-1] != d or dout.numel() != T * d:
+    T, d = ids.numel(), grad.shape[-1] if grad.shape else -1
+    if dout.shape[-1:] != (d,) or dout.numel() != T * d:
         raise ValueError("dout must have a row of grad's width for every id")
     _one_device(grad, (dout, ids, workspace))
     it, dt, gt = _ids(ids, "ids"), _elem(dout, "dout"), _elem(grad, "grad")
