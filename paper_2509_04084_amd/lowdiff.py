@@ -686,12 +686,15 @@ def ld_embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, 
     requires_grad: the table's gradient is ld_embed_grad's to make."""
     if (pos_table is None) != (positions is None):
         raise ValueError("pos_table and positions go together")
-    d, T = table.shape[-1] if table.shape else -1, ids.numel()
-    if pos_table is not None:
-        if positions.numel() != T or positions.dtype != ids.dtype:
-            raise ValueError("positions must be as many as ids, and of their type")
-        if pos_table.shape[-1:] != (d,) or pos_table.dtype != table.dtype:
-            raise ValueError("table and pos_table differ in width or type")
+    try:
+        d, T = table.shape[-1], ids.numel()
+        if pos_table is not None:
+            if positions.numel() != T or positions.dtype != ids.dtype:
+                raise ValueError("positions must be as many as ids, and of their type")
+            if pos_table.shape[-1] != d or pos_table.dtype != table.dtype:
+                raise ValueError("table and pos_table differ in width or type")
+    except IndexError:
+        raise TypeError("table, pos_table: expected a 2-D tensor on the GPU") from None
     _one_device(table, (ids, pos_table, positions, out))
     code, it = _elem(table, "table"), _ids(ids, "ids")
     tp, V, ts = _rows(table, "table")
@@ -721,9 +724,12 @@ def ld_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, sca
     row stride): written to `grad` [V, d], or with `accumulate` added to it. Deterministic. A workspace that is not given is
     allocated for the call: ld_embed_grad_workspace bytes, for a small batch about as many as its `dout` has in 16 bits."""
     lib = load()
-    T, d = ids.numel(), grad.shape[-1] if grad.shape else -1
-    if dout.shape[-1:] != (d,) or dout.numel() != T * d:
-        raise ValueError("dout must have a row of grad's width for every id")
+    try:
+        T, d = ids.numel(), grad.shape[-1]
+        if dout.shape[-1] != d or dout.numel() != T * d:
+            raise ValueError("dout must have a row of grad's width for every id")
+    except IndexError:
+        raise TypeError("dout, grad: expected rows") from None
     _one_device(grad, (dout, ids, workspace))
     it, dt, gt = _ids(ids, "ids"), _elem(dout, "dout"), _elem(grad, "grad")
     dp, _, ds = _rows(dout, "dout", None)
