@@ -206,9 +206,9 @@ def prepare(case, seed):
         stats = torch.empty(case["T"], 2, device=DEV)
         entropy = torch.empty(case["T"], device=DEV) if case["entropy"] else None
         for t0, t1 in _row_chunks(case["T"], case["V"]):
-            x = logits[t0:t1].double() * case["scale"]
+            x = logits[t0:t1].double()
             stats[t0:t1, 0] = x.max(dim=1).values
-            x -= stats[t0:t1, :1]
+            x = (x - stats[t0:t1, :1]) * case["scale"]
             stats[t0:t1, 1] = x.exp().sum(dim=1).log()
             if case["entropy"]:
                 x -= stats[t0:t1, 1:].double()
@@ -228,9 +228,9 @@ def prepare(case, seed):
 def _plain_score(state):
     logits, ids, top = state["logits"], state["ids"], state["top"]
     V = logits.shape[1]
-    x = logits.float() * state["scale"]
+    x = logits.float()
     high = x.max(dim=1).values
-    x = x - high[:, None]
+    x = (x - high[:, None]) * state["scale"]
     e = torch.exp(x)
     total = e.sum(dim=1)
     log_total = torch.log(total)
@@ -254,7 +254,7 @@ def _plain_score(state):
 def _plain_logit_grad(state):
     logits, ids, stats = state["logits"], state["ids"], state["stats"]
     T, V = logits.shape
-    logp = logits.float() * state["scale"] - stats[:, :1] - stats[:, 1:]
+    logp = (logits.float() - stats[:, :1]) * state["scale"] - stats[:, 1:]
     p = torch.exp(logp)
     inside = (ids >= 0) & (ids < V)
     g = torch.where(inside, state["d_logprob"], 0.0)
@@ -346,10 +346,11 @@ def exact(case, seed):
         if case["top"]:
             out.update(top_ids=None, top_logprob=new(T, case["top"]))
         for t0, t1 in _row_chunks(T, V):
-            x, y = logits[t0:t1].double() * scale, ids[t0:t1]
+            x, y = logits[t0:t1].double(), ids[t0:t1]
             high = x.max(dim=1).values
+            x *= scale
             lse = torch.logsumexp(x, dim=1)
-            out["stats"][t0:t1, 0], out["stats"][t0:t1, 1] = high, lse - high
+            out["stats"][t0:t1, 0], out["stats"][t0:t1, 1] = high, lse - high * scale
             out["logprob"][t0:t1] = torch.where(y >= 0, x.gather(1, y.clamp_min(0)[:, None])[:, 0] - lse, 0.0)
             if case["top"]:
                 out["top_logprob"][t0:t1] = x.topk(case["top"], dim=1).values - lse[:, None]
