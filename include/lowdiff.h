@@ -530,6 +530,59 @@ ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_t dtype,
                         void* workspace, size_t workspace_bytes, ld_stream stream);
 
 /* ------------------------------------------------------------------------
+ * ld_token_logprob - log probabilities of given tokens, entropy, and the most
+ * probable tokens, of T rows of logits over a vocabulary of V:
+ *   M = max_j logits[t][j];  x_j = scale (logits[t][j] - M);  L = log sum_j exp(x_j)
+ *   stats[t]       = (M, L)                       (log sum exp of the scaled logits: scale M + L)
+ *   logprob[t]     = x_ids[t] - L;  0 where ids[t] is outside [0, V) (padding, -1)
+ *   entropy[t]     = L - sum_j exp(x_j - L) x_j
+ *   top_ids[t], top_logprob[t] = the `top` tokens of the largest logits, in that order, the
+ *                    lower index first among equal ones (-0 and +0 are), and x_j - L of each
+ * in 32 bits.  Masked tokens are minus infinity: their probability is 0.  A row in which
+ * nothing is left (all minus infinity) has M = -inf, L = 0, entropy 0 and log probabilities of
+ * -inf.  An infinite logit or a NaN makes a row's L, entropy and log probabilities NaN; a NaN
+ * counts as the largest of all logits among the alternatives.
+ *
+ *   logits     dev [T] rows of V elements of `dtype`, stride >= 0 elements apart
+ *   ids        dev [T] of `id_dtype` (LD_I32 or LD_I64); NULL together with logprob
+ *   scale      1 / temperature, 1e-30 <= scale <= 1e30
+ *   logprob    dev [T] fp32 or NULL;  entropy  dev [T] fp32 or NULL;  stats  dev [T][2] fp32
+ *   top        0 <= top <= LD_MAX_TOP, top <= V (T > 0)
+ *   top_ids    dev [T][top] int32, top_logprob  dev [T][top] fp32; read only where top > 0
+ *   workspace  dev, 256-byte aligned, ld_token_logprob_workspace() bytes (0 where rows are not
+ *              split, as with many of them: then it may be NULL)
+ *   0 <= T <= LD_MAX_TOKENS;  1 <= V <= LD_MAX_VOCAB where T > 0
+ * No output overlaps another or an input.
+ *
+ * ld_token_logprob_grad - its gradient by the logits, from those by the log probabilities (g)
+ * and by the entropies (h):
+ *   p_j = exp(scale (logits[t][j] - M) - L)
+ *   d_logits[t][j] = round(scale (g (delta_j,ids[t] - p_j) - h p_j (log p_j + entropy[t])))
+ * g counts as 0 where ids[t] is outside [0, V); a row in which nothing is left has a gradient of
+ * zeros.  The alternatives have no gradient.
+ *
+ *   stats, entropy  what ld_token_logprob gave for the same logits and scale
+ *   d_logprob  dev [T] fp32, d_logprob_stride >= 0 apart (0: one for all); NULL together with ids
+ *   d_entropy  dev [T] fp32, d_entropy_stride >= 0 apart; NULL together with entropy
+ *   d_logits   dev [T] rows of V elements of `out_dtype`, out_stride >= V apart; the logits
+ *              themselves (in place: of the same type and stride), or overlaps no input
+ * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_WORKSPACE, LD_ERR_HIP.
+ */
+#define LD_MAX_TOP   64
+#define LD_MAX_VOCAB (1 << 24)
+size_t    ld_token_logprob_workspace(int64_t T, int32_t V, int32_t top);
+ld_status ld_token_logprob(const void* logits, int64_t T, int32_t V, int64_t stride, int32_t dtype,
+                           const void* ids, int32_t id_dtype, float scale,
+                           float* logprob, float* entropy, float* stats,
+                           int32_t top, int32_t* top_ids, float* top_logprob,
+                           void* workspace, size_t workspace_bytes, ld_stream stream);
+ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_t stride, int32_t dtype,
+                                const void* ids, int32_t id_dtype, float scale, const float* stats,
+                                const float* d_logprob, int64_t d_logprob_stride,
+                                const float* entropy, const float* d_entropy, int64_t d_entropy_stride,
+                                void* d_logits, int64_t out_stride, int32_t out_dtype, ld_stream stream);
+
+/* ------------------------------------------------------------------------
  * Checkpointing configuration model (Sec. V-C).  Host arithmetic only; nothing is
  * enqueued.  f = full-checkpoint interval in iterations, b = differentials per
  * batched checkpoint, 1 <= b <= f.

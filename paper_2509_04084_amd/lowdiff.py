@@ -11,7 +11,7 @@ import ctypes
 import importlib
 import math
 import os
-from typing import List, Optional, Sequence, Tuple
+from typing import List, NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -144,6 +144,12 @@ def load() -> ctypes.CDLL:
     lib.ld_embed_grad_workspace.restype = sz
     lib.ld_embed_grad.argtypes = [vp, i64, i32, vp, i32, i64, i32, f32, vp, i64, i64, i32, i32, vp, sz, vp]
     lib.ld_embed_grad.restype = i32
+    lib.ld_token_logprob_workspace.argtypes = [i64, i32, i32]
+    lib.ld_token_logprob_workspace.restype = sz
+    lib.ld_token_logprob.argtypes = [vp, i64, i32, i64, i32, vp, i32, f32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.ld_token_logprob.restype = i32
+    lib.ld_token_logprob_grad.argtypes = [vp, i64, i32, i64, i32, vp, i32, f32, vp, vp, i64, vp, vp, i64, vp, i64, i32, vp]
+    lib.ld_token_logprob_grad.restype = i32
     dbl = ctypes.c_double
     lib.ld_config_wasted_time.argtypes = [vp, dbl, dbl, dbl, dbl]
     lib.ld_config_wasted_time.restype = dbl
@@ -739,6 +745,115 @@ def ld_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, sca
     st = lib.ld_embed_grad(dp, ds, dt, ids.data_ptr(), it, T, d, scale, gp, V, gs, gt, int(accumulate),
                            _dev(workspace, torch.uint8, "workspace"), workspace.numel() if workspace is not None else 0, _stream(stream))
     _check("ld_embed_grad", st)
+
+
+class TokenLogprob(NamedTuple):
+    """What ld_token_logprob gives; None where it was not asked for."""
+    logprob: Optional[torch.Tensor]      # float32, of the ids' shape
+    entropy: Optional[torch.Tensor]      # float32, the same
+    stats: torch.Tensor                  # float32 [..., 2]: the largest logit M, and log sum exp(scale (logit - M))
+    top_ids: Optional[torch.Tensor]      # int32 [..., top]
+    top_logprob: Optional[torch.Tensor]  # float32 [..., top]
+
+
+def _on_device_of(stream, t: torch.Tensor) -> None:
+    """A call runs on the device of its stream: the given one's, or the current device."""
+    at = torch.cuda.current_device() if stream is None else stream.device_index
+    if t.get_device() != at:
+        raise ValueError(f"tensors lie on {t.device}, the call's stream belongs to cuda:{at}")
+
+
+def _vocabulary_rows(logits: torch.Tensor, ids: Optional[torch.Tensor]) -> Tuple[Tuple[int, ...], int, int]:
+    """(shape of the rows, their number, vocabulary)."""
+    if logits.dim() < 1:
+        raise TypeError("logits: expected rows over a vocabulary")
+    rows = tuple(logits.shape[:-1])
+    if ids is not None and tuple(ids.shape) != rows:
+        raise ValueError("ids must name one token for every row of logits")
+    return rows, math.prod(rows), logits.shape[-1]
+
+
+def ld_token_logprob_workspace(T: int, V: int, top: int = 0) -> int:
+    return int(load().ld_token_logprob_workspace(int(T), int(V), int(top)))
+
+
+def ld_token_logprob(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, scale: float = 1.0, entropy: bool = False, top: int = 0,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> TokenLogprob:
+    """Log probabilities of the tokens `ids` under softmax(scale * logits) (0 where an id names no token, as -1 for padding), the
+    rows' entropies, and their `top` most probable tokens (ties: the lower id first) with log probabilities. logits: [..., V], or
+    [T, V] with any row stride; masked tokens are -inf. A row that is masked entirely has entropy 0 and log probabilities of -inf.
+    Autograd records nothing: the gradient is ld_token_logprob_grad's, which takes the stats (and entropy) given here."""
+    lib = load()
+    rows, T, V = _vocabulary_rows(logits, ids)
+    _one_device(logits, (ids, workspace))
+    code, it = _elem(logits, "logits"), _ids(ids, "ids") if ids is not None else 0
+    lp, _, stride = _rows(logits, "logits", None)
+    _on_device_of(stream, logits)
+    if not 0 <= top <= max(V, 0):
+        raise ValueError("top: more alternatives than tokens")
+    dev = logits.device
+    logprob = _output(torch.float32, dev, stream, rows) if ids is not None else None
+    ent = _output(torch.float32, dev, stream, rows) if entropy else None
+    stats = _output(torch.float32, dev, stream, *rows, 2)
+    top_ids = _output(torch.int32, dev, stream, *rows, top) if top else None
+    top_logprob = _output(torch.float32, dev, stream, *rows, top) if top else None
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    if workspace is None and (need := lib.ld_token_logprob_workspace(T, V, top)) > 0:
+        workspace = _scratch(need, dev, stream)
+    st = lib.ld_token_logprob(lp, T, V, stride, code, at(ids), it, scale, at(logprob), at(ent), stats.data_ptr(), top, at(top_ids),
+                              at(top_logprob), _dev(workspace, torch.uint8, "workspace"), workspace.numel() if workspace is not None else 0,
+                              _stream(stream))
+    _check("ld_token_logprob", st)
+    return TokenLogprob(logprob, ent, stats, top_ids, top_logprob)
+
+
+def _per_row(t: torch.Tensor, rows: Tuple[int, ...], name: str) -> Tuple[int, int]:
+    """Address and stride of a float32 for every row: contiguous, [T] with any stride, or one for all (expanded)."""
+    if t.dtype != torch.float32 or not t.is_cuda:
+        raise TypeError(f"{name}: expected a float32 tensor on the GPU")
+    if tuple(t.shape) != rows:
+        raise ValueError(f"{name}: expected one value for every row of logits")
+    if t.is_contiguous():
+        return t.data_ptr(), 1
+    if not any(t.stride()):
+        return t.data_ptr(), 0
+    if t.dim() != 1:
+        raise TypeError(f"{name}: expected a contiguous tensor, a strided one of one dimension, or one value expanded")
+    return t.data_ptr(), t.stride(0)
+
+
+def ld_token_logprob_grad(logits: torch.Tensor, stats: torch.Tensor, ids: Optional[torch.Tensor] = None,
+                          d_logprob: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                          d_entropy: Optional[torch.Tensor] = None, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                          out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """The gradient of ld_token_logprob by its logits, from that of its log probabilities (with the ids) and that of its
+    entropies (with them): in `out`, which may be the logits themselves, or a new tensor of the logits' shape and type `out_dtype`
+    (theirs unless given). `stats` and `entropy` are what the call gave for the same logits and scale."""
+    rows, T, V = _vocabulary_rows(logits, ids)
+    if (ids is None) != (d_logprob is None):
+        raise ValueError("ids and d_logprob go together")
+    if (entropy is None) != (d_entropy is None):
+        raise ValueError("entropy and d_entropy go together")
+    if tuple(stats.shape) != rows + (2,):
+        raise ValueError("stats must have two values for every row of logits")
+    if entropy is not None and tuple(entropy.shape) != rows:
+        raise ValueError("entropy must have one value for every row of logits")
+    _one_device(logits, (stats, ids, d_logprob, entropy, d_entropy, out))
+    code, it = _elem(logits, "logits"), _ids(ids, "ids") if ids is not None else 0
+    lp, _, stride = _rows(logits, "logits", None)
+    _on_device_of(stream, logits)
+    gp, gs = _per_row(d_logprob, rows, "d_logprob") if d_logprob is not None else (None, 0)
+    hp, hs = _per_row(d_entropy, rows, "d_entropy") if d_entropy is not None else (None, 0)
+    if out is None:
+        out = _output(out_dtype or logits.dtype, logits.device, stream, *logits.shape)
+    elif out.shape != logits.shape or (out_dtype is not None and out.dtype != out_dtype):
+        raise ValueError("out differs in shape or type from what the gradient has")
+    op, _, os_ = _rows(out, "out", None, written=True)
+    st = load().ld_token_logprob_grad(lp, T, V, stride, code, None if ids is None else ids.data_ptr(), it, scale,
+                                      _dev(stats, torch.float32, "stats"), gp, gs, _dev(entropy, torch.float32, "entropy"), hp, hs, op, os_,
+                                      _elem(out, "out"), _stream(stream))
+    _check("ld_token_logprob_grad", st)
+    return out
 
 
 class ConfigParams(ctypes.Structure):
