@@ -583,6 +583,59 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
                                 void* d_logits, int64_t out_stride, int32_t out_dtype, ld_stream stream);
 
 /* ------------------------------------------------------------------------
+ * ld_orthogonalize - replaces each of a list of matrices by one with (nearly) the same singular
+ * vectors and singular values near 1, by Newton-Schulz steps:
+ *   X = U / (|U|_F + eps);  `steps` times  X <- (a I + b A + c A^2) X,  A = X X^T
+ * (the steps run on the smaller side: for U with more rows than columns, on its transposed, which
+ * is the same map).  Everything is as precise as products in 32 bits are, and rounded once to
+ * out_dtype; U's squares are summed in 64 bits.  A matrix of zeros stays zeros.  An infinity or a
+ * NaN anywhere in a matrix makes all of it NaN; other matrices of the call are not touched by it.
+ * What a matrix becomes depends on nothing but itself: not on the others of the call.
+ *
+ *   src, dst   host arrays of n_mats dev pointers: [rows][cols] elements of `dtype` and of
+ *              `out_dtype`, rows src_stride >= 0 and dst_stride >= cols elements apart
+ *              (NULL: contiguous).  A dst is its own src (in place: of the same type and stride)
+ *              or overlaps none of the call
+ *   rows, cols host [n_mats] int64, each side <= LD_MAX_SIDE; matrices without elements are
+ *              passed over
+ *   coeff      host [steps][3] of a, b, c; NULL: 3.4445, -4.7750, 2.0315 in every step.
+ *              LD_ERR_RANGE where they let singular values of up to 1 grow beyond 8, or grow them
+ *              by a factor of more than 64 in a step
+ *   steps      1 <= steps <= 16;  eps >= 0
+ *   workspace  dev, 256-byte aligned, ld_orthogonalize_workspace() bytes: about
+ *              (12 n + 20 m) m a matrix of sides m <= n, for as many at a time as 2 GiB hold
+ *
+ * ld_merge_dense_muon - replays W dense gradients of a list of weight matrices as steps of the
+ * optimizer that orthogonalises its updates; W = 1 is a training step.  In order t = 0 .. W-1:
+ *   m <- fl(mu m + g_t)                                       (one fused multiply-add)
+ *   u  = nesterov ? fl(mu m + g_t) : m
+ *   w <- fl(fl(w keep) - rate O(u)),  keep = fl(1 - lr weight_decay),  rate = fl(lr scale[i])
+ * with O the map above, its result in 32 bits.  One call with W gradients gives the same bits as
+ * W calls with one.
+ *
+ *   w, m       host arrays of n_mats dev pointers, fp32 [rows][cols] contiguous, in/out; no two
+ *              overlap
+ *   grad       host array of W n_mats dev pointers, gradient t of matrix i at [t n_mats + i],
+ *              [rows][cols] contiguous elements of `dtype`
+ *   scale      host [n_mats] fp32, or NULL: sqrt(max(1, rows / cols))
+ *   0 <= W <= LD_MAX_WINDOW
+ *   workspace  dev, 256-byte aligned, ld_merge_dense_muon_workspace() bytes
+ * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_WORKSPACE, LD_ERR_HIP.
+ */
+#define LD_MAX_SIDE 65536
+size_t    ld_orthogonalize_workspace(const int64_t* rows, const int64_t* cols, int32_t n_mats);
+ld_status ld_orthogonalize(const void* const* src, const int64_t* src_stride, void* const* dst, const int64_t* dst_stride,
+                           const int64_t* rows, const int64_t* cols, int32_t n_mats, int32_t dtype, int32_t out_dtype,
+                           int32_t steps, const float* coeff /* may be NULL */, float eps,
+                           void* workspace, size_t workspace_bytes, ld_stream stream);
+size_t    ld_merge_dense_muon_workspace(const int64_t* rows, const int64_t* cols, int32_t n_mats, int32_t W);
+ld_status ld_merge_dense_muon(float* const* w, float* const* m, const void* const* grad,
+                              const int64_t* rows, const int64_t* cols, int32_t n_mats, int32_t W, int32_t dtype,
+                              float lr, float mu, int32_t nesterov, float weight_decay, const float* scale /* may be NULL */,
+                              int32_t steps, const float* coeff /* may be NULL */, float eps,
+                              void* workspace, size_t workspace_bytes, ld_stream stream);
+
+/* ------------------------------------------------------------------------
  * Checkpointing configuration model (Sec. V-C).  Host arithmetic only; nothing is
  * enqueued.  f = full-checkpoint interval in iterations, b = differentials per
  * batched checkpoint, 1 <= b <= f.

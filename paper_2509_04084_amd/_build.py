@@ -9,7 +9,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liblowdiff.so")
 SOURCES = ["ld_api.hip", "ld_config.hip", "ld_merge_sparse.hip", "ld_recover.hip", "ld_check_diff.hip", "ld_merge_sparse_adam.hip", "ld_combine_sparse.hip", "ld_dense.hip", "ld_grad_norm.hip", "ld_embed.hip",
-           "ld_embed_grad.hip", "ld_logprob.hip", "ld_compress.hip"]
+           "ld_embed_grad.hip", "ld_logprob.hip", "ld_muon.hip", "ld_compress.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
@@ -43,7 +43,7 @@ def build_library(force: bool = True, verbose: bool = False) -> str:
     """Compiles every HIP source into liblowdiff.so; returns its path."""
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
     deps = srcs + [os.path.join(CSRC, "ld_common.h"), os.path.join(CSRC, "ld_sparse_common.h"), os.path.join(CSRC, "ld_thin.h"),
-                   os.path.join(CSRC, "ld_map.h"), os.path.join(CSRC, "ld_combine_shape.h"), os.path.join(CSRC, "ld_elem.h"), os.path.join(CSRC, "ld_grid.h"),
+                   os.path.join(CSRC, "ld_map.h"), os.path.join(CSRC, "ld_combine_shape.h"), os.path.join(CSRC, "ld_elem.h"), os.path.join(CSRC, "ld_grid.h"), os.path.join(CSRC, "ld_muon_shape.h"),
                    os.path.join(ROOT, "include", "lowdiff.h")]
     if not force and os.path.exists(LIB) and all(os.path.getmtime(LIB) >= os.path.getmtime(d) for d in deps):
         return LIB

@@ -1,0 +1,745 @@
+// Orthogonalising updates by Newton-Schulz products, and the replay of dense gradients through the optimizer that does so (Muon).
+//
+//   X_0 = U / (|U|_F + eps);  X_{s+1} = (a I + b A + c A^2) X_s,  A = X_s X_s^T      (of U or its transposed, rows <= columns)
+//   replay: m = mu m + g;  U = g + mu m (Nesterov) or m;  w = (1 - lr wd) w - lr s X_S
+//
+// Products are what bounds it. Results are compared, and replayed, as 32-bit values, so operands are kept as pairs of halves, h + l with
+// 22 bits, and a product is three MFMA products: hh + hl + lh, summed in 32 bits. Values are scaled by powers of two that the
+// coefficients bound. A run of steps works on the Gram matrix alone: with P = a I + b A + c A^2, A' = P A P and Q' = P Q, all of m by
+// m, symmetric and commuting, so that half of each is computed and mirrored; X is read for its Gram matrix and multiplied by Q once a
+// run (ld_muon_shape.h says when a run ends, and why). Five steps on m x n cost 6 m^2 n + 14 m^3 products' operations where n >= 2.5 m,
+// else 9 m^2 n + 11 m^3, instead of 15 m^2 n + 5 m^3 (symmetric halves there too).
+//
+// In memory a matrix lies as blocks of 32 columns, in each of them row after row: 32 upper halves, 32 lower halves, 128 bytes, whose eight
+// 16-byte pieces are permuted by the row, as shared memory wants them: a tile's block is contiguous, and is copied into shared memory as it is.
+// Every element's sum runs over the columns in order and depends on nothing but its own row and column: any mixture of matrices
+// in a call, and any cut of a window into calls, gives the same bits.
+#include <math.h>
+#include <string.h>
+
+#include <type_traits>
+
+#include "ld_elem.h"
+#include "ld_grid.h"
+#include "ld_muon_shape.h"
+
+namespace {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kThreads = 256;
+constexpr int kMost = 64;                                    // problems of a group
+constexpr int64_t kGroupBytes = static_cast<int64_t>(2) << 30;  // scratch of a group, unless one problem needs more
+constexpr int kSumParts = 256;                               // partial sums of squares of a problem at most
+constexpr int64_t kSumElems = 8192;                          // elements of one, at least
+
+enum Buffer { kX, kXT, kYT, kA, kP, kR, kQ0, kQ1 };
+
+// The matrices of a group: m <= n, `flipped` where U has more rows than columns.
+struct Batch {
+    char* base[kMost];
+    int32_t m[kMost], n[kMost];
+    int32_t flipped[kMost];
+    int32_t first[kMost + 1];  // tiles of a launch before a problem's
+    int32_t count;
+};
+
+__device__ __forceinline__ int64_t padded(int64_t n) { return (n + kMuonPad - 1) / kMuonPad * kMuonPad; }
+__device__ __forceinline__ char* buffer_of(const Batch& b, int32_t i, int32_t which) {
+    const int64_t m = padded(b.m[i]), n = padded(b.n[i]), slack = 3 * kMuonPad * kMuonRowBytes;
+    const int64_t large = m * n * 4 + slack, small = m * m * 4 + slack;
+    return b.base[i] + (which < 3 ? which * large : 3 * large + (which - 3) * small);
+}
+// Where the eight upper halves of row r, columns [8 c, 8 c + 8) lie, in bytes; the lower ones are 64 bytes on, permuted alike.
+__device__ __forceinline__ int64_t piece_at(int64_t rows, int64_t r, int64_t c, int32_t lower) {
+    return ((c >> 2) * rows + r) * kMuonRowBytes + ((((c & 3) | lower << 2) ^ (r & 7)) << 4);
+}
+
+__device__ __forceinline__ void split(const f32x8& x, half8& h, half8& l) {
+    h = __builtin_convertvector(x, half8);
+    l = __builtin_convertvector(x - __builtin_convertvector(h, f32x8), half8);
+}
+__device__ __forceinline__ void store_split(char* to, int64_t rows, int64_t r, int64_t c, const f32x8& x) {
+    half8 h, l;
+    split(x, h, l);
+    *reinterpret_cast<half8*>(to + piece_at(rows, r, c, 0)) = h;
+    *reinterpret_cast<half8*>(to + piece_at(rows, r, c, 1)) = l;
+}
+__device__ __forceinline__ f32x8 load_split(const char* from, int64_t rows, int64_t r, int64_t c) {
+    const half8 h = *reinterpret_cast<const half8*>(from + piece_at(rows, r, c, 0)), l = *reinterpret_cast<const half8*>(from + piece_at(rows, r, c, 1));
+    return __builtin_convertvector(h, f32x8) + __builtin_convertvector(l, f32x8);
+}
+
+// ------------------------------------------------------------------------------------------------------------------- products
+
+// C = left right^T of every problem: rows of `left` by rows of `right`, both over the same columns.
+struct Product {
+    int32_t left, right;   // buffers
+    int32_t out, out_t;    // of C and, where not symmetric, of its transposed
+};
+struct Plan {
+    Product prod[2];       // the second of a launch with twice as many tiles
+    int32_t products;
+    int32_t apply;         // X' = Q X, with `final` where it goes
+    int32_t final;
+    int32_t long_sum;      // the columns are n, not m
+    int32_t poly;          // C is A^2: what is kept is a I + b A + c C
+    float inv;             // 1 / scale of the operands' product
+    float scale[2];        // of what is kept
+    float ca, cb, cc;      // coefficients, cb times 1 / scale of A
+};
+// Where X_S goes.
+struct FinalArgs {
+    void* out[kMost];
+    int64_t stride[kMost];
+};
+
+typedef const void __attribute__((address_space(1))) * global_ptr;
+typedef void __attribute__((address_space(3))) * shared_ptr;
+
+// TILE rows of a block of columns into shared memory, 16 bytes a lane, as they lie.
+template <int TILE>
+__device__ __forceinline__ void fetch(const char* from, char* to) {
+    const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LD_WAVE);
+#pragma unroll
+    for (int i = 0; i < TILE / 32; ++i) {
+        const int32_t at = (wave * (TILE / 32) + i) * 1024;
+        __builtin_amdgcn_global_load_lds((global_ptr)(from + at + ld_lane() * 16), (shared_ptr)(to + at), 16, 0, 0);
+    }
+}
+
+__device__ __forceinline__ half8 fragment(const char* tile, int32_t row, int32_t piece) {
+    return *reinterpret_cast<const half8*>(tile + row * kMuonRowBytes + ((piece ^ (row & 7)) << 4));
+}
+
+// A tile's sums, four waves of a quarter each.
+template <int TILE>
+__device__ __forceinline__ void multiply(const char* left, int64_t left_rows, const char* right, int64_t right_rows, int32_t blocks, char* shared,
+                                         f32x16 (&acc)[TILE / 64][TILE / 64]) {
+    constexpr int N = TILE / 64, kBytes = TILE * static_cast<int>(kMuonRowBytes);
+    const int32_t lane = ld_lane(), wave = threadIdx.x / LD_WAVE, row = (wave >> 1) * (TILE / 2) + (lane & 31), col = (wave & 1) * (TILE / 2) + (lane & 31);
+    const int64_t left_step = left_rows * kMuonRowBytes, right_step = right_rows * kMuonRowBytes;
+    fetch<TILE>(left, shared);
+    fetch<TILE>(right, shared + kBytes);
+    __syncthreads();
+    for (int32_t k = 0; k < blocks; ++k) {
+        char* now = shared + (k & 1) * 2 * kBytes;
+        if (k + 1 < blocks) {
+            char* next = shared + (~k & 1) * 2 * kBytes;
+            fetch<TILE>(left + (k + 1) * left_step, next);
+            fetch<TILE>(right + (k + 1) * right_step, next + kBytes);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            half8 a[N][2], b[N][2];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int l = 0; l < 2; ++l) {
+                    a[i][l] = fragment(now, row + 32 * i, 4 * l + 2 * s + (lane >> 5));
+                    b[i][l] = fragment(now + kBytes, col + 32 * i, 4 * l + 2 * s + (lane >> 5));
+                }
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][1], b[j][0], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][1], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][0], acc[i][j], 0, 0, 0);
+                }
+        }
+        __syncthreads();
+    }
+}
+
+template <int TILE> constexpr int tile_stride() { return TILE + 4; }  // floats from a row to the next of a tile in shared memory
+template <int TILE> constexpr int shared_bytes() {
+    constexpr int operands = 4 * TILE * static_cast<int>(kMuonRowBytes), tile = TILE * tile_stride<TILE>() * 4;
+    return operands > tile ? operands : tile;
+}
+
+// The sums, times `inv`, as rows of 32-bit values in shared memory.
+template <int TILE>
+__device__ __forceinline__ void lay_out(const f32x16 (&acc)[TILE / 64][TILE / 64], float inv, float* tile) {
+    const int32_t lane = ld_lane(), wave = threadIdx.x / LD_WAVE;
+#pragma unroll
+    for (int i = 0; i < TILE / 64; ++i)
+#pragma unroll
+        for (int j = 0; j < TILE / 64; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const int32_t r = (wave >> 1) * (TILE / 2) + 32 * i + (q & 3) + 8 * (q >> 2) + 4 * (lane >> 5);
+                const int32_t c = (wave & 1) * (TILE / 2) + 32 * j + (lane & 31);
+                tile[r * tile_stride<TILE>() + c] = acc[i][j][q] * inv;
+            }
+    __syncthreads();
+}
+
+// Which problem a tile is of, and its number there.
+__device__ __forceinline__ int32_t problem_of(const Batch& b, int32_t& tile) {
+    int32_t lo = 0, hi = b.count - 1;
+    while (lo < hi) {
+        const int32_t mid = (lo + hi + 1) >> 1;
+        if (b.first[mid] <= tile) lo = mid;
+        else hi = mid - 1;
+    }
+    tile -= b.first[lo];
+    return lo;
+}
+
+template <int TILE>
+__global__ __launch_bounds__(kThreads, 2) void k_symmetric(Batch batch, Plan a) {
+    __shared__ __attribute__((aligned(16))) char shared[shared_bytes<TILE>()];
+    int32_t tile = blockIdx.x;
+    const int32_t tiles = batch.first[batch.count], second = tile >= tiles;
+    if (second) tile -= tiles;
+    const int32_t i = problem_of(batch, tile);
+    const Product prod = a.prod[second];
+    const float scale = a.scale[second];
+    // row by row of the lower triangle
+    int32_t tr = static_cast<int32_t>((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
+    while (tr * (tr + 1) / 2 > tile) --tr;
+    while ((tr + 1) * (tr + 2) / 2 <= tile) ++tr;
+    const int32_t tc = tile - tr * (tr + 1) / 2, m = batch.m[i];
+    const int64_t rows = padded(m);
+    f32x16 acc[TILE / 64][TILE / 64] = {};
+    multiply<TILE>(buffer_of(batch, i, prod.left) + tr * TILE * kMuonRowBytes, rows, buffer_of(batch, i, prod.right) + tc * TILE * kMuonRowBytes, rows,
+                   static_cast<int32_t>((a.long_sum ? padded(batch.n[i]) : rows) / kMuonBlock), shared, acc);
+    float* sums = reinterpret_cast<float*>(shared);
+    lay_out<TILE>(acc, a.inv, sums);
+    constexpr int S = tile_stride<TILE>(), kPieces = TILE / 8;
+    char* out = buffer_of(batch, i, prod.out);
+    const char* gram = buffer_of(batch, i, prod.left);
+    const auto keep = [&](f32x8 x, int32_t r, int32_t c) {  // eight columns from c on of row r, of the whole matrix
+        if (a.poly) {
+            x = a.cc * x + a.cb * load_split(gram, rows, r, c >> 3);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (r == c + e && r < m) x[e] += a.ca;
+        }
+        store_split(out, rows, r, c >> 3, x * scale);
+    };
+    for (int32_t p = threadIdx.x; p < TILE * kPieces; p += kThreads) {
+        const int32_t r = p / kPieces, c = p % kPieces * 8;
+        if (tr * TILE + r >= rows || tc * TILE + c >= rows) continue;
+        f32x8 x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = sums[tr == tc && c + e > r ? (c + e) * S + r : r * S + c + e];
+        keep(x, tr * TILE + r, tc * TILE + c);
+    }
+    if (tr == tc) return;
+    for (int32_t p = threadIdx.x; p < TILE * kPieces; p += kThreads) {
+        const int32_t c = p % TILE, r = p / TILE * 8;  // mirrored: row c, columns from r on
+        if (tr * TILE + r >= rows || tc * TILE + c >= rows) continue;
+        f32x8 x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = sums[(r + e) * S + c];
+        keep(x, tc * TILE + c, tr * TILE + r);
+    }
+}
+
+// X' = Q X: kept both ways, or, the last, written where it goes. left: Q (m rows); right: X transposed (n rows).
+template <int TILE, bool FINAL, int OT>
+__global__ __launch_bounds__(kThreads, 2) void k_apply(Batch batch, Plan a, FinalArgs f) {
+    __shared__ __attribute__((aligned(16))) char shared[shared_bytes<TILE>()];
+    int32_t tile = blockIdx.x;
+    const int32_t i = problem_of(batch, tile);
+    const int32_t m = batch.m[i], n = batch.n[i], down = (m + TILE - 1) / TILE;
+    const int32_t tc = tile / down, tr = tile % down;
+    const int64_t rows = padded(m), cols = padded(n);
+    f32x16 acc[TILE / 64][TILE / 64] = {};
+    multiply<TILE>(buffer_of(batch, i, a.prod[0].left) + tr * TILE * kMuonRowBytes, rows, buffer_of(batch, i, a.prod[0].right) + tc * TILE * kMuonRowBytes, cols,
+                   static_cast<int32_t>(rows / kMuonBlock), shared, acc);
+    float* sums = reinterpret_cast<float*>(shared);
+    lay_out<TILE>(acc, a.inv, sums);
+    constexpr int S = tile_stride<TILE>(), kPieces = TILE / 8;
+    typedef typename LdElem<OT>::type elem;
+    elem* final_out = FINAL ? static_cast<elem*>(f.out[i]) : nullptr;
+    const int64_t stride = FINAL ? f.stride[i] : 0;
+    const auto write = [&](const f32x8& x, int32_t r, int32_t c, int32_t width) {
+        elem* to = final_out + r * stride + c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < width) to[e] = static_cast<elem>(x[e]);
+    };
+    if (!FINAL || !batch.flipped[i]) {
+        for (int32_t p = threadIdx.x; p < TILE * kPieces; p += kThreads) {
+            const int32_t r = p / kPieces, c = p % kPieces * 8, ri = tr * TILE + r, ci = tc * TILE + c;
+            f32x8 x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = sums[r * S + c + e];
+            if (FINAL) {
+                if (ri < m) write(x, ri, ci, n);
+            } else if (ri < rows && ci < cols) {
+                store_split(buffer_of(batch, i, a.prod[0].out), rows, ri, ci >> 3, x * a.scale[0]);
+            }
+        }
+    }
+    if (!FINAL || batch.flipped[i]) {
+        for (int32_t p = threadIdx.x; p < TILE * kPieces; p += kThreads) {
+            const int32_t c = p % TILE, r = p / TILE * 8, ri = tr * TILE + r, ci = tc * TILE + c;
+            f32x8 x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = sums[(r + e) * S + c];
+            if (FINAL) {
+                if (ci < n) write(x, ci, ri, m);
+            } else if (ri < rows && ci < cols) {
+                store_split(buffer_of(batch, i, a.prod[0].out_t), cols, ci, ri >> 3, x * a.scale[0]);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- before and after
+
+__device__ __forceinline__ double block_sum(double x, double* sh) {
+    for (int d = LD_WAVE / 2; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    __syncthreads();
+    if (ld_lane() == 0) sh[threadIdx.x / LD_WAVE] = x;
+    __syncthreads();
+    double sum = 0.0;
+    for (int w = 0; w < kThreads / LD_WAVE; ++w) sum += sh[w];
+    return sum;
+}
+
+// Updates to orthogonalise: user rows and columns are those of the update, not of X.
+struct Source {
+    const void* src[kMost];
+    int64_t stride[kMost];
+    double* sums;              // [problem][kSumParts]
+    float eps;
+};
+__device__ __forceinline__ int32_t user_rows(const Batch& b, int32_t i) { return b.flipped[i] ? b.n[i] : b.m[i]; }
+__device__ __forceinline__ int32_t user_cols(const Batch& b, int32_t i) { return b.flipped[i] ? b.m[i] : b.n[i]; }
+// How many partial sums the squares of a matrix have, by its size alone.
+__host__ __device__ __forceinline__ int32_t sum_parts(int64_t elems) {
+    const int64_t parts = (elems + kSumElems - 1) / kSumElems;
+    return static_cast<int32_t>(parts < kSumParts ? parts : kSumParts);
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void k_squares(Batch b, Source s) {
+    __shared__ double sh[kThreads / LD_WAVE];
+    typedef typename LdElem<DT>::type elem;
+    const int32_t i = blockIdx.y, rows = user_rows(b, i), cols = user_cols(b, i);
+    const int64_t elems = static_cast<int64_t>(rows) * cols;
+    const int32_t parts = sum_parts(elems);
+    if (static_cast<int32_t>(blockIdx.x) >= parts) return;
+    const elem* src = static_cast<const elem*>(s.src[i]);
+    const int64_t stride = s.stride[i];
+    double sum = 0.0;
+    for (int64_t e = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; e < elems; e += static_cast<int64_t>(parts) * kThreads) {
+        const double x = static_cast<double>(static_cast<float>(src[e / cols * stride + e % cols]));
+        sum = fma(x, x, sum);
+    }
+    sum = block_sum(sum, sh);
+    if (threadIdx.x == 0) s.sums[i * kSumParts + blockIdx.x] = sum;
+}
+
+// X and its transposed from the update: 64 by 64 elements a workgroup, zeros behind its edges.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void k_lay_out(Batch b, Source s, float scale) {
+    __shared__ float tile[kMuonPad][kMuonPad + 1];
+    __shared__ double sh[kThreads / LD_WAVE];
+    typedef typename LdElem<DT>::type elem;
+    const int32_t i = blockIdx.y, rows = user_rows(b, i), cols = user_cols(b, i);
+    const int32_t across = (cols + kMuonPad - 1) / kMuonPad, r0 = static_cast<int32_t>(blockIdx.x) / across * kMuonPad, c0 = static_cast<int32_t>(blockIdx.x) % across * kMuonPad;
+    if (r0 >= rows) return;
+    const int32_t parts = sum_parts(static_cast<int64_t>(rows) * cols);
+    const double total = block_sum(static_cast<int32_t>(threadIdx.x) < parts ? s.sums[i * kSumParts + threadIdx.x] : 0.0, sh);
+    const double norm = sqrt(total);
+    const double f = norm == 0.0 ? 0.0 : static_cast<double>(scale) / (norm + static_cast<double>(s.eps));
+    const elem* src = static_cast<const elem*>(s.src[i]);
+    const int64_t stride = s.stride[i];
+    for (int32_t e = threadIdx.x; e < kMuonPad * kMuonPad; e += kThreads) {
+        const int32_t r = e / kMuonPad, c = e % kMuonPad;
+        float x = 0.0f;
+        if (r0 + r < rows && c0 + c < cols) x = static_cast<float>(static_cast<double>(static_cast<float>(src[(r0 + r) * stride + c0 + c])) * f);
+        tile[r][c] = x;
+    }
+    __syncthreads();
+    char* straight = buffer_of(b, i, b.flipped[i] ? kXT : kX);
+    char* turned = buffer_of(b, i, b.flipped[i] ? kX : kXT);
+    const int64_t all_rows = padded(rows), all_cols = padded(cols);
+    for (int32_t p = threadIdx.x; p < kMuonPad * kMuonPad / 8; p += kThreads) {
+        const int32_t r = p / 8, c = p % 8 * 8;
+        f32x8 x, y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = tile[r][c + e], y[e] = tile[c + e][r];
+        store_split(straight, all_rows, r0 + r, (c0 + c) >> 3, x);
+        store_split(turned, all_cols, c0 + r, (r0 + c) >> 3, y);
+    }
+}
+
+// Momentum of a window's steps, one after another, and every step's update and the sum of its squares.
+struct MomentumArgs {
+    float* momentum[kMost];
+    const void* grad[kMost];   // of every problem
+    int32_t problem[kMost];    // a matrix's first
+    int32_t steps[kMost];      // and how many it has
+    double* sums;
+    float mu;
+    int32_t nesterov;
+};
+template <int DT>
+__global__ __launch_bounds__(kThreads) void k_momentum(Batch b, MomentumArgs a) {
+    __shared__ double sh[kThreads / LD_WAVE];
+    typedef typename LdElem<DT>::type elem;
+    const int32_t p0 = a.problem[blockIdx.y], steps = a.steps[blockIdx.y];
+    const int64_t elems = static_cast<int64_t>(b.m[p0]) * b.n[p0];
+    const int32_t parts = sum_parts(elems);
+    if (static_cast<int32_t>(blockIdx.x) >= parts) return;
+    float* momentum = a.momentum[blockIdx.y];
+    const int64_t from = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x, step = static_cast<int64_t>(parts) * kThreads;
+    for (int32_t t = 0; t < steps; ++t) {
+        const elem* grad = static_cast<const elem*>(a.grad[p0 + t]);
+        float* update = reinterpret_cast<float*>(buffer_of(b, p0 + t, kYT));
+        double sum = 0.0;
+        for (int64_t e = from; e < elems; e += step) {
+            const float g = static_cast<float>(grad[e]), m = __fmaf_rn(a.mu, momentum[e], g), u = a.nesterov ? __fmaf_rn(a.mu, m, g) : m;
+            momentum[e] = m;
+            update[e] = u;
+            sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
+        }
+        sum = block_sum(sum, sh);
+        if (threadIdx.x == 0) a.sums[(p0 + t) * kSumParts + blockIdx.x] = sum;
+    }
+}
+
+struct UpdateArgs {
+    float* w[kMost];
+    int32_t problem[kMost], steps[kMost];
+    float rate[kMost];         // lr times the matrix's scale
+    float keep;                // 1 - lr wd
+};
+__global__ __launch_bounds__(kThreads) void k_update(Batch b, UpdateArgs a) {
+    const int32_t p0 = a.problem[blockIdx.y], steps = a.steps[blockIdx.y];
+    const int64_t elems = static_cast<int64_t>(b.m[p0]) * b.n[p0];
+    float* w = a.w[blockIdx.y];
+    for (int64_t e = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; e < elems; e += static_cast<int64_t>(gridDim.x) * kThreads) {
+        float x = w[e];
+        for (int32_t t = 0; t < steps; ++t) x = __fmaf_rn(-a.rate[blockIdx.y], reinterpret_cast<const float*>(buffer_of(b, p0 + t, kX))[e], x * a.keep);
+        w[e] = x;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------------------ host
+
+struct Polynomial {
+    int32_t steps;
+    float coeff[3 * kMuonMaxSteps];
+    LdMuonBounds bounds;
+};
+
+// What a kind of matrices goes through, launch by launch.
+struct Program {
+    int32_t count;
+    Plan plan[6 * kMuonMaxSteps];
+};
+
+bool polynomial(Polynomial& p, int32_t steps, const float* coeff) {
+    if (steps < 0 || steps > kMuonMaxSteps) return false;
+    p.steps = steps;
+    for (int32_t s = 0; s < steps; ++s) {
+        const float usual[3] = {3.4445f, -4.7750f, 2.0315f};
+        for (int32_t k = 0; k < 3; ++k) p.coeff[3 * s + k] = coeff ? coeff[3 * s + k] : usual[k];
+    }
+    return ld_muon_bounds(p.bounds, steps, p.coeff);
+}
+
+bool known_sides(int64_t rows, int64_t cols) { return rows >= 0 && cols >= 0 && rows <= LD_MAX_SIDE && cols <= LD_MAX_SIDE; }
+
+// Bytes that a group's partial sums take before its scratch.
+constexpr int64_t kSumBytes = static_cast<int64_t>(kMost) * kSumParts * sizeof(double);
+
+int64_t scratch_of(int64_t rows, int64_t cols) {
+    const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    return (ld_muon_scratch(static_cast<int32_t>(m), static_cast<int32_t>(n)) + 255) / 256 * 256;
+}
+
+// Appends a problem; whether it still has room. The first always has.
+bool append(Batch& b, int64_t& used, char* scratch, int64_t rows, int64_t cols) {
+    const int64_t need = scratch_of(rows, cols);
+    if (b.count == kMost || (b.count > 0 && used + need > kGroupBytes)) return false;
+    const int32_t i = b.count++;
+    b.base[i] = scratch + used;
+    b.flipped[i] = rows > cols;
+    b.m[i] = static_cast<int32_t>(rows > cols ? cols : rows);
+    b.n[i] = static_cast<int32_t>(rows > cols ? rows : cols);
+    used += need;
+    return true;
+}
+
+// Bytes of the largest group of `repeats` problems of every matrix in turn; a group begins anew wherever one is full.
+size_t workspace_of(const int64_t* rows, const int64_t* cols, int32_t n, int64_t repeats) {
+    int64_t most = 0, used = 0, count = 0;  // of the group that is filled
+    for (int32_t i = 0; i < n; ++i) {
+        if (rows[i] == 0 || cols[i] == 0) continue;
+        const int64_t need = scratch_of(rows[i], cols[i]);
+        const auto room = [&]() {
+            const int64_t fit = (kGroupBytes - used) / need;
+            return count == 0 && fit < 1 ? 1 : fit < kMost - count ? fit : kMost - count;
+        };
+        int64_t left = repeats;
+        while (left > 0) {
+            int64_t fit = room();
+            if (fit < 1) used = count = 0, fit = room();
+            if (left > fit && count == 0) {  // whole groups of this matrix alone
+                left -= (left - 1) / fit * fit;
+                if (fit * need > most) most = fit * need;
+            }
+            const int64_t taken = left < fit ? left : fit;
+            used += taken * need, count += taken, left -= taken;
+            if (used > most) most = used;
+        }
+    }
+    return most == 0 ? 0 : static_cast<size_t>(kSumBytes + most);
+}
+
+int32_t tiles_of(int64_t side, int32_t tile) { return static_cast<int32_t>((side + tile - 1) / tile); }
+
+constexpr int32_t kTile = 128;
+
+void program_of(const Polynomial& p, bool wide, Program& out) {
+    const auto scale = [](double bound) { return ld_muon_scale(bound); };
+    const LdMuonBounds& b = p.bounds;
+    int32_t begin[kMuonMaxSteps + 1];
+    const int32_t runs = ld_muon_runs(b, p.steps, wide, begin);
+    int32_t xt = kXT, other = kYT;
+    out.count = 0;
+    for (int32_t run = 0; run < runs; ++run) {
+        const int32_t from = begin[run], to = begin[run + 1];
+        const float sx = scale(b.x[from]);
+        float sa = scale(b.x[from] * b.x[from]), sq = 0.0f;
+        Plan gram = {};
+        gram.prod[0] = {kX, kX, kA, 0};
+        gram.products = 1, gram.long_sum = 1, gram.inv = 1.0f / (sx * sx), gram.scale[0] = sa;
+        out.plan[out.count++] = gram;
+        int32_t q = kP, free_q = kQ0;
+        for (int32_t step = from; step < to; ++step) {
+            const bool first = step == from, last = step + 1 == to;
+            const float sp = scale(b.p[step]), sr = scale(b.r[step]), new_sq = scale(ld_muon_grown(b, from, step));
+            const int32_t poly = first && !last ? kQ1 : kP;  // the first P is the first Q, and is kept
+            Plan a = {};
+            a.prod[0] = {kA, kA, poly, 0};
+            a.products = 1, a.poly = 1, a.inv = 1.0f / (sa * sa), a.scale[0] = sp;
+            a.ca = p.coeff[3 * step], a.cb = p.coeff[3 * step + 1] / sa, a.cc = p.coeff[3 * step + 2];
+            out.plan[out.count++] = a;
+            // P A and P Q at once: their operands' scales differ, which the scale of what is kept takes up
+            Plan next = {};
+            next.inv = 1.0f;
+            if (!last) {
+                next.prod[next.products] = {poly, kA, kR, 0};
+                next.scale[next.products++] = sr / (sp * sa);
+            }
+            if (!first) {
+                next.prod[next.products] = {poly, q, free_q, 0};
+                next.scale[next.products++] = new_sq / (sp * sq);
+            }
+            if (next.products > 0) out.plan[out.count++] = next;
+            if (first) {
+                q = poly, sq = sp;
+            } else {
+                const int32_t was = q;
+                q = free_q, free_q = was, sq = new_sq;
+            }
+            if (last) continue;
+            const float new_sa = scale(b.x[step + 1] * b.x[step + 1]);
+            Plan g = {};
+            g.prod[0] = {poly, kR, kA, 0};
+            g.products = 1, g.inv = 1.0f / (sp * sr), g.scale[0] = new_sa;
+            out.plan[out.count++] = g;
+            sa = new_sa;
+        }
+        Plan a = {};
+        a.prod[0] = {q, xt, kX, other};
+        a.products = 1, a.apply = 1, a.inv = 1.0f / (sq * sx);
+        if (run + 1 == runs) a.final = 1;
+        else a.scale[0] = scale(b.x[to]);
+        out.plan[out.count++] = a;
+        const int32_t was = xt;
+        xt = other, other = was;
+    }
+}
+
+// All steps of a group whose X is laid out. Wide matrices and others go through launches of their own from where their programs differ.
+ld_status run_steps(Batch& b, const Polynomial& p, const FinalArgs& out, int32_t out_type, hipStream_t s) {
+    bool any[2] = {false, false};
+    for (int32_t i = 0; i < b.count; ++i) any[ld_muon_wide(b.m[i], b.n[i])] = true;
+    Program prog[2];
+    for (int32_t w = 0; w < 2; ++w) program_of(p, w == 1, prog[w]);
+    const auto launch = [&](const Plan& a, bool with_wide, bool with_others) {
+        int32_t tiles = 0;
+        for (int32_t i = 0; i < b.count; ++i) {
+            b.first[i] = tiles;
+            if (!(ld_muon_wide(b.m[i], b.n[i]) ? with_wide : with_others)) continue;
+            const int32_t down = tiles_of(b.m[i], kTile), across = tiles_of(b.n[i], kTile);
+            tiles += a.apply ? down * across : down * (down + 1) / 2;
+        }
+        for (int32_t i = b.count; i <= kMost; ++i) b.first[i] = tiles;
+        const dim3 grid(tiles * a.products);
+        if (!a.apply) k_symmetric<kTile><<<grid, dim3(kThreads), 0, s>>>(b, a);
+        else if (a.final) ld_with_type(out_type, [&](auto type) { k_apply<kTile, true, type><<<grid, dim3(kThreads), 0, s>>>(b, a, out); });
+        else k_apply<kTile, false, LD_F32><<<grid, dim3(kThreads), 0, s>>>(b, a, out);
+        return ld_launch_status();
+    };
+    int32_t at = 0;
+    if (any[0] && any[1])
+        for (; at < prog[0].count && at < prog[1].count && memcmp(&prog[0].plan[at], &prog[1].plan[at], sizeof(Plan)) == 0; ++at)
+            if (launch(prog[0].plan[at], true, true) != LD_OK) return LD_ERR_HIP;
+    for (int32_t w = 0; w < 2; ++w)
+        for (int32_t k = at; any[w] && k < prog[w].count; ++k)
+            if (launch(prog[w].plan[k], w == 1, w == 0) != LD_OK) return LD_ERR_HIP;
+    return LD_OK;
+}
+
+int32_t most_parts(const Batch& b) {
+    int32_t most = 1;
+    for (int32_t i = 0; i < b.count; ++i) {
+        const int32_t parts = sum_parts(static_cast<int64_t>(b.m[i]) * b.n[i]);
+        if (parts > most) most = parts;
+    }
+    return most;
+}
+
+ld_status lay_out_group(const Batch& b, const Source& src, int32_t dtype, const Polynomial& p, hipStream_t s) {
+    int32_t most = 1;
+    for (int32_t i = 0; i < b.count; ++i) {
+        const int32_t tiles = tiles_of(b.m[i], kMuonPad) * tiles_of(b.n[i], kMuonPad);
+        if (tiles > most) most = tiles;
+    }
+    ld_with_type(dtype, [&](auto type) { k_lay_out<type><<<dim3(most, b.count), dim3(kThreads), 0, s>>>(b, src, ld_muon_scale(p.bounds.x[0])); });
+    return ld_launch_status();
+}
+
+}  // namespace
+
+extern "C" size_t ld_orthogonalize_workspace(const int64_t* rows, const int64_t* cols, int32_t n_mats) {
+    if (!rows || !cols || n_mats < 0 || n_mats > LD_MAX_TENSORS) return 0;
+    for (int32_t i = 0; i < n_mats; ++i)
+        if (!known_sides(rows[i], cols[i])) return 0;
+    return workspace_of(rows, cols, n_mats, 1);
+}
+
+extern "C" ld_status ld_orthogonalize(const void* const* src, const int64_t* src_stride, void* const* dst, const int64_t* dst_stride, const int64_t* rows,
+                                      const int64_t* cols, int32_t n_mats, int32_t dtype, int32_t out_dtype, int32_t steps, const float* coeff,
+                                      float eps, void* workspace, size_t workspace_bytes, ld_stream stream) {
+    if (n_mats < 0 || n_mats > LD_MAX_TENSORS || !ld_known_type(dtype) || !ld_known_type(out_dtype) || steps < 1 || !(eps >= 0.0f && eps <= 1e30f))
+        return LD_ERR_RANGE;
+    if (n_mats > 0 && (!src || !dst || !rows || !cols)) return LD_ERR_NULL;
+    Polynomial p;
+    if (!polynomial(p, steps, coeff)) return LD_ERR_RANGE;
+    for (int32_t i = 0; i < n_mats; ++i) {
+        if (!known_sides(rows[i], cols[i])) return LD_ERR_RANGE;
+        if (rows[i] == 0 || cols[i] == 0) continue;
+        if ((src_stride && src_stride[i] < 0) || (dst_stride && dst_stride[i] < cols[i])) return LD_ERR_RANGE;
+        if (!src[i] || !dst[i]) return LD_ERR_NULL;
+        if (!ld_aligned(src[i], ld_type_bytes(dtype)) || !ld_aligned(dst[i], ld_type_bytes(out_dtype))) return LD_ERR_ALIGN;
+    }
+    const size_t need = workspace_of(rows, cols, n_mats, 1);
+    if (need == 0) return LD_OK;
+    if (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < need) return LD_ERR_WORKSPACE;
+    ld_begin_call();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* scratch = static_cast<char*>(workspace) + kSumBytes;
+    for (int32_t i = 0; i < n_mats;) {
+        Batch b = {};
+        Source source = {};
+        FinalArgs out = {};
+        int64_t used = 0;
+        for (; i < n_mats; ++i) {
+            if (rows[i] == 0 || cols[i] == 0) continue;
+            if (!append(b, used, scratch, rows[i], cols[i])) break;
+            source.src[b.count - 1] = src[i], source.stride[b.count - 1] = src_stride ? src_stride[i] : cols[i];
+            out.out[b.count - 1] = dst[i], out.stride[b.count - 1] = dst_stride ? dst_stride[i] : cols[i];
+        }
+        if (b.count == 0) break;
+        source.sums = static_cast<double*>(workspace), source.eps = eps;
+        ld_with_type(dtype, [&](auto type) { k_squares<type><<<dim3(most_parts(b), b.count), dim3(kThreads), 0, s>>>(b, source); });
+        if (ld_launch_status() != LD_OK || lay_out_group(b, source, dtype, p, s) != LD_OK || run_steps(b, p, out, out_dtype, s) != LD_OK) return LD_ERR_HIP;
+    }
+    return LD_OK;
+}
+
+extern "C" size_t ld_merge_dense_muon_workspace(const int64_t* rows, const int64_t* cols, int32_t n_mats, int32_t W) {
+    if (!rows || !cols || n_mats < 0 || n_mats > LD_MAX_TENSORS || W < 0 || W > LD_MAX_WINDOW) return 0;
+    for (int32_t i = 0; i < n_mats; ++i)
+        if (!known_sides(rows[i], cols[i])) return 0;
+    return workspace_of(rows, cols, n_mats, W);
+}
+
+extern "C" ld_status ld_merge_dense_muon(float* const* w, float* const* m, const void* const* grad, const int64_t* rows, const int64_t* cols, int32_t n_mats,
+                                         int32_t W, int32_t dtype, float lr, float mu, int32_t nesterov, float weight_decay, const float* scale,
+                                         int32_t steps, const float* coeff, float eps, void* workspace, size_t workspace_bytes, ld_stream stream) {
+    if (n_mats < 0 || n_mats > LD_MAX_TENSORS || W < 0 || W > LD_MAX_WINDOW || !ld_known_type(dtype) || steps < 1 || !(eps >= 0.0f && eps <= 1e30f) ||
+        !(fabsf(lr) <= 1e30f) || !(fabsf(mu) <= 1e30f) || !(fabsf(weight_decay) <= 1e30f))
+        return LD_ERR_RANGE;
+    if (n_mats > 0 && W > 0 && (!w || !m || !grad || !rows || !cols)) return LD_ERR_NULL;
+    Polynomial p;
+    if (!polynomial(p, steps, coeff)) return LD_ERR_RANGE;
+    if (n_mats == 0 || W == 0) return LD_OK;
+    for (int32_t i = 0; i < n_mats; ++i) {
+        if (!known_sides(rows[i], cols[i]) || (scale && !(fabsf(scale[i]) <= 1e30f))) return LD_ERR_RANGE;
+        if (rows[i] == 0 || cols[i] == 0) continue;
+        if (!w[i] || !m[i]) return LD_ERR_NULL;
+        if (!ld_aligned(w[i], 4) || !ld_aligned(m[i], 4)) return LD_ERR_ALIGN;
+        for (int32_t t = 0; t < W; ++t) {
+            const void* g = grad[static_cast<int64_t>(t) * n_mats + i];
+            if (!g) return LD_ERR_NULL;
+            if (!ld_aligned(g, ld_type_bytes(dtype))) return LD_ERR_ALIGN;
+        }
+    }
+    const size_t need = workspace_of(rows, cols, n_mats, W);
+    if (need == 0) return LD_OK;
+    if (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < need) return LD_ERR_WORKSPACE;
+    ld_begin_call();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* scratch = static_cast<char*>(workspace) + kSumBytes;
+    int32_t i = 0, t = 0;  // the next problem
+    while (i < n_mats) {
+        Batch b = {};
+        MomentumArgs mom = {};
+        UpdateArgs up = {};
+        Source source = {};
+        FinalArgs out = {};
+        int64_t used = 0;
+        int32_t mats = 0;
+        for (bool room = true; room && i < n_mats;) {
+            if (rows[i] == 0 || cols[i] == 0) {
+                ++i;
+                continue;
+            }
+            const int32_t from = t;
+            for (; t < W && (room = append(b, used, scratch, rows[i], cols[i])); ++t) {
+                const int32_t k = b.count - 1;
+                mom.grad[k] = grad[static_cast<int64_t>(t) * n_mats + i];
+                source.stride[k] = out.stride[k] = cols[i];
+            }
+            if (t > from) {
+                mom.momentum[mats] = m[i], up.w[mats] = w[i];
+                mom.problem[mats] = up.problem[mats] = b.count - (t - from);
+                mom.steps[mats] = up.steps[mats] = t - from;
+                const double s = scale ? static_cast<double>(scale[i]) : rows[i] > cols[i] ? sqrt(static_cast<double>(rows[i]) / cols[i]) : 1.0;
+                up.rate[mats++] = static_cast<float>(static_cast<double>(lr) * s);
+            }
+            if (t == W) ++i, t = 0;
+        }
+        if (mats == 0) break;
+        for (int32_t k = 0; k < b.count; ++k) {
+            const int64_t large = ld_muon_large(b.m[k], b.n[k]);
+            source.src[k] = b.base[k] + kYT * large;  // the update lies there until X is laid out
+            out.out[k] = b.base[k] + kX * large;
+        }
+        source.sums = mom.sums = static_cast<double*>(workspace), source.eps = eps;
+        mom.mu = mu, mom.nesterov = nesterov;
+        up.keep = static_cast<float>(1.0 - static_cast<double>(lr) * static_cast<double>(weight_decay));
+        const dim3 grid(most_parts(b), mats);
+        ld_with_type(dtype, [&](auto type) { k_momentum<type><<<grid, dim3(kThreads), 0, s>>>(b, mom); });
+        if (ld_launch_status() != LD_OK || lay_out_group(b, source, LD_F32, p, s) != LD_OK || run_steps(b, p, out, LD_F32, s) != LD_OK) return LD_ERR_HIP;
+        k_update<<<dim3(2 * most_parts(b), mats), dim3(kThreads), 0, s>>>(b, up);
+        if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
+    }
+    return LD_OK;
+}

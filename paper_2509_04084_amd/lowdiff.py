@@ -150,6 +150,14 @@ def load() -> ctypes.CDLL:
     lib.ld_token_logprob.restype = i32
     lib.ld_token_logprob_grad.argtypes = [vp, i64, i32, i64, i32, vp, i32, f32, vp, vp, i64, vp, vp, i64, vp, i64, i32, vp]
     lib.ld_token_logprob_grad.restype = i32
+    lib.ld_orthogonalize_workspace.argtypes = [vp, vp, i32]
+    lib.ld_orthogonalize_workspace.restype = sz
+    lib.ld_orthogonalize.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, f32, vp, sz, vp]
+    lib.ld_orthogonalize.restype = i32
+    lib.ld_merge_dense_muon_workspace.argtypes = [vp, vp, i32, i32]
+    lib.ld_merge_dense_muon_workspace.restype = sz
+    lib.ld_merge_dense_muon.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, f32, f32, i32, f32, vp, i32, vp, f32, vp, sz, vp]
+    lib.ld_merge_dense_muon.restype = i32
     dbl = ctypes.c_double
     lib.ld_config_wasted_time.argtypes = [vp, dbl, dbl, dbl, dbl]
     lib.ld_config_wasted_time.restype = dbl
@@ -854,6 +862,118 @@ def ld_token_logprob_grad(logits: torch.Tensor, stats: torch.Tensor, ids: Option
                                       _elem(out, "out"), _stream(stream))
     _check("ld_token_logprob_grad", st)
     return out
+
+
+def _sides(mats: Sequence[torch.Tensor], name: str) -> Tuple[np.ndarray, np.ndarray]:
+    """Rows and columns of a list of matrices."""
+    shapes = [tuple(t.shape) for t in mats]
+    if any(len(s) != 2 for s in shapes):
+        raise TypeError(f"{name}: expected 2-D tensors")
+    both = np.array(shapes, dtype=np.int64).reshape(-1, 2)
+    return np.ascontiguousarray(both[:, 0]), np.ascontiguousarray(both[:, 1])
+
+
+def _coefficients(coeffs, steps: int) -> Optional[np.ndarray]:
+    """Three a step: from None (the usual ones), three for all steps, or three for each."""
+    if coeffs is None:
+        return None
+    c = np.asarray(coeffs, dtype=np.float32)
+    if c.shape == (3,):
+        c = np.broadcast_to(c, (max(int(steps), 0), 3))
+    if c.shape != (steps, 3):
+        raise ValueError("coeffs: three numbers, or three for every step")
+    return np.ascontiguousarray(c)
+
+
+def ld_orthogonalize_workspace(shapes: Sequence[Tuple[int, int]]) -> int:
+    both = np.array([tuple(s) for s in shapes], dtype=np.int64).reshape(-1, 2)
+    rows, cols = np.ascontiguousarray(both[:, 0]), np.ascontiguousarray(both[:, 1])
+    return int(load().ld_orthogonalize_workspace(_hp(rows), _hp(cols), len(both)))
+
+
+def ld_orthogonalize(mats: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None, steps: int = 5, coeffs=None,
+                     eps: float = 1e-7, out_dtype: Optional[torch.dtype] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> List[torch.Tensor]:
+    """Every matrix's nearest orthogonal one, about: `steps` Newton-Schulz steps of X <- (a I + b X X^T + c (X X^T)^2) X from
+    X = U / (|U|_F + eps), as precise as products in float32. Into `outs` (which may be the matrices themselves) or new tensors
+    of type `out_dtype` (theirs unless given). Matrices of one call share a type, their shapes are any, and rows may have any stride.
+    A matrix's result does not depend on the others of the call. `coeffs`: (a, b, c), or three for every step; those that
+    let singular values grow too far are refused."""
+    lib, n = load(), len(mats)
+    if outs is not None and len(outs) != n:
+        raise ValueError("mats and outs differ in length")
+    if not n:
+        return []
+    rows, cols = _sides(mats, "mats")
+    code, first = _elem(mats[0], "mats"), mats[0]
+    if any(t.dtype != first.dtype for t in mats):
+        raise TypeError("mats: expected tensors of one type")
+    coeff = _coefficients(coeffs, steps)
+    _one_device(first, (workspace, *mats[1:], *(outs or ())))
+    sp, ss = np.empty(n, np.uint64), np.empty(n, np.int64)
+    for i, t in enumerate(mats):
+        sp[i], _, ss[i] = _rows(t, "mats")
+    _on_device_of(stream, first)
+    if outs is None:
+        outs = [_output(out_dtype or first.dtype, first.device, stream, *t.shape) for t in mats]
+    elif any(a.shape != b.shape for a, b in zip(mats, outs)) or any(o.dtype != (out_dtype or outs[0].dtype) for o in outs):
+        raise ValueError("outs differ in shape from mats, or in type from one another or from out_dtype")
+    dp, ds = np.empty(n, np.uint64), np.empty(n, np.int64)
+    for i, t in enumerate(outs):
+        dp[i], _, ds[i] = _rows(t, "outs", written=True)
+        if dp[i] == sp[i] and t.numel() and (t.dtype != first.dtype or ds[i] != ss[i]):
+            raise ValueError("outs: in place a matrix keeps its type and stride")
+    if workspace is None and (need := lib.ld_orthogonalize_workspace(_hp(rows), _hp(cols), n)) > 0:
+        workspace = _scratch(need, first.device, stream)
+    st = lib.ld_orthogonalize(_hp(sp), _hp(ss), _hp(dp), _hp(ds), _hp(rows), _hp(cols), n, code, _elem(outs[0], "outs"), int(steps),
+                              None if coeff is None else _hp(coeff), eps, _dev(workspace, torch.uint8, "workspace"),
+                              workspace.numel() if workspace is not None else 0, _stream(stream))
+    _check("ld_orthogonalize", st)
+    return list(outs)
+
+
+def ld_merge_dense_muon_workspace(shapes: Sequence[Tuple[int, int]], W: int = 1) -> int:
+    both = np.array([tuple(s) for s in shapes], dtype=np.int64).reshape(-1, 2)
+    rows, cols = np.ascontiguousarray(both[:, 0]), np.ascontiguousarray(both[:, 1])
+    return int(load().ld_merge_dense_muon_workspace(_hp(rows), _hp(cols), len(both), int(W)))
+
+
+def ld_merge_dense_muon(ws: Sequence[torch.Tensor], ms: Sequence[torch.Tensor], grads: Sequence[Sequence[torch.Tensor]], lr: float,
+                        momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale=None, steps: int = 5,
+                        coeffs=None, eps: float = 1e-7, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Replays dense gradients, grads[t][i] of matrix i, as steps of the optimizer that orthogonalises its updates, onto the
+    weights ws and momenta ms (float32), in place; with one t it is a training step. Per step: m = momentum * m + g, u = g + momentum * m
+    with nesterov, else m, w = (1 - lr * weight_decay) * w - lr * scale[i] * orthogonalize(u). scale: one number, one for every
+    matrix, or None: sqrt(max(1, rows / cols)). Gradients share one of the types float32, bfloat16 and float16. Any cut of the
+    gradients into calls gives the same bits."""
+    lib, n, W = load(), len(ws), len(grads)
+    if len(ms) != n or any(len(g) != n for g in grads):
+        raise ValueError("ws, ms and every step's grads differ in length")
+    if not n:
+        return
+    rows, cols = _sides(ws, "ws")
+    shapes = [t.shape for t in ws]
+    if any(m.shape != s for m, s in zip(ms, shapes)) or any(g.shape != s for step in grads for g, s in zip(step, shapes)):
+        raise ValueError("a weight, its momentum and its gradients differ in shape")
+    flat = [g for step in grads for g in step]
+    dtype = flat[0].dtype if flat else torch.float32
+    code = _ELEM.get(dtype)
+    if code is None:
+        raise TypeError(f"grads: expected float32, bfloat16 or float16, got {dtype}")
+    coeff = _coefficients(coeffs, steps)
+    w, m, g = _Table(ws, torch.float32), _Table(ms, torch.float32), _Table(flat, dtype)
+    _one_device(ws[0], (workspace,), w, m, g)
+    wp, mp, gp = w.checked("ws"), m.checked("ms"), g.checked("grads")
+    _on_device_of(stream, ws[0])
+    factor = None
+    if scale is not None:
+        factor = np.ascontiguousarray(np.broadcast_to(np.asarray(scale, dtype=np.float32), (n,)))
+    if workspace is None and (need := lib.ld_merge_dense_muon_workspace(_hp(rows), _hp(cols), n, W)) > 0:
+        workspace = _scratch(need, ws[0].device, stream)
+    st = lib.ld_merge_dense_muon(wp, mp, gp, _hp(rows), _hp(cols), n, W, code, lr, momentum, int(nesterov), weight_decay,
+                                 None if factor is None else _hp(factor), int(steps), None if coeff is None else _hp(coeff), eps,
+                                 _dev(workspace, torch.uint8, "workspace"), workspace.numel() if workspace is not None else 0, _stream(stream))
+    _check("ld_merge_dense_muon", st)
 
 
 class ConfigParams(ctypes.Structure):

@@ -1,0 +1,383 @@
+"""Orthogonalised updates, and their replay, on the GPU against the definitions in 64 bits.
+
+Tolerances come from the roundings of the computation, put into it one by one in 64 bits as random ones (`noisy`): an operand of a
+product is known to 22 bits (two halves), 2^-22 relative and no better than 2^-25 of its scaled unit, 2^-39; the product of two lower
+halves is left out, 2^-22 of both operands; sums of K terms are rounded to 32 bits 3 K / 16 times, 2^-24 of a partial sum each, which add up as a
+random walk. The result may be off by four times the noise of three such runs in the Frobenius norm, by eight times their
+largest element's where that is compared, and by the rounding to its own type. What a mistake does is far larger: a forgotten lower half
+is 2^10 times these roundings.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2509_04084_amd import lowdiff as ld
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16, F16, F64 = torch.float32, torch.bfloat16, torch.float16, torch.float64
+U = 2.0 ** -24
+UNIT = {F32: U, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+STEP = {F32: 2.0 ** -149, BF16: 2.0 ** -133, F16: 2.0 ** -24}
+USUAL = (3.4445, -4.7750, 2.0315)
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def same_bits(a, b):
+    return torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+def coefficients(coeffs, steps):
+    c = np.broadcast_to(np.float32(USUAL if coeffs is None else coeffs), (steps, 3)) if np.ndim(coeffs) < 2 else np.float32(coeffs)
+    return c.astype(np.float64).tolist()
+
+
+def orthogonal64(u, steps=5, coeffs=None, eps=1e-7):
+    """The definition."""
+    x = u.double()
+    norm = float(x.square().sum().sqrt())
+    x = x / (norm + float(np.float32(eps))) if norm else x
+    flip = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if flip else x
+    for a, b, c in coefficients(coeffs, steps):
+        A = torch.mm(x, x.t().contiguous())
+        x = a * x + torch.mm(b * A + c * torch.mm(A, A), x)
+    return x.t().contiguous() if flip else x
+
+
+def runs_of(coeffs, wide):
+    """Numbers of steps that go by one Gram matrix: up to three or a growth of 48, from the last, of wide matrices, else two or 16."""
+    top, grows, longest, most = 1.0, [], 3 if wide else 2, 48 if wide else 16
+    for a, b, c in coeffs:
+        x = np.linspace(0, top, 10001)
+        f = a + b * x ** 2 + c * x ** 4
+        grows.append(float(np.abs(f).max()))
+        top = float(np.abs(x * f).max())
+    runs, grown = [], 0.0
+    for g in grows[::-1] if wide else grows:
+        if not runs or runs[-1] == longest or grown * g > most:
+            runs, grown = runs + [0], 1.0
+        runs[-1], grown = runs[-1] + 1, grown * g
+    return runs[::-1] if wide else runs
+
+
+def noisy(u, seed, steps=5, coeffs=None, eps=1e-7, source=0.0):
+    """The computation with its roundings; `source`: relative error of the update itself."""
+    g = gen(seed)
+    noise = lambda x: torch.rand(x.shape, generator=g, device=DEV, dtype=F64) * 2 - 1  # noqa: E731
+    held = lambda x: x + noise(x) * (2 ** -22 * x.abs() + 2 ** -39)  # noqa: E731
+
+    def product(p, q):  # p q^T, q given as its rows
+        qt, K = q.t().contiguous(), p.shape[1]
+        y = torch.mm(held(p), held(q).t().contiguous())
+        size = torch.mm(p * p, qt * qt).sqrt()
+        walk = torch.randn(y.shape, generator=g, device=DEV, dtype=F64) * U * math.sqrt(max(1.0, 3 * K / 16))
+        return y + noise(y) * 2 ** -22 * size + walk * (y.abs() + size)
+
+    def symmetric(y):
+        return torch.tril(y) + torch.tril(y, -1).t()
+    x = u.double()
+    x = x + noise(x) * source * x.abs()
+    norm = float(x.square().sum().sqrt())
+    x = x / (norm + float(np.float32(eps))) if norm else x
+    x = x * (1 + U * noise(x))
+    flip = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if flip else x
+    c, s = coefficients(coeffs, steps), 0
+    for n in runs_of(c, 2 * x.shape[1] >= 5 * x.shape[0]):
+        A, q = symmetric(product(x, x)), None
+        for k in range(n):
+            ca, cb, cc = c[s]
+            s += 1
+            p = cb * held(A) + cc * symmetric(product(A, A)) + ca * torch.eye(A.shape[0], dtype=F64, device=DEV)
+            q_next = p if q is None else symmetric(product(p, q))
+            if k + 1 < n:
+                A = symmetric(product(p, symmetric(product(p, A))))
+            q = q_next
+        x = product(q, x.t().contiguous())
+    return x.t().contiguous() if flip else x
+
+
+def check(got, u, tag, out_dtype=F32, **kw):
+    want = orthogonal64(u, **kw)
+    runs = [noisy(u, seed, **kw) - want for seed in range(3)]
+    norm, most = max(float(r.norm()) for r in runs), max(float(r.abs().max()) for r in runs)
+    assert got.shape == want.shape and got.dtype == out_dtype
+    off = got.double() - want
+    rounding = UNIT[out_dtype] * want.abs() + 0.5 * STEP[out_dtype]
+    assert not bool(off.isnan().any()), tag
+    assert float(off.norm()) <= 4 * norm + float(rounding.norm()), (tag, float(off.norm()), norm, float(rounding.norm()))
+    assert bool((off.abs() <= 8 * most + rounding).all()), (tag, float(off.abs().max()), most)
+
+
+def matrix(r, c, g, kind="plain"):
+    z = torch.randn(r, c, generator=g, device=DEV, dtype=F64)
+    if kind == "plain":
+        return z
+    if kind == "heavy":
+        return z * (torch.randn(r, c, generator=g, device=DEV, dtype=F64) ** 2 + 0.1) * torch.exp(torch.randn(r, 1, generator=g, device=DEV, dtype=F64))
+    low = torch.mm(torch.randn(r, 3, generator=g, device=DEV, dtype=F64), torch.randn(3, c, generator=g, device=DEV, dtype=F64))
+    return low + {"low rank": 1e-3, "lower rank": 1e-5, "rank 3": 0.0}[kind] * z
+
+
+SHAPES = [(1, 1), (1, 2), (1, 500), (500, 1), (2, 3), (7, 7), (31, 33), (33, 31), (63, 64), (64, 64), (65, 64), (64, 65), (100, 37), (128, 128), (129, 127),
+          (127, 300), (192, 192), (257, 130), (320, 1000), (513, 511)]
+
+
+@pytest.mark.parametrize("r,c", SHAPES)
+def test_shapes(r, c):
+    print(f"[orthogonalize] {r} x {c}", flush=True)
+    u = matrix(r, c, gen(r * 1000 + c)).to(F32)
+    check(ld.ld_orthogonalize([u])[0], u, (r, c))
+
+
+@pytest.mark.parametrize("kind", ["plain", "heavy", "low rank", "lower rank", "rank 3"])
+@pytest.mark.parametrize("r,c", [(96, 700), (300, 200)])
+def test_spectra(r, c, kind):
+    print(f"[orthogonalize] {r} x {c} {kind}", flush=True)
+    u = matrix(r, c, gen(3), kind).to(F32)
+    check(ld.ld_orthogonalize([u])[0], u, kind)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("out_dtype", [F32, BF16, F16])
+def test_types(dtype, out_dtype):
+    us = [matrix(r, c, gen(5), "heavy").mul(1e-2).to(dtype) for r, c in ((70, 150), (150, 70), (129, 129))]
+    for o, u in zip(ld.ld_orthogonalize(us, out_dtype=out_dtype), us):
+        check(o, u, (dtype, out_dtype), out_dtype)
+
+
+@pytest.mark.parametrize("steps", range(1, 17))
+def test_steps(steps):
+    u = matrix(90, 140, gen(steps)).to(F32)
+    gentle = (1.5, -0.5, 0.0)
+    check(ld.ld_orthogonalize([u], steps=steps)[0], u, steps, steps=steps)
+    check(ld.ld_orthogonalize([u], steps=steps, coeffs=gentle)[0], u, (steps, gentle), steps=steps, coeffs=gentle)
+
+
+def test_coefficients_of_every_step():
+    """Other coefficients at every step, the first ones growing further than a run may; and ones that only scale."""
+    schedule = [(8.2, -22.9, 16.5), (4.06, -2.86, 0.518), (3.9, -2.82, 0.525), (3.28, -2.41, 0.485), (2.28, -1.62, 0.4)]
+    for r, c in ((100, 260), (200, 210)):
+        u = matrix(r, c, gen(9), "heavy").to(F32)
+        check(ld.ld_orthogonalize([u], coeffs=schedule)[0], u, "schedule", coeffs=schedule)
+    check(ld.ld_orthogonalize([u], steps=2, coeffs=(0.5, 0.0, 0.0))[0], u, "scaling", steps=2, coeffs=(0.5, 0.0, 0.0))
+    check(ld.ld_orthogonalize([u], steps=3, coeffs=(-1.5, 0.5, 0.0))[0], u, "sign", steps=3, coeffs=(-1.5, 0.5, 0.0))
+
+
+@pytest.mark.parametrize("r,c", [(768, 768), (1600, 400), (1001, 1333), (2048, 2048)])
+def test_larger(r, c):
+    print(f"[orthogonalize] {r} x {c}", flush=True)
+    u = matrix(r, c, gen(r + c), "heavy").to(F32)
+    check(ld.ld_orthogonalize([u])[0], u, (r, c))
+
+
+@pytest.mark.parametrize("size", [1e-44, 1e-30, 1e30, 1e38])
+def test_magnitudes(size):
+    u = torch.sign(matrix(40, 50, gen(1))).mul(size).to(F32) if size < 1e-40 else matrix(40, 50, gen(1)).clamp(-3, 3).mul(size).to(F32)
+    check(ld.ld_orthogonalize([u], eps=0.0)[0], u, size, eps=0.0)
+    check(ld.ld_orthogonalize([u])[0], u, size)
+
+
+def test_a_matrix_does_not_depend_on_the_others_of_its_call():
+    g = gen(11)
+    us = [matrix(r, c, g).to(F32) for r, c in SHAPES * 4]  # more than a group holds
+    us[5].zero_()
+    together = ld.ld_orthogonalize(us)
+    for i in (0, 3, 5, 13, 40, 63, 64, 79):
+        assert same_bits(ld.ld_orthogonalize([us[i]])[0], together[i]), i
+    assert not together[5].any()
+    for bad in (math.nan, math.inf, -math.inf):
+        us[7][3, 2] = bad
+        after = ld.ld_orthogonalize(us)
+        assert bool(after[7].isnan().all())
+        for i, (x, y) in enumerate(zip(after, together)):
+            assert i == 7 or same_bits(x, y), (bad, i)
+
+
+def test_strides_in_place_and_what_lies_around():
+    g = gen(13)
+    wide = matrix(90, 200, g).to(BF16)
+    u = wide[:, 7:130]
+    want = ld.ld_orthogonalize([u.contiguous()])[0]
+    assert same_bits(ld.ld_orthogonalize([u])[0], want)
+    room = torch.full((90, 200), 7.0, dtype=BF16, device=DEV)
+    assert ld.ld_orthogonalize([u], [room[:, 3:126]])[0].data_ptr() == room[:, 3:126].data_ptr()
+    assert same_bits(room[:, 3:126], want) and bool((room[:, :3] == 7).all()) and bool((room[:, 126:] == 7).all())
+    place = wide.clone()
+    ld.ld_orthogonalize([place[:, 7:130]], [place[:, 7:130]])
+    assert same_bits(place[:, 7:130], want) and same_bits(place[:, :7], wide[:, :7]) and same_bits(place[:, 130:], wide[:, 130:])
+    tall = matrix(200, 90, g).to(F32)
+    many = ld.ld_orthogonalize([tall[:, 1:80], tall[::2], tall[:0], tall[:, :0]])
+    assert same_bits(many[0], ld.ld_orthogonalize([tall[:, 1:80].contiguous()])[0])
+    assert same_bits(many[1], ld.ld_orthogonalize([tall[::2].contiguous()])[0]) and many[2].shape == (0, 90) and many[3].shape == (200, 0)
+    one = tall[:1].expand(50, 90)  # fifty times one row
+    check(ld.ld_orthogonalize([one])[0], one.contiguous(), "expanded")
+
+
+def test_workspace_holds_anything_on_entry():
+    u = [matrix(130, 257, gen(15)).to(F32), matrix(65, 20, gen(16)).to(F32)]
+    want = ld.ld_orthogonalize(u)
+    need = ld.ld_orthogonalize_workspace([t.shape for t in u])
+    for fill in (0, 255, 0x7C):
+        ws = torch.full((need,), fill, dtype=torch.uint8, device=DEV)
+        for a, b in zip(ld.ld_orthogonalize(u, workspace=ws), want):
+            assert same_bits(a, b)
+
+
+# ------------------------------------------------------------------------------------------------------ replay
+
+def window(shapes, W, dtype, seed):
+    g = gen(seed)
+    ws = [(torch.randn(s, generator=g, device=DEV) * 0.02) for s in shapes]
+    ms = [matrix(*s, g, "heavy").mul(1e-2).to(F32) for s in shapes]
+    grads = [[matrix(*s, g, "heavy").mul(1e-3).to(dtype) for s in shapes] for _ in range(W)]
+    return ws, ms, grads
+
+
+def replay64(w, m, grads, lr, mu, nesterov, decay, scale):
+    """w and m after the window, and bounds on their errors."""
+    lr, mu, decay, scale = (float(np.float32(v)) for v in (lr, mu, decay, scale))
+    w, m = w.double(), m.double()
+    e_m, e_w = torch.zeros_like(m), torch.zeros_like(w)
+    for g in grads:
+        g = g.double()
+        m = mu * m + g
+        e_m = mu * e_m + U * m.abs()
+        u = g + mu * m if nesterov else m
+        rel = float((e_m / m.abs().clamp_min(1e-30)).median()) * 2 + U  # of the update, as noise in it
+        o = orthogonal64(u)
+        noise = max(float((noisy(u, s, source=rel) - o).abs().max()) for s in range(3))
+        w = (1 - lr * decay) * w - lr * scale * o
+        # keep and rate are rounded once each, the product with keep, and the sum
+        e_w = e_w + abs(lr * scale) * 8 * noise + U * (3 * w.abs() + 3 * abs(lr * scale) * o.abs())
+    return w, m, e_w, e_m
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("W,nesterov,decay", [(1, True, 0.0), (1, False, 0.1), (4, True, 0.05)])
+def test_replay(W, nesterov, decay, dtype):
+    print(f"[muon] W={W} {dtype}", flush=True)
+    shapes = [(64, 200), (200, 64), (129, 129), (1, 50)]
+    ws, ms, grads = window(shapes, W, dtype, 21)
+    w0, m0 = [w.clone() for w in ws], [m.clone() for m in ms]
+    for scale in (None, 0.3, [0.1, 2.0, 0.0, -1.0]):
+        for a, b in zip(ws + ms, w0 + m0):
+            a.copy_(b)
+        ld.ld_merge_dense_muon(ws, ms, grads, 0.02, 0.9, nesterov, decay, scale)
+        for i, s in enumerate(shapes):
+            f = math.sqrt(max(1.0, s[0] / s[1])) if scale is None else scale if isinstance(scale, float) else scale[i]
+            w, m, e_w, e_m = replay64(w0[i], m0[i], [g[i] for g in grads], 0.02, 0.9, nesterov, decay, f)
+            assert bool(((ms[i].double() - m).abs() <= 1.01 * e_m).all()), (scale, i, "m")
+            assert bool(((ws[i].double() - w).abs() <= 1.01 * e_w).all()), (scale, i, "w")
+
+
+def test_any_cut_of_a_window_gives_the_same_bits():
+    shapes = [(130, 70), (64, 64), (5, 300)]
+    W = 70  # more than a group holds
+    ws, ms, grads = window(shapes, W, BF16, 23)
+    w0, m0 = [w.clone() for w in ws], [m.clone() for m in ms]
+    ld.ld_merge_dense_muon(ws, ms, grads, 0.02, weight_decay=0.01)
+    for cut in (1, 13, 64):
+        w1, m1 = [w.clone() for w in w0], [m.clone() for m in m0]
+        for t in range(0, W, cut):
+            ld.ld_merge_dense_muon(w1, m1, grads[t:t + cut], 0.02, weight_decay=0.01)
+        for a, b in zip(ws + ms, w1 + m1):
+            assert same_bits(a, b), cut
+    one = [w0[1].clone()], [m0[1].clone()]  # and a matrix alone
+    ld.ld_merge_dense_muon(*one, [[g[1]] for g in grads], 0.02, weight_decay=0.01)
+    assert same_bits(one[0][0], ws[1]) and same_bits(one[1][0], ms[1])
+
+
+def test_a_replay_is_the_orthogonalised_update():
+    """Without momentum the update is the gradient: what ld_orthogonalize makes of it is what is subtracted."""
+    (w,), (m,), ((g,),) = window([(100, 180)], 1, BF16, 25)
+    w0 = w.clone()
+    ld.ld_merge_dense_muon([w], [m], [[g]], 0.5, momentum=0.0, scale=1.0)
+    o = ld.ld_orthogonalize([g], out_dtype=F32)[0]
+    assert same_bits(m, g.float()) and same_bits(w, (w0.double() - 0.5 * o.double()).float())  # half of o is exact
+
+
+def test_nothing_to_replay():
+    w, m = torch.ones(3, 4, device=DEV), torch.ones(3, 4, device=DEV)
+    ld.ld_merge_dense_muon([w], [m], [], 0.1)
+    assert bool((w == 1).all()) and bool((m == 1).all())
+    e = torch.zeros(0, 4, device=DEV)
+    ld.ld_merge_dense_muon([e, w], [e, m], [[e, w.clone()]], 0.1)
+    assert bool((m == float(np.float32(0.95) + np.float32(1.0))).all())
+
+
+def test_on_another_stream_and_in_graphs():
+    """Two graphs that share a workspace, replayed in turn with eager calls between."""
+    shapes = [(150, 90), (64, 130)]
+    ws, ms, grads = window(shapes, 2, BF16, 27)
+    us = [matrix(*s, gen(28)).to(F32) for s in shapes]
+    state = lambda: [t.clone() for t in ws + ms]  # noqa: E731
+    start = state()
+
+    def reset():
+        for a, b in zip(ws + ms, start):
+            a.copy_(b)
+
+    def step(stream=None):
+        ld.ld_merge_dense_muon(ws, ms, grads, 0.02, stream=stream)
+        return ld.ld_orthogonalize(us, stream=stream)
+    want_o = step()
+    want = state()
+    reset()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got_o = step(side)
+    torch.cuda.current_stream().wait_stream(side)
+    for a, b in zip(state() + got_o, want + want_o):
+        assert same_bits(a, b)
+    workspace = torch.empty(max(ld.ld_orthogonalize_workspace(shapes), ld.ld_merge_dense_muon_workspace(shapes, 2)), dtype=torch.uint8, device=DEV)
+    outs = [torch.empty_like(u) for u in us]
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with torch.cuda.graph(graphs[0]):
+        ld.ld_merge_dense_muon(ws, ms, grads, 0.02, workspace=workspace)
+    with torch.cuda.graph(graphs[1]):
+        ld.ld_orthogonalize(us, outs, workspace=workspace)
+    for _ in range(3):
+        reset()
+        for o in outs:
+            o.fill_(5.0)
+        graphs[0].replay()
+        graphs[1].replay()
+        for a, b in zip(state() + outs, want + want_o):
+            assert same_bits(a, b)
+        reset()
+        step()
+
+
+def test_refusals_on_the_gpu():
+    a = torch.zeros(4, 6, device=DEV)
+    with pytest.raises(ld.LowDiffError):
+        ld.ld_orthogonalize([a], steps=0)
+    with pytest.raises(ld.LowDiffError):
+        ld.ld_orthogonalize([a], coeffs=(9.0, 0.0, 0.0))
+    with pytest.raises(ld.LowDiffError):
+        ld.ld_orthogonalize([a], eps=-1.0)
+    with pytest.raises(TypeError):
+        ld.ld_orthogonalize([a.t()])
+    with pytest.raises(ValueError, match="rows overlap"):
+        ld.ld_orthogonalize([a], [torch.zeros(6, device=DEV).expand(4, 6)])
+    with pytest.raises(ValueError):
+        ld.ld_orthogonalize([a], [a.t()])
+    with pytest.raises(ValueError, match="in place"):
+        ld.ld_orthogonalize([torch.zeros(4, 6, device=DEV, dtype=BF16)[:2]] * 0 + [a[:, :3]], [a.view(-1)[:12].view(4, 3)])
+    with pytest.raises(ld.LowDiffError):
+        ld.ld_orthogonalize([a], workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+    with pytest.raises(TypeError):
+        ld.ld_merge_dense_muon([a.half()], [a.half()], [[a]], 0.1)
+    with pytest.raises(TypeError):
+        ld.ld_merge_dense_muon([a], [a.clone()], [[a.double()]], 0.1)
+    with pytest.raises(ld.LowDiffError):
+        ld.ld_merge_dense_muon([a], [a.clone()], [[a.clone()]], float("nan"))
