@@ -602,8 +602,10 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
  *              LD_ERR_RANGE where they let singular values of up to 1 grow beyond 8, or grow them
  *              by a factor of more than 64 in a step
  *   steps      1 <= steps <= 16;  eps >= 0
- *   workspace  dev, 256-byte aligned, ld_orthogonalize_workspace() bytes: about
- *              (12 n + 20 m) m a matrix of sides m <= n, for as many at a time as 2 GiB hold
+ *   workspace  dev, 256-byte aligned, ld_orthogonalize_workspace() bytes: about (12 n + 20 m) m for
+ *              a matrix of sides m <= n, for as many at a time as 8 GiB hold.  With less, down to
+ *              what the largest matrix alone needs, a call takes fewer at a time: the same results,
+ *              slower
  *
  * ld_merge_dense_muon - replays W dense gradients of a list of weight matrices as steps of the
  * optimizer that orthogonalises its updates; W = 1 is a training step.  In order t = 0 .. W-1:
@@ -619,7 +621,7 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
  *              [rows][cols] contiguous elements of `dtype`
  *   scale      host [n_mats] fp32, or NULL: sqrt(max(1, rows / cols))
  *   0 <= W <= LD_MAX_WINDOW
- *   workspace  dev, 256-byte aligned, ld_merge_dense_muon_workspace() bytes
+ *   workspace  dev, 256-byte aligned, ld_merge_dense_muon_workspace() bytes, or fewer, as above
  * Errors: LD_ERR_NULL, LD_ERR_RANGE, LD_ERR_ALIGN, LD_ERR_WORKSPACE, LD_ERR_HIP.
  */
 #define LD_MAX_SIDE 65536

@@ -7,8 +7,8 @@
 // 22 bits, and a product is three MFMA products: hh + hl + lh, summed in 32 bits. Values are scaled by powers of two that the
 // coefficients bound. A run of steps works on the Gram matrix alone: with P = a I + b A + c A^2, A' = P A P and Q' = P Q, all of m by
 // m, symmetric and commuting, so that half of each is computed and mirrored; X is read for its Gram matrix and multiplied by Q once a
-// run (ld_muon_shape.h says when a run ends, and why). Five steps on m x n cost 6 m^2 n + 14 m^3 products' operations where n >= 2.5 m,
-// else 9 m^2 n + 11 m^3, instead of 15 m^2 n + 5 m^3 (symmetric halves there too).
+// run (ld_muon_shape.h says when a run ends, and why): 6 m^2 n + 14 m^3 products' operations for five steps of a wide matrix instead of
+// 15 m^2 n + 5 m^3 (symmetric halves there too).
 //
 // In memory a matrix lies as blocks of 32 columns, in each of them row after row: 32 upper halves, 32 lower halves, 128 bytes, whose eight
 // 16-byte pieces are permuted by the row, as shared memory wants them: a tile's block is contiguous, and is copied into shared memory as it is.
@@ -30,10 +30,11 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
+constexpr int kCUs = 256;
 constexpr int kMost = 64;                                    // problems of a group
-constexpr int64_t kGroupBytes = static_cast<int64_t>(2) << 30;  // scratch of a group, unless one problem needs more
+constexpr int64_t kGroupBytes = static_cast<int64_t>(8) << 30;  // scratch of a group, unless one problem needs more
 constexpr int kSumParts = 256;                               // partial sums of squares of a problem at most
-constexpr int64_t kSumElems = 8192;                          // elements of one, at least
+constexpr int64_t kSumElems = 4096;                          // elements of one, at least
 
 enum Buffer { kX, kXT, kYT, kA, kP, kR, kQ0, kQ1 };
 
@@ -42,6 +43,7 @@ struct Batch {
     char* base[kMost];
     int32_t m[kMost], n[kMost];
     int32_t flipped[kMost];
+    int32_t kind[kMost];       // which of a launch's plans is a problem's
     int32_t first[kMost + 1];  // tiles of a launch before a problem's
     int32_t count;
 };
@@ -52,6 +54,8 @@ __device__ __forceinline__ char* buffer_of(const Batch& b, int32_t i, int32_t wh
     const int64_t large = m * n * 4 + slack, small = m * m * 4 + slack;
     return b.base[i] + (which < 3 ? which * large : 3 * large + (which - 3) * small);
 }
+// Tiles over a side: all of its padding is written too.
+__host__ __device__ __forceinline__ int32_t tiles_of(int64_t side, int32_t tile) { return static_cast<int32_t>((side + tile - 1) / tile); }
 // Where the eight upper halves of row r, columns [8 c, 8 c + 8) lie, in bytes; the lower ones are 64 bytes on, permuted alike.
 __device__ __forceinline__ int64_t piece_at(int64_t rows, int64_t r, int64_t c, int32_t lower) {
     return ((c >> 2) * rows + r) * kMuonRowBytes + ((((c & 3) | lower << 2) ^ (r & 7)) << 4);
@@ -80,8 +84,8 @@ struct Product {
     int32_t out, out_t;    // of C and, where not symmetric, of its transposed
 };
 struct Plan {
-    Product prod[2];       // the second of a launch with twice as many tiles
-    int32_t products;
+    Product prod[2];
+    int32_t products;      // 0: a problem has no part in the launch
     int32_t apply;         // X' = Q X, with `final` where it goes
     int32_t final;
     int32_t long_sum;      // the columns are n, not m
@@ -89,6 +93,9 @@ struct Plan {
     float inv;             // 1 / scale of the operands' product
     float scale[2];        // of what is kept
     float ca, cb, cc;      // coefficients, cb times 1 / scale of A
+};
+struct Plans {
+    Plan of[kMuonKinds];
 };
 // Where X_S goes.
 struct FinalArgs {
@@ -99,13 +106,27 @@ struct FinalArgs {
 typedef const void __attribute__((address_space(1))) * global_ptr;
 typedef void __attribute__((address_space(3))) * shared_ptr;
 
-// TILE rows of a block of columns into shared memory, 16 bytes a lane, as they lie.
-template <int TILE>
+// A tile of SIDE by SIDE sums, by DOWN x ACROSS waves, BLOCKS blocks of columns at a time in shared memory, and as many on their way;
+// without blocks each wave loads what it needs for itself.
+template <int SIDE_, int DOWN_, int ACROSS_, int BLOCKS_> struct Tile {
+    static constexpr int SIDE = SIDE_, DOWN = DOWN_, ACROSS = ACROSS_, BLOCKS = BLOCKS_;
+    static constexpr int THREADS = DOWN * ACROSS * LD_WAVE, WAVES = BLOCKS == 1 ? 2 : 1;  // waves of a SIMD
+    static constexpr int R = SIDE / DOWN / 32, C = SIDE / ACROSS / 32;            // MFMA tiles of a wave
+    static constexpr int BLOCK_BYTES = SIDE * static_cast<int>(kMuonRowBytes);     // an operand's, of a block
+    static constexpr int STAGE_BYTES = 2 * BLOCKS * BLOCK_BYTES;
+    static constexpr int ROWS = SIDE < 64 ? SIDE : 64;                             // rows of sums laid out at a time
+    static constexpr int STRIDE = SIDE + 2;                                        // floats of one: rows and columns read by eights lie in different banks
+    static constexpr int SHARED = 2 * STAGE_BYTES > ROWS * STRIDE * 4 ? 2 * STAGE_BYTES : ROWS * STRIDE * 4;
+};
+
+// A block of an operand's rows into shared memory, 16 bytes a lane, as they lie.
+template <typename T>
 __device__ __forceinline__ void fetch(const char* from, char* to) {
+    constexpr int kEach = T::BLOCK_BYTES / 1024 / (T::THREADS / LD_WAVE);
     const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LD_WAVE);
 #pragma unroll
-    for (int i = 0; i < TILE / 32; ++i) {
-        const int32_t at = (wave * (TILE / 32) + i) * 1024;
+    for (int i = 0; i < kEach; ++i) {
+        const int32_t at = (wave * kEach + i) * 1024;
         __builtin_amdgcn_global_load_lds((global_ptr)(from + at + ld_lane() * 16), (shared_ptr)(to + at), 16, 0, 0);
     }
 }
@@ -114,66 +135,107 @@ __device__ __forceinline__ half8 fragment(const char* tile, int32_t row, int32_t
     return *reinterpret_cast<const half8*>(tile + row * kMuonRowBytes + ((piece ^ (row & 7)) << 4));
 }
 
-// A tile's sums, four waves of a quarter each.
-template <int TILE>
-__device__ __forceinline__ void multiply(const char* left, int64_t left_rows, const char* right, int64_t right_rows, int32_t blocks, char* shared,
-                                         f32x16 (&acc)[TILE / 64][TILE / 64]) {
-    constexpr int N = TILE / 64, kBytes = TILE * static_cast<int>(kMuonRowBytes);
-    const int32_t lane = ld_lane(), wave = threadIdx.x / LD_WAVE, row = (wave >> 1) * (TILE / 2) + (lane & 31), col = (wave & 1) * (TILE / 2) + (lane & 31);
+// One wave's tile, straight from memory: kAhead blocks' operands on their way while one is multiplied.
+template <typename T>
+__device__ __forceinline__ void multiply_alone(const char* left, int64_t left_rows, const char* right, int64_t right_rows, int32_t blocks,
+                                               f32x16 (&acc)[T::R][T::C]) {
+    constexpr int kAhead = 8;
+    const int32_t row = ld_lane() & 31, half = ld_lane() >> 5;
     const int64_t left_step = left_rows * kMuonRowBytes, right_step = right_rows * kMuonRowBytes;
-    fetch<TILE>(left, shared);
-    fetch<TILE>(right, shared + kBytes);
-    __syncthreads();
-    for (int32_t k = 0; k < blocks; ++k) {
-        char* now = shared + (k & 1) * 2 * kBytes;
-        if (k + 1 < blocks) {
-            char* next = shared + (~k & 1) * 2 * kBytes;
-            fetch<TILE>(left + (k + 1) * left_step, next);
-            fetch<TILE>(right + (k + 1) * right_step, next + kBytes);
+    half8 x[kAhead][2][2], y[kAhead][2][2];  // [block][lower][16 columns]
+    const auto load = [&](int32_t k, int at) {
+#pragma unroll
+        for (int l = 0; l < 2; ++l)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                x[at][l][s] = fragment(left + k * left_step, row, 4 * l + 2 * s + half);
+                y[at][l][s] = fragment(right + k * right_step, row, 4 * l + 2 * s + half);
+            }
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (u < blocks) load(u, u);
+    for (int32_t k = 0; k < blocks; k += kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (k + u >= blocks) break;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int l = 0; l < 3; ++l) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[u][l == 0][s], y[u][l == 1][s], acc[0][0], 0, 0, 0);
+            if (k + u + kAhead < blocks) load(k + u + kAhead, u);
         }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void multiply(const char* left, int64_t left_rows, const char* right, int64_t right_rows, int32_t blocks, char* shared,
+                                         f32x16 (&acc)[T::R][T::C]) {
+    const int32_t lane = ld_lane(), wave = threadIdx.x / LD_WAVE;
+    const int32_t row = wave / T::ACROSS * (T::SIDE / T::DOWN) + (lane & 31), col = wave % T::ACROSS * (T::SIDE / T::ACROSS) + (lane & 31);
+    const int64_t left_step = left_rows * kMuonRowBytes, right_step = right_rows * kMuonRowBytes;
+    const auto fetch_stage = [&](int32_t k, char* to) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            half8 a[N][2], b[N][2];
+        for (int b = 0; b < T::BLOCKS; ++b)
+            if (k + b < blocks) {
+                fetch<T>(left + (k + b) * left_step, to + 2 * b * T::BLOCK_BYTES);
+                fetch<T>(right + (k + b) * right_step, to + (2 * b + 1) * T::BLOCK_BYTES);
+            }
+    };
+    if constexpr (T::BLOCKS == 0) {
+        multiply_alone<T>(left, left_rows, right, right_rows, blocks, acc);
+        return;
+    }
+    fetch_stage(0, shared);
+    __syncthreads();
+    int32_t stage = 0;
+    for (int32_t k = 0; k < blocks; k += T::BLOCKS ? T::BLOCKS : 1) {
+        char* now = shared + stage * T::STAGE_BYTES;
+        stage ^= 1;
+        if (k + T::BLOCKS < blocks) fetch_stage(k + T::BLOCKS, shared + stage * T::STAGE_BYTES);
+        const int32_t held = T::BLOCKS == 1 ? 1 : blocks - k < T::BLOCKS ? blocks - k : T::BLOCKS;
+        for (int32_t b = 0; b < held; ++b, now += 2 * T::BLOCK_BYTES) {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
+            for (int s = 0; s < 2; ++s) {
+                half8 x[T::R][2], y[T::C][2];
 #pragma unroll
                 for (int l = 0; l < 2; ++l) {
-                    a[i][l] = fragment(now, row + 32 * i, 4 * l + 2 * s + (lane >> 5));
-                    b[i][l] = fragment(now + kBytes, col + 32 * i, 4 * l + 2 * s + (lane >> 5));
-                }
 #pragma unroll
-            for (int i = 0; i < N; ++i)
+                    for (int i = 0; i < T::R; ++i) x[i][l] = fragment(now, row + 32 * i, 4 * l + 2 * s + (lane >> 5));
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][1], b[j][0], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][1], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][0], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < T::C; ++j) y[j][l] = fragment(now + T::BLOCK_BYTES, col + 32 * j, 4 * l + 2 * s + (lane >> 5));
                 }
+                // lower halves first; one after another for every sum, whatever the tile
+#pragma unroll
+                for (int l = 0; l < 3; ++l)
+#pragma unroll
+                    for (int i = 0; i < T::R; ++i)
+#pragma unroll
+                        for (int j = 0; j < T::C; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][l == 0], y[j][l == 1], acc[i][j], 0, 0, 0);
+            }
         }
         __syncthreads();
     }
 }
 
-template <int TILE> constexpr int tile_stride() { return TILE + 4; }  // floats from a row to the next of a tile in shared memory
-template <int TILE> constexpr int shared_bytes() {
-    constexpr int operands = 4 * TILE * static_cast<int>(kMuonRowBytes), tile = TILE * tile_stride<TILE>() * 4;
-    return operands > tile ? operands : tile;
-}
-
-// The sums, times `inv`, as rows of 32-bit values in shared memory.
-template <int TILE>
-__device__ __forceinline__ void lay_out(const f32x16 (&acc)[TILE / 64][TILE / 64], float inv, float* tile) {
-    const int32_t lane = ld_lane(), wave = threadIdx.x / LD_WAVE;
+// The sums of the `part`-th T::ROWS rows, times `inv`, as rows of 32-bit values in shared memory.
+template <typename T>
+__device__ __forceinline__ void lay_out(const f32x16 (&acc)[T::R][T::C], int32_t part, float inv, float* sums, int32_t stride = T::STRIDE) {
+    const int32_t lane = ld_lane(), wave = threadIdx.x / LD_WAVE, first = wave / T::ACROSS * (T::SIDE / T::DOWN);
+    if (part > 0) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < TILE / 64; ++i)
+    for (int i = 0; i < T::R; ++i) {
+        if ((first + 32 * i) / T::ROWS != part) continue;
 #pragma unroll
-        for (int j = 0; j < TILE / 64; ++j)
+        for (int j = 0; j < T::C; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) {
-                const int32_t r = (wave >> 1) * (TILE / 2) + 32 * i + (q & 3) + 8 * (q >> 2) + 4 * (lane >> 5);
-                const int32_t c = (wave & 1) * (TILE / 2) + 32 * j + (lane & 31);
-                tile[r * tile_stride<TILE>() + c] = acc[i][j][q] * inv;
+                const int32_t r = (first + 32 * i) % T::ROWS + (q & 3) + 8 * (q >> 2) + 4 * (lane >> 5);
+                const int32_t c = wave % T::ACROSS * (T::SIDE / T::ACROSS) + 32 * j + (lane & 31);
+                sums[r * stride + c] = acc[i][j][q] * inv;
             }
+    }
     __syncthreads();
 }
 
@@ -189,27 +251,27 @@ __device__ __forceinline__ int32_t problem_of(const Batch& b, int32_t& tile) {
     return lo;
 }
 
-template <int TILE>
-__global__ __launch_bounds__(kThreads, 2) void k_symmetric(Batch batch, Plan a) {
-    __shared__ __attribute__((aligned(16))) char shared[shared_bytes<TILE>()];
+template <typename T>
+__global__ __launch_bounds__(T::THREADS, T::WAVES) void k_symmetric(Batch batch, Plans plans) {
+    __shared__ __attribute__((aligned(16))) char shared[T::SHARED];
     int32_t tile = blockIdx.x;
-    const int32_t tiles = batch.first[batch.count], second = tile >= tiles;
-    if (second) tile -= tiles;
     const int32_t i = problem_of(batch, tile);
+    const Plan a = plans.of[batch.kind[i]];
+    const int32_t side = tiles_of(padded(batch.m[i]), T::SIDE), tiles = side * (side + 1) / 2, second = tile >= tiles;
+    if (second) tile -= tiles;
     const Product prod = a.prod[second];
     const float scale = a.scale[second];
     // row by row of the lower triangle
     int32_t tr = static_cast<int32_t>((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
     while (tr * (tr + 1) / 2 > tile) --tr;
     while ((tr + 1) * (tr + 2) / 2 <= tile) ++tr;
-    const int32_t tc = tile - tr * (tr + 1) / 2, m = batch.m[i];
+    const int32_t tc = tile - tr * (tr + 1) / 2, m = batch.m[i], r0 = tr * T::SIDE, c0 = tc * T::SIDE;
     const int64_t rows = padded(m);
-    f32x16 acc[TILE / 64][TILE / 64] = {};
-    multiply<TILE>(buffer_of(batch, i, prod.left) + tr * TILE * kMuonRowBytes, rows, buffer_of(batch, i, prod.right) + tc * TILE * kMuonRowBytes, rows,
-                   static_cast<int32_t>((a.long_sum ? padded(batch.n[i]) : rows) / kMuonBlock), shared, acc);
+    f32x16 acc[T::R][T::C] = {};
+    multiply<T>(buffer_of(batch, i, prod.left) + r0 * kMuonRowBytes, rows, buffer_of(batch, i, prod.right) + c0 * kMuonRowBytes, rows,
+                static_cast<int32_t>((a.long_sum ? padded(batch.n[i]) : rows) / kMuonBlock), shared, acc);
     float* sums = reinterpret_cast<float*>(shared);
-    lay_out<TILE>(acc, a.inv, sums);
-    constexpr int S = tile_stride<TILE>(), kPieces = TILE / 8;
+    constexpr int S = T::STRIDE, kPieces = T::SIDE / 8;
     char* out = buffer_of(batch, i, prod.out);
     const char* gram = buffer_of(batch, i, prod.left);
     const auto keep = [&](f32x8 x, int32_t r, int32_t c) {  // eight columns from c on of row r, of the whole matrix
@@ -221,52 +283,82 @@ __global__ __launch_bounds__(kThreads, 2) void k_symmetric(Batch batch, Plan a) 
         }
         store_split(out, rows, r, c >> 3, x * scale);
     };
-    for (int32_t p = threadIdx.x; p < TILE * kPieces; p += kThreads) {
-        const int32_t r = p / kPieces, c = p % kPieces * 8;
-        if (tr * TILE + r >= rows || tc * TILE + c >= rows) continue;
-        f32x8 x;
+    // Only sums on and below the diagonal are kept, and mirrored, in squares of eight by eight. Four lanes write the halves of 32 columns
+    // of a row, which lie side by side, the next four those of the row behind it.
+    for (int32_t h = 0; h < T::SIDE / T::ROWS; ++h) {
+        lay_out<T>(acc, h, a.inv, sums);
+        const int32_t h0 = r0 + T::ROWS * h;
+        for (int32_t p = threadIdx.x; p < T::ROWS * kPieces; p += T::THREADS) {
+            const int32_t r = (p >> 2) % T::ROWS, c = (p >> 2) / T::ROWS * 32 + (p & 3) * 8, at = h0 + r - c0;  // at: the row's number among the columns
+            if (h0 + r >= rows || c0 + c >= rows || c > at) continue;
+            f32x8 x;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = sums[tr == tc && c + e > r ? (c + e) * S + r : r * S + c + e];
-        keep(x, tr * TILE + r, tc * TILE + c);
-    }
-    if (tr == tc) return;
-    for (int32_t p = threadIdx.x; p < TILE * kPieces; p += kThreads) {
-        const int32_t c = p % TILE, r = p / TILE * 8;  // mirrored: row c, columns from r on
-        if (tr * TILE + r >= rows || tc * TILE + c >= rows) continue;
-        f32x8 x;
+            for (int e = 0; e < 8; ++e) x[e] = sums[c + e > at ? (c + e - at + r) * S + at : r * S + c + e];
+            keep(x, h0 + r, c0 + c);
+        }
+        for (int32_t p = threadIdx.x; p < T::ROWS / 8 * T::SIDE; p += T::THREADS) {
+            const int32_t c = (p >> 2) % T::SIDE, r = (p >> 2) / T::SIDE * 32 + (p & 3) * 8;
+            if (h0 + r >= rows || c0 + c >= rows || (h0 + r) / 8 <= (c0 + c) / 8) continue;
+            f32x8 x;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = sums[(r + e) * S + c];
-        keep(x, tc * TILE + c, tr * TILE + r);
+            for (int e = 0; e < 8; ++e) x[e] = sums[(r + e) * S + c];
+            keep(x, c0 + c, h0 + r);
+        }
     }
 }
 
 // X' = Q X: kept both ways, or, the last, written where it goes. left: Q (m rows); right: X transposed (n rows).
-template <int TILE, bool FINAL, int OT>
-__global__ __launch_bounds__(kThreads, 2) void k_apply(Batch batch, Plan a, FinalArgs f) {
-    __shared__ __attribute__((aligned(16))) char shared[shared_bytes<TILE>()];
+template <typename T, bool FINAL, int OT>
+__global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Plans plans, FinalArgs f) {
+    __shared__ __attribute__((aligned(16))) char shared[T::SHARED];
     int32_t tile = blockIdx.x;
     const int32_t i = problem_of(batch, tile);
-    const int32_t m = batch.m[i], n = batch.n[i], down = (m + TILE - 1) / TILE;
-    const int32_t tc = tile / down, tr = tile % down;
+    const Plan a = plans.of[batch.kind[i]];
+    const int32_t m = batch.m[i], n = batch.n[i], down = tiles_of(padded(m), T::SIDE);
+    const int32_t r0 = tile % down * T::SIDE, c0 = tile / down * T::SIDE;
     const int64_t rows = padded(m), cols = padded(n);
-    f32x16 acc[TILE / 64][TILE / 64] = {};
-    multiply<TILE>(buffer_of(batch, i, a.prod[0].left) + tr * TILE * kMuonRowBytes, rows, buffer_of(batch, i, a.prod[0].right) + tc * TILE * kMuonRowBytes, cols,
-                   static_cast<int32_t>(rows / kMuonBlock), shared, acc);
+    f32x16 acc[T::R][T::C] = {};
+    multiply<T>(buffer_of(batch, i, a.prod[0].left) + r0 * kMuonRowBytes, rows, buffer_of(batch, i, a.prod[0].right) + c0 * kMuonRowBytes, cols,
+                static_cast<int32_t>(rows / kMuonBlock), shared, acc);
     float* sums = reinterpret_cast<float*>(shared);
-    lay_out<TILE>(acc, a.inv, sums);
-    constexpr int S = tile_stride<TILE>(), kPieces = TILE / 8;
+    constexpr int S = T::STRIDE, kPieces = T::SIDE / 8;
     typedef typename LdElem<OT>::type elem;
     elem* final_out = FINAL ? static_cast<elem*>(f.out[i]) : nullptr;
     const int64_t stride = FINAL ? f.stride[i] : 0;
     const auto write = [&](const f32x8& x, int32_t r, int32_t c, int32_t width) {
         elem* to = final_out + r * stride + c;
+        if (c + 8 <= width) {
+            if constexpr (OT == LD_F32) {
+                typedef typename LdVec<LD_F32, 4>::type half;
+                *reinterpret_cast<half*>(to) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
+                *reinterpret_cast<half*>(to + 4) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+            } else {
+                typedef LdVec<OT, 8> V;
+                *reinterpret_cast<typename V::type*>(to) = V::narrow(x);
+            }
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (c + e < width) to[e] = static_cast<elem>(x[e]);
     };
-    if (!FINAL || !batch.flipped[i]) {
-        for (int32_t p = threadIdx.x; p < TILE * kPieces; p += kThreads) {
-            const int32_t r = p / kPieces, c = p % kPieces * 8, ri = tr * TILE + r, ci = tc * TILE + c;
+    for (int32_t h = 0; h < T::SIDE / T::ROWS; ++h) {
+        if (FINAL && batch.flipped[i]) {
+            // an odd stride, and the lanes along the columns that are rows of the update: what they write lies side by side
+            constexpr int kOdd = T::SIDE + 1, kDeep = T::ROWS / 8;
+            lay_out<T>(acc, h, a.inv, sums, kOdd);
+            for (int32_t p = threadIdx.x; p < kDeep * T::SIDE; p += T::THREADS) {
+                const int32_t c = p / kDeep, r = p % kDeep * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
+                f32x8 x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = sums[(r + e) * kOdd + c];
+                if (ci < n) write(x, ci, ri, m);
+            }
+            continue;
+        }
+        lay_out<T>(acc, h, a.inv, sums);
+        for (int32_t p = threadIdx.x; p < T::ROWS * kPieces; p += T::THREADS) {
+            const int32_t r = FINAL ? p / kPieces : (p >> 2) % T::ROWS, c = FINAL ? p % kPieces * 8 : (p >> 2) / T::ROWS * 32 + (p & 3) * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
             f32x8 x;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = sums[r * S + c + e];
@@ -276,18 +368,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_apply(Batch batch, Plan a, Fina
                 store_split(buffer_of(batch, i, a.prod[0].out), rows, ri, ci >> 3, x * a.scale[0]);
             }
         }
-    }
-    if (!FINAL || batch.flipped[i]) {
-        for (int32_t p = threadIdx.x; p < TILE * kPieces; p += kThreads) {
-            const int32_t c = p % TILE, r = p / TILE * 8, ri = tr * TILE + r, ci = tc * TILE + c;
+        for (int32_t p = threadIdx.x; !FINAL && p < T::ROWS / 8 * T::SIDE; p += T::THREADS) {
+            const int32_t c = (p >> 2) % T::SIDE, r = (p >> 2) / T::SIDE * 32 + (p & 3) * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
             f32x8 x;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = sums[(r + e) * S + c];
-            if (FINAL) {
-                if (ci < n) write(x, ci, ri, m);
-            } else if (ri < rows && ci < cols) {
-                store_split(buffer_of(batch, i, a.prod[0].out_t), cols, ci, ri >> 3, x * a.scale[0]);
-            }
+            if (ri < rows && ci < cols) store_split(buffer_of(batch, i, a.prod[0].out_t), cols, ci, ri >> 3, x * a.scale[0]);
         }
     }
 }
@@ -319,21 +405,49 @@ __host__ __device__ __forceinline__ int32_t sum_parts(int64_t elems) {
     return static_cast<int32_t>(parts < kSumParts ? parts : kSumParts);
 }
 
+// Threads of a row, a power of two, when each takes eight elements side by side at a time.
+__device__ __forceinline__ int32_t lanes_log2_of(int32_t cols) {
+    int32_t lanes_log2 = 0;
+    while (lanes_log2 < 8 && (8 << lanes_log2) < cols) ++lanes_log2;
+    return lanes_log2;
+}
+// Up to eight elements from p on, zeros behind them.
+template <int DT>
+__device__ __forceinline__ f32x8 load_eight(const typename LdElem<DT>::type* p, int32_t n) {
+    f32x8 x;
+    if (n >= 8) {
+        if constexpr (DT == LD_F32) {
+            typedef typename LdVec<LD_F32, 4>::type half;
+            const half lo = *reinterpret_cast<const half*>(p), hi = *reinterpret_cast<const half*>(p + 4);
+            x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            typedef LdVec<DT, 8> V;
+            x = V::widen(*reinterpret_cast<const typename V::type*>(p));
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e < n ? static_cast<float>(p[e]) : 0.0f;
+    }
+    return x;
+}
+
 template <int DT>
 __global__ __launch_bounds__(kThreads) void k_squares(Batch b, Source s) {
     __shared__ double sh[kThreads / LD_WAVE];
     typedef typename LdElem<DT>::type elem;
     const int32_t i = blockIdx.y, rows = user_rows(b, i), cols = user_cols(b, i);
-    const int64_t elems = static_cast<int64_t>(rows) * cols;
-    const int32_t parts = sum_parts(elems);
+    const int32_t parts = sum_parts(static_cast<int64_t>(rows) * cols);
     if (static_cast<int32_t>(blockIdx.x) >= parts) return;
     const elem* src = static_cast<const elem*>(s.src[i]);
     const int64_t stride = s.stride[i];
+    const int32_t lanes_log2 = lanes_log2_of(cols), lanes = 1 << lanes_log2, at_once = kThreads >> lanes_log2;
     double sum = 0.0;
-    for (int64_t e = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; e < elems; e += static_cast<int64_t>(parts) * kThreads) {
-        const double x = static_cast<double>(static_cast<float>(src[e / cols * stride + e % cols]));
-        sum = fma(x, x, sum);
-    }
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * at_once + (threadIdx.x >> lanes_log2); r < rows; r += static_cast<int64_t>(parts) * at_once)
+        for (int32_t c = (threadIdx.x & (lanes - 1)) * 8; c < cols; c += lanes * 8) {
+            const f32x8 x = load_eight<DT>(src + r * stride + c, cols - c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fma(static_cast<double>(x[e]), static_cast<double>(x[e]), sum);
+        }
     sum = block_sum(sum, sh);
     if (threadIdx.x == 0) s.sums[i * kSumParts + blockIdx.x] = sum;
 }
@@ -373,6 +487,18 @@ __global__ __launch_bounds__(kThreads) void k_lay_out(Batch b, Source s, float s
     }
 }
 
+__device__ __forceinline__ void store_eight(float* p, const f32x8& x, int32_t n) {
+    typedef typename LdVec<LD_F32, 4>::type half;
+    if (n >= 8) {
+        *reinterpret_cast<half*>(p) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
+        *reinterpret_cast<half*>(p + 4) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[e] = x[e];
+    }
+}
+
 // Momentum of a window's steps, one after another, and every step's update and the sum of its squares.
 struct MomentumArgs {
     float* momentum[kMost];
@@ -392,16 +518,23 @@ __global__ __launch_bounds__(kThreads) void k_momentum(Batch b, MomentumArgs a) 
     const int32_t parts = sum_parts(elems);
     if (static_cast<int32_t>(blockIdx.x) >= parts) return;
     float* momentum = a.momentum[blockIdx.y];
-    const int64_t from = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x, step = static_cast<int64_t>(parts) * kThreads;
+    const int64_t from = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 8, step = static_cast<int64_t>(parts) * kThreads * 8;
     for (int32_t t = 0; t < steps; ++t) {
         const elem* grad = static_cast<const elem*>(a.grad[p0 + t]);
         float* update = reinterpret_cast<float*>(buffer_of(b, p0 + t, kYT));
         double sum = 0.0;
         for (int64_t e = from; e < elems; e += step) {
-            const float g = static_cast<float>(grad[e]), m = __fmaf_rn(a.mu, momentum[e], g), u = a.nesterov ? __fmaf_rn(a.mu, m, g) : m;
-            momentum[e] = m;
-            update[e] = u;
-            sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
+            const int32_t n = elems - e < 8 ? static_cast<int32_t>(elems - e) : 8;
+            const f32x8 g = load_eight<DT>(grad + e, n);
+            f32x8 m = load_eight<LD_F32>(momentum + e, n), u;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                m[k] = __fmaf_rn(a.mu, m[k], g[k]);
+                u[k] = a.nesterov ? __fmaf_rn(a.mu, m[k], g[k]) : m[k];
+                if (k < n) sum = fma(static_cast<double>(u[k]), static_cast<double>(u[k]), sum);
+            }
+            store_eight(momentum + e, m, n);
+            store_eight(update + e, u, n);
         }
         sum = block_sum(sum, sh);
         if (threadIdx.x == 0) a.sums[(p0 + t) * kSumParts + blockIdx.x] = sum;
@@ -418,10 +551,15 @@ __global__ __launch_bounds__(kThreads) void k_update(Batch b, UpdateArgs a) {
     const int32_t p0 = a.problem[blockIdx.y], steps = a.steps[blockIdx.y];
     const int64_t elems = static_cast<int64_t>(b.m[p0]) * b.n[p0];
     float* w = a.w[blockIdx.y];
-    for (int64_t e = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; e < elems; e += static_cast<int64_t>(gridDim.x) * kThreads) {
-        float x = w[e];
-        for (int32_t t = 0; t < steps; ++t) x = __fmaf_rn(-a.rate[blockIdx.y], reinterpret_cast<const float*>(buffer_of(b, p0 + t, kX))[e], x * a.keep);
-        w[e] = x;
+    for (int64_t e = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 8; e < elems; e += static_cast<int64_t>(gridDim.x) * kThreads * 8) {
+        const int32_t n = elems - e < 8 ? static_cast<int32_t>(elems - e) : 8;
+        f32x8 x = load_eight<LD_F32>(w + e, n);
+        for (int32_t t = 0; t < steps; ++t) {
+            const f32x8 o = load_eight<LD_F32>(reinterpret_cast<const float*>(buffer_of(b, p0 + t, kX)) + e, n);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = __fmaf_rn(-a.rate[blockIdx.y], o[k], x[k] * a.keep);
+        }
+        store_eight(w + e, x, n);
     }
 }
 
@@ -460,12 +598,13 @@ int64_t scratch_of(int64_t rows, int64_t cols) {
 }
 
 // Appends a problem; whether it still has room. The first always has.
-bool append(Batch& b, int64_t& used, char* scratch, int64_t rows, int64_t cols) {
+bool append(Batch& b, int64_t& used, char* scratch, int64_t room, int64_t rows, int64_t cols) {
     const int64_t need = scratch_of(rows, cols);
-    if (b.count == kMost || (b.count > 0 && used + need > kGroupBytes)) return false;
+    if (b.count == kMost || (b.count > 0 && used + need > room)) return false;
     const int32_t i = b.count++;
     b.base[i] = scratch + used;
     b.flipped[i] = rows > cols;
+    b.kind[i] = ld_muon_kind(rows > cols ? cols : rows, rows > cols ? rows : cols);
     b.m[i] = static_cast<int32_t>(rows > cols ? cols : rows);
     b.n[i] = static_cast<int32_t>(rows > cols ? rows : cols);
     used += need;
@@ -473,11 +612,13 @@ bool append(Batch& b, int64_t& used, char* scratch, int64_t rows, int64_t cols) 
 }
 
 // Bytes of the largest group of `repeats` problems of every matrix in turn; a group begins anew wherever one is full.
-size_t workspace_of(const int64_t* rows, const int64_t* cols, int32_t n, int64_t repeats) {
+size_t workspace_of(const int64_t* rows, const int64_t* cols, int32_t n, int64_t repeats, size_t* least = nullptr) {
+    if (least) *least = 0;
     int64_t most = 0, used = 0, count = 0;  // of the group that is filled
     for (int32_t i = 0; i < n; ++i) {
         if (rows[i] == 0 || cols[i] == 0) continue;
         const int64_t need = scratch_of(rows[i], cols[i]);
+        if (least && repeats > 0 && static_cast<size_t>(kSumBytes + need) > *least) *least = static_cast<size_t>(kSumBytes + need);
         const auto room = [&]() {
             const int64_t fit = (kGroupBytes - used) / need;
             return count == 0 && fit < 1 ? 1 : fit < kMost - count ? fit : kMost - count;
@@ -498,15 +639,16 @@ size_t workspace_of(const int64_t* rows, const int64_t* cols, int32_t n, int64_t
     return most == 0 ? 0 : static_cast<size_t>(kSumBytes + most);
 }
 
-int32_t tiles_of(int64_t side, int32_t tile) { return static_cast<int32_t>((side + tile - 1) / tile); }
+typedef Tile<32, 1, 1, 0> Least;
+typedef Tile<64, 2, 2, 4> Small;
+typedef Tile<128, 2, 2, 1> Middle;
+typedef Tile<256, 2, 4, 1> Large;
 
-constexpr int32_t kTile = 128;
-
-void program_of(const Polynomial& p, bool wide, Program& out) {
+void program_of(const Polynomial& p, int32_t kind, Program& out) {
     const auto scale = [](double bound) { return ld_muon_scale(bound); };
     const LdMuonBounds& b = p.bounds;
     int32_t begin[kMuonMaxSteps + 1];
-    const int32_t runs = ld_muon_runs(b, p.steps, wide, begin);
+    const int32_t runs = ld_muon_runs(b, p.steps, kind, begin);
     int32_t xt = kXT, other = kYT;
     out.count = 0;
     for (int32_t run = 0; run < runs; ++run) {
@@ -564,35 +706,66 @@ void program_of(const Polynomial& p, bool wide, Program& out) {
     }
 }
 
-// All steps of a group whose X is laid out. Wide matrices and others go through launches of their own from where their programs differ.
+// All steps of a group whose X is laid out. Matrices of different kinds go through their programs side by side, a launch for all whose next is of
+// a sort: first those that multiply X, then those that are symmetric; who comes to the last first waits.
 ld_status run_steps(Batch& b, const Polynomial& p, const FinalArgs& out, int32_t out_type, hipStream_t s) {
-    bool any[2] = {false, false};
-    for (int32_t i = 0; i < b.count; ++i) any[ld_muon_wide(b.m[i], b.n[i])] = true;
-    Program prog[2];
-    for (int32_t w = 0; w < 2; ++w) program_of(p, w == 1, prog[w]);
-    const auto launch = [&](const Plan& a, bool with_wide, bool with_others) {
+    Program prog[kMuonKinds];
+    int32_t at[kMuonKinds] = {};
+    for (int32_t k = 0; k < kMuonKinds; ++k) prog[k].count = 0;
+    for (int32_t i = 0; i < b.count; ++i)
+        if (prog[b.kind[i]].count == 0) program_of(p, b.kind[i], prog[b.kind[i]]);
+    const auto launch_as = [&](auto tile, const Plans& a) {
+        typedef decltype(tile) T;
+        bool apply = false, final = false;
+        for (const Plan& plan : a.of) apply |= plan.apply != 0, final |= plan.final != 0;
         int32_t tiles = 0;
         for (int32_t i = 0; i < b.count; ++i) {
             b.first[i] = tiles;
-            if (!(ld_muon_wide(b.m[i], b.n[i]) ? with_wide : with_others)) continue;
-            const int32_t down = tiles_of(b.m[i], kTile), across = tiles_of(b.n[i], kTile);
-            tiles += a.apply ? down * across : down * (down + 1) / 2;
+            const int32_t down = tiles_of(ld_muon_padded(b.m[i]), T::SIDE), across = tiles_of(ld_muon_padded(b.n[i]), T::SIDE);
+            tiles += a.of[b.kind[i]].products * (apply ? down * across : down * (down + 1) / 2);
         }
         for (int32_t i = b.count; i <= kMost; ++i) b.first[i] = tiles;
-        const dim3 grid(tiles * a.products);
-        if (!a.apply) k_symmetric<kTile><<<grid, dim3(kThreads), 0, s>>>(b, a);
-        else if (a.final) ld_with_type(out_type, [&](auto type) { k_apply<kTile, true, type><<<grid, dim3(kThreads), 0, s>>>(b, a, out); });
-        else k_apply<kTile, false, LD_F32><<<grid, dim3(kThreads), 0, s>>>(b, a, out);
+        const dim3 grid(tiles), threads(T::THREADS);
+        if (!apply) k_symmetric<T><<<grid, threads, 0, s>>>(b, a);
+        else if (final) ld_with_type(out_type, [&](auto type) { k_apply<T, true, type><<<grid, threads, 0, s>>>(b, a, out); });
+        else k_apply<T, false, LD_F32><<<grid, threads, 0, s>>>(b, a, out);
         return ld_launch_status();
     };
-    int32_t at = 0;
-    if (any[0] && any[1])
-        for (; at < prog[0].count && at < prog[1].count && memcmp(&prog[0].plan[at], &prog[1].plan[at], sizeof(Plan)) == 0; ++at)
-            if (launch(prog[0].plan[at], true, true) != LD_OK) return LD_ERR_HIP;
-    for (int32_t w = 0; w < 2; ++w)
-        for (int32_t k = at; any[w] && k < prog[w].count; ++k)
-            if (launch(prog[w].plan[k], w == 1, w == 0) != LD_OK) return LD_ERR_HIP;
-    return LD_OK;
+    // Which tile: the one that is done first, by what blocks of 32 columns take a CU (ns) with each, as measured. 256: a tile at a time;
+    // 128: two, or one, at a time; 64: one; 32: eight at a time, of which few wait on memory alone.
+    const auto launch = [&](const Plans& a) {
+        bool apply = false;
+        for (const Plan& plan : a.of) apply |= plan.apply != 0;
+        const int32_t sides[4] = {32, 64, 128, 256};
+        double best = 0.0;
+        int32_t side = 0;
+        for (int32_t k = 0; k < 4; ++k) {
+            double tiles = 0.0, blocks = 0.0;
+            for (int32_t i = 0; i < b.count; ++i) {
+                const Plan& plan = a.of[b.kind[i]];
+                const int32_t down = tiles_of(ld_muon_padded(b.m[i]), sides[k]), across = tiles_of(ld_muon_padded(b.n[i]), sides[k]);
+                const double mine = static_cast<double>(plan.products) * (apply ? static_cast<double>(down) * across : 0.5 * down * (down + 1.0));
+                tiles += mine, blocks += mine * (ld_muon_padded(plan.long_sum ? b.n[i] : b.m[i]) / kMuonBlock);
+            }
+            const double each = blocks / tiles, rounds = ceil(tiles / kCUs), pairs = floor(rounds / 2.0);
+            const double time = sides[k] == 256 ? 20000.0 + each * 2700.0 * rounds
+                                : sides[k] == 128 ? 10000.0 + each * (1600.0 * pairs + 900.0 * (rounds - 2.0 * pairs))
+                                : sides[k] == 64 ? 5000.0 + each * 400.0 * rounds : 4000.0 + each * fmax(200.0, 220.0 * rounds);
+            if (k == 0 || time < best) best = time, side = sides[k];
+        }
+        return side == 256 ? launch_as(Large(), a) : side == 128 ? launch_as(Middle(), a) : side == 64 ? launch_as(Small(), a) : launch_as(Least(), a);
+    };
+    for (;;) {
+        const auto sort_of = [](const Plan& plan) { return plan.final ? 0 : plan.apply ? 2 : 1; };
+        int32_t sort = -1;
+        for (int32_t k = 0; k < kMuonKinds; ++k)
+            if (at[k] < prog[k].count && sort_of(prog[k].plan[at[k]]) > sort) sort = sort_of(prog[k].plan[at[k]]);
+        if (sort < 0) return LD_OK;
+        Plans plans = {};
+        for (int32_t k = 0; k < kMuonKinds; ++k)
+            if (at[k] < prog[k].count && sort_of(prog[k].plan[at[k]]) == sort) plans.of[k] = prog[k].plan[at[k]++];
+        if (launch(plans) != LD_OK) return LD_ERR_HIP;
+    }
 }
 
 int32_t most_parts(const Batch& b) {
@@ -638,12 +811,13 @@ extern "C" ld_status ld_orthogonalize(const void* const* src, const int64_t* src
         if (!src[i] || !dst[i]) return LD_ERR_NULL;
         if (!ld_aligned(src[i], ld_type_bytes(dtype)) || !ld_aligned(dst[i], ld_type_bytes(out_dtype))) return LD_ERR_ALIGN;
     }
-    const size_t need = workspace_of(rows, cols, n_mats, 1);
-    if (need == 0) return LD_OK;
+    size_t need;  // of one problem at a time
+    if (workspace_of(rows, cols, n_mats, 1, &need) == 0) return LD_OK;
     if (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < need) return LD_ERR_WORKSPACE;
     ld_begin_call();
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* scratch = static_cast<char*>(workspace) + kSumBytes;
+    const int64_t room_bytes = static_cast<int64_t>(workspace_bytes < (static_cast<size_t>(1) << 62) ? workspace_bytes : static_cast<size_t>(1) << 62) - kSumBytes;
     for (int32_t i = 0; i < n_mats;) {
         Batch b = {};
         Source source = {};
@@ -651,7 +825,7 @@ extern "C" ld_status ld_orthogonalize(const void* const* src, const int64_t* src
         int64_t used = 0;
         for (; i < n_mats; ++i) {
             if (rows[i] == 0 || cols[i] == 0) continue;
-            if (!append(b, used, scratch, rows[i], cols[i])) break;
+            if (!append(b, used, scratch, room_bytes, rows[i], cols[i])) break;
             source.src[b.count - 1] = src[i], source.stride[b.count - 1] = src_stride ? src_stride[i] : cols[i];
             out.out[b.count - 1] = dst[i], out.stride[b.count - 1] = dst_stride ? dst_stride[i] : cols[i];
         }
@@ -691,12 +865,13 @@ extern "C" ld_status ld_merge_dense_muon(float* const* w, float* const* m, const
             if (!ld_aligned(g, ld_type_bytes(dtype))) return LD_ERR_ALIGN;
         }
     }
-    const size_t need = workspace_of(rows, cols, n_mats, W);
-    if (need == 0) return LD_OK;
+    size_t need;  // of one problem at a time
+    if (workspace_of(rows, cols, n_mats, W, &need) == 0) return LD_OK;
     if (!workspace || !ld_aligned(workspace, 256) || workspace_bytes < need) return LD_ERR_WORKSPACE;
     ld_begin_call();
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* scratch = static_cast<char*>(workspace) + kSumBytes;
+    const int64_t room_bytes = static_cast<int64_t>(workspace_bytes < (static_cast<size_t>(1) << 62) ? workspace_bytes : static_cast<size_t>(1) << 62) - kSumBytes;
     int32_t i = 0, t = 0;  // the next problem
     while (i < n_mats) {
         Batch b = {};
@@ -712,7 +887,7 @@ extern "C" ld_status ld_merge_dense_muon(float* const* w, float* const* m, const
                 continue;
             }
             const int32_t from = t;
-            for (; t < W && (room = append(b, used, scratch, rows[i], cols[i])); ++t) {
+            for (; t < W && (room = append(b, used, scratch, room_bytes, rows[i], cols[i])); ++t) {
                 const int32_t k = b.count - 1;
                 mom.grad[k] = grad[static_cast<int64_t>(t) * n_mats + i];
                 source.stride[k] = out.stride[k] = cols[i];
@@ -738,7 +913,7 @@ extern "C" ld_status ld_merge_dense_muon(float* const* w, float* const* m, const
         const dim3 grid(most_parts(b), mats);
         ld_with_type(dtype, [&](auto type) { k_momentum<type><<<grid, dim3(kThreads), 0, s>>>(b, mom); });
         if (ld_launch_status() != LD_OK || lay_out_group(b, source, LD_F32, p, s) != LD_OK || run_steps(b, p, out, LD_F32, s) != LD_OK) return LD_ERR_HIP;
-        k_update<<<dim3(2 * most_parts(b), mats), dim3(kThreads), 0, s>>>(b, up);
+        k_update<<<dim3(4 * most_parts(b), mats), dim3(kThreads), 0, s>>>(b, up);
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
     }
     return LD_OK;

@@ -54,15 +54,18 @@ inline bool ld_muon_bounds(LdMuonBounds& m, int32_t steps, const float* coeff) {
 
 // A run of steps works on one Gram matrix; X is multiplied by what they amount to, and its Gram matrix formed anew, between runs. The
 // Gram matrix loses directions of small singular values, the more the further a run grows them (each usual step 3.4 times), and
-// a matrix that is about square has more of those than a wide one. So a run ends at three steps or 48 times for wide matrices,
-// counted from the last step on, and at two steps or 16 times for others, counted from the first: 2 + 3 and 2 + 2 + 1 of five usual
-// ones. Errors against 64 bits (relative, Frobenius), of products in 32 bits in the order of the formula, 2 + 3 and 2 + 2 + 1: 768 x
-// 768 1.6e-6, 4.2e-6, 2.1e-6; 333 x 1001 1.9e-6, 1.9e-6, 2.0e-6. In products' operations 2 + 3 is 6 m^2 n + 14 m^3, 2 + 2 + 1
-// 9 m^2 n + 11 m^3: as much for square matrices.
-inline bool ld_muon_wide(int64_t m, int64_t n) { return 2 * n >= 5 * m; }
+// a matrix that is about square has more of those than a wide one. So a run of a wide matrix (kind 2) ends at three steps or 48 times,
+// counted from the last step on, of a less wide one (1) at two steps or 16 times, counted from the first, and one that is about square
+// (0), to which a run's matrices of m x m are no smaller than X, has runs of one step: 2 + 3, 2 + 2 + 1 and five times 1 of five usual
+// steps. Errors against 64 bits (relative, Frobenius) of products in 32 bits in the order of the formula, 2 + 3, 2 + 2 + 1 and 1s:
+// 768 x 768 1.6e-6, 4.2e-6, 2.1e-6, 1.8e-6; 333 x 1001 1.9e-6, 1.9e-6, 2.0e-6, 1.7e-6. In products' operations they are
+// 6 m^2 n + 14 m^3, 9 m^2 n + 11 m^3 and 15 m^2 n + 5 m^3, in launches, of which a small call's time is made, 17, 18 and 15.
+constexpr int32_t kMuonKinds = 3;
+inline int32_t ld_muon_kind(int64_t m, int64_t n) { return 2 * n >= 5 * m ? 2 : 4 * n >= 5 * m ? 1 : 0; }
 // First steps of the runs, and behind them the number of steps; returns the number of runs.
-inline int32_t ld_muon_runs(const LdMuonBounds& b, int32_t steps, bool wide, int32_t* begin) {
-    const int32_t longest = wide ? 3 : 2;
+inline int32_t ld_muon_runs(const LdMuonBounds& b, int32_t steps, int32_t kind, int32_t* begin) {
+    const bool wide = kind == 2;
+    const int32_t longest = kind + 1;
     const double most = wide ? 48.0 : 16.0;
     int32_t runs = 0, length = 0;
     double grown = 1.0;

@@ -52,20 +52,22 @@ def orthogonal64(u, steps=5, coeffs=None, eps=1e-7):
     return x.t().contiguous() if flip else x
 
 
-def runs_of(coeffs, wide):
-    """Numbers of steps that go by one Gram matrix: up to three or a growth of 48, from the last, of wide matrices, else two or 16."""
-    top, grows, longest, most = 1.0, [], 3 if wide else 2, 48 if wide else 16
+def runs_of(coeffs, m, n):
+    """Numbers of steps that go by one Gram matrix: up to three or a growth of 48, counted from the last, of wide matrices, two or 16 of
+    less wide ones, and one of those that are about square."""
+    kind = 2 if 2 * n >= 5 * m else 1 if 4 * n >= 5 * m else 0
+    top, grows, longest, most = 1.0, [], kind + 1, 48 if kind == 2 else 16
     for a, b, c in coeffs:
         x = np.linspace(0, top, 10001)
         f = a + b * x ** 2 + c * x ** 4
         grows.append(float(np.abs(f).max()))
         top = float(np.abs(x * f).max())
     runs, grown = [], 0.0
-    for g in grows[::-1] if wide else grows:
+    for g in grows[::-1] if kind == 2 else grows:
         if not runs or runs[-1] == longest or grown * g > most:
             runs, grown = runs + [0], 1.0
         runs[-1], grown = runs[-1] + 1, grown * g
-    return runs[::-1] if wide else runs
+    return runs[::-1] if kind == 2 else runs
 
 
 def noisy(u, seed, steps=5, coeffs=None, eps=1e-7, source=0.0):
@@ -91,7 +93,7 @@ def noisy(u, seed, steps=5, coeffs=None, eps=1e-7, source=0.0):
     flip = x.shape[0] > x.shape[1]
     x = x.t().contiguous() if flip else x
     c, s = coefficients(coeffs, steps), 0
-    for n in runs_of(c, 2 * x.shape[1] >= 5 * x.shape[0]):
+    for n in runs_of(c, *x.shape):
         A, q = symmetric(product(x, x)), None
         for k in range(n):
             ca, cb, cc = c[s]
@@ -139,7 +141,7 @@ def test_shapes(r, c):
 
 
 @pytest.mark.parametrize("kind", ["plain", "heavy", "low rank", "lower rank", "rank 3"])
-@pytest.mark.parametrize("r,c", [(96, 700), (300, 200)])
+@pytest.mark.parametrize("r,c", [(96, 700), (300, 200), (260, 260)])
 def test_spectra(r, c, kind):
     print(f"[orthogonalize] {r} x {c} {kind}", flush=True)
     u = matrix(r, c, gen(3), kind).to(F32)
@@ -156,10 +158,12 @@ def test_types(dtype, out_dtype):
 
 @pytest.mark.parametrize("steps", range(1, 17))
 def test_steps(steps):
-    u = matrix(90, 140, gen(steps)).to(F32)
     gentle = (1.5, -0.5, 0.0)
-    check(ld.ld_orthogonalize([u], steps=steps)[0], u, steps, steps=steps)
-    check(ld.ld_orthogonalize([u], steps=steps, coeffs=gentle)[0], u, (steps, gentle), steps=steps, coeffs=gentle)
+    us = [matrix(*s, gen(steps)).to(F32) for s in ((90, 140), (140, 140), (300, 100))]  # a matrix of every kind, side by side
+    for coeffs in (None, gentle):
+        for o, u in zip(ld.ld_orthogonalize(us, steps=steps, coeffs=coeffs), us):
+            check(o, u, (steps, coeffs, u.shape), steps=steps, coeffs=coeffs)
+            assert same_bits(ld.ld_orthogonalize([u], steps=steps, coeffs=coeffs)[0], o)
 
 
 def test_coefficients_of_every_step():
@@ -226,8 +230,10 @@ def test_workspace_holds_anything_on_entry():
     u = [matrix(130, 257, gen(15)).to(F32), matrix(65, 20, gen(16)).to(F32)]
     want = ld.ld_orthogonalize(u)
     need = ld.ld_orthogonalize_workspace([t.shape for t in u])
-    for fill in (0, 255, 0x7C):
-        ws = torch.full((need,), fill, dtype=torch.uint8, device=DEV)
+    least = max(ld.ld_orthogonalize_workspace([t.shape]) for t in u)
+    assert least < need
+    for fill, size in ((0, need), (255, need), (0x7C, least), (255, need - 1)):  # with less, one matrix after another
+        ws = torch.full((size,), fill, dtype=torch.uint8, device=DEV)
         for a, b in zip(ld.ld_orthogonalize(u, workspace=ws), want):
             assert same_bits(a, b)
 

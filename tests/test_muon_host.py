@@ -21,10 +21,10 @@ SHIM = """
 extern "C" {
 double largest(double a, double b, double c, double top, int32_t odd) { return ld_muon_largest(a, b, c, top, odd); }
 // begin: first steps of the runs, then their end
-int32_t bounds(int32_t steps, const float* coeff, int32_t wide, double* x, double* p, double* r, double* q, int32_t* begin, int32_t* runs) {
+int32_t bounds(int32_t steps, const float* coeff, int32_t kind, double* x, double* p, double* r, double* q, int32_t* begin, int32_t* runs) {
     LdMuonBounds m = {};
     if (!ld_muon_bounds(m, steps, coeff)) return 0;
-    *runs = ld_muon_runs(m, steps, wide != 0, begin);
+    *runs = ld_muon_runs(m, steps, kind, begin);
     x[0] = m.x[0];
     for (int32_t run = 0, s = 0; s < steps; ++s) {
         if (s == begin[run + 1]) ++run;
@@ -32,6 +32,7 @@ int32_t bounds(int32_t steps, const float* coeff, int32_t wide, double* x, doubl
     }
     return 1;
 }
+int32_t kind(int64_t m, int64_t n) { return ld_muon_kind(m, n); }
 float scale(double bound) { return ld_muon_scale(bound); }
 int64_t scratch(int32_t m, int32_t n) { return ld_muon_scratch(m, n); }
 }
@@ -59,10 +60,10 @@ def _p(a):
     return V(a.ctypes.data)
 
 
-def bounds(shim, steps, coeff, wide):
+def bounds(shim, steps, coeff, kind):
     x, p, r, q = (np.zeros(17) for _ in range(4))
     begin, runs = np.zeros(18, np.int32), np.zeros(1, np.int32)
-    ok = shim.bounds(steps, _p(coeff), int(wide), _p(x), _p(p), _p(r), _p(q), _p(begin), _p(runs))
+    ok = shim.bounds(steps, _p(coeff), int(kind), _p(x), _p(p), _p(r), _p(q), _p(begin), _p(runs))
     return (x, p, r, q, begin[:runs[0] + 1].tolist()) if ok else None
 
 
@@ -71,10 +72,13 @@ def usual(steps):
 
 
 def test_runs_of_the_usual_steps(shim):
-    for wide, want in ((True, {1: [0], 2: [0], 3: [0], 4: [0, 1], 5: [0, 2], 6: [0, 3], 7: [0, 1, 4], 16: [0, 1, 4, 7, 10, 13]}),
-                       (False, {1: [0], 2: [0], 3: [0, 2], 4: [0, 2], 5: [0, 2, 4], 16: list(range(0, 16, 2))})):
+    for kind, want in ((2, {1: [0], 2: [0], 3: [0], 4: [0, 1], 5: [0, 2], 6: [0, 3], 7: [0, 1, 4], 16: [0, 1, 4, 7, 10, 13]}),
+                       (1, {1: [0], 2: [0], 3: [0, 2], 4: [0, 2], 5: [0, 2, 4], 16: list(range(0, 16, 2))}),
+                       (0, {1: [0], 5: [0, 1, 2, 3, 4], 16: list(range(16))})):
         for steps, begin in want.items():
-            assert bounds(shim, steps, usual(steps), wide)[4] == begin + [steps], (wide, steps)
+            assert bounds(shim, steps, usual(steps), kind)[4] == begin + [steps], (kind, steps)
+    i64 = ctypes.c_int64
+    assert [shim.kind(i64(m), i64(n)) for m, n in ((1, 1), (100, 124), (100, 125), (100, 249), (100, 250), (65536, 65536), (1, 65536))] == [0, 0, 1, 1, 2, 0, 2]
 
 
 def test_bounds_hold_for_every_singular_value(shim):
@@ -82,15 +86,15 @@ def test_bounds_hold_for_every_singular_value(shim):
     sigma = np.linspace(0, 1, 200001)
     tried = 0
     for case in range(80):
-        steps, wide = int(rs.randint(1, 17)), bool(rs.randint(2))
+        steps, kind = int(rs.randint(1, 17)), int(rs.randint(3))
         coeff = usual(steps) if case == 0 else (np.float32([2.0, -1.5, 0.5]) + rs.uniform(-0.3, 0.3, (steps, 3))).astype(np.float32)
         coeff[0] *= np.float32(rs.choice([1.0, 4.0]))
-        got = bounds(shim, steps, coeff, wide)
+        got = bounds(shim, steps, coeff, kind)
         if got is None:
             continue
         tried += 1
         x, p, r, q, begin = got
-        assert begin[0] == 0 and begin[-1] == steps and all(0 < b - a <= (3 if wide else 2) for a, b in zip(begin, begin[1:]))
+        assert begin[0] == 0 and begin[-1] == steps and all(0 < b - a <= kind + 1 for a, b in zip(begin, begin[1:]))
         s, amount = sigma.copy(), np.ones_like(sigma)
         for t in range(steps):
             if t in begin:
@@ -152,7 +156,8 @@ def test_orthogonalize_refusals():
         assert refused(**bad) == RANGE, bad
     for bad in (dict(src=(V * 2)(FAKE + 2, FAKE)), dict(dst=(V * 2)(FAKE, FAKE + 1)), dict(dtype=1, src=(V * 2)(FAKE + 1, FAKE))):
         assert refused(**bad) == ALIGN, bad
-    assert refused(ws=0) == WORKSPACE and refused(ws=FAKE + 128) == WORKSPACE and refused(wsb=wsb - 1) == WORKSPACE
+    least = max(ld.ld_orthogonalize_workspace([s]) for s in ((64, 128), (100, 50)))
+    assert least < wsb and refused(ws=0) == WORKSPACE and refused(ws=FAKE + 128) == WORKSPACE and refused(wsb=least - 1) == WORKSPACE
     assert refused(n=0, src=None, dst=None, rows=None, cols=None) == 0
     assert refused(rows=i64(0, 10), cols=i64(10, 0), src=(V * 2)(0, 0), dst=(V * 2)(0, 0), ws=0, wsb=0) == 0
 
@@ -180,12 +185,13 @@ def test_muon_refusals():
         assert call(**bad) == RANGE, bad
     for bad in (dict(w=(V * 2)(FAKE + 2, FAKE)), dict(m=(V * 2)(FAKE, FAKE + 1)), dict(g=(V * 6)(FAKE, FAKE, FAKE, FAKE + 1, FAKE, FAKE))):
         assert call(**bad) == ALIGN, bad
-    assert call(ws=0) == WORKSPACE and call(ws=FAKE + 16) == WORKSPACE and call(wsb=wsb - 1) == WORKSPACE
+    least = max(ld.ld_merge_dense_muon_workspace([s]) for s in ((64, 128), (100, 50)))
+    assert call(ws=0) == WORKSPACE and call(ws=FAKE + 16) == WORKSPACE and call(wsb=least - 1) == WORKSPACE
     assert call(W=0, g=None) == 0 and call(n=0) == 0
 
 
 def test_workspace_is_that_of_the_largest_group(shim):
-    """Groups hold up to 64 problems and 2 GiB of scratch, or one problem; counted here one problem at a time."""
+    """Groups hold up to 64 problems and 8 GiB of scratch, or one problem; counted here one problem at a time."""
     rs = np.random.RandomState(3)
     pad = lambda x: (x + 255) // 256 * 256  # noqa: E731
     for case in range(60):
@@ -198,7 +204,7 @@ def test_workspace_is_that_of_the_largest_group(shim):
                 continue
             need = pad(shim.scratch(min(r, c), max(r, c)))
             for _ in range(W):
-                if count == 64 or (count and used + need > 2 ** 31):
+                if count == 64 or (count and used + need > 2 ** 33):
                     used = count = 0
                 used, count = used + need, count + 1
                 most = max(most, used)
