@@ -58,7 +58,7 @@ __device__ __forceinline__ char* buffer_of(const Batch& b, int32_t i, int32_t wh
 __host__ __device__ __forceinline__ int32_t tiles_of(int64_t side, int32_t tile) { return static_cast<int32_t>((side + tile - 1) / tile); }
 // Where the eight upper halves of row r, columns [8 c, 8 c + 8) lie, in bytes; the lower ones are 64 bytes on, permuted alike.
 __device__ __forceinline__ int64_t piece_at(int64_t rows, int64_t r, int64_t c, int32_t lower) {
-    return ((c >> 2) * rows + r) * kMuonRowBytes + ((((c & 3) | lower << 2) ^ (r & 7)) << 4);
+    return ((c >> 2) * rows + r) * kMuonRowBytes + ((((c & 3) | lower << 2) ^ (r >> 1 & 7)) << 4);
 }
 
 __device__ __forceinline__ void split(const f32x8& x, half8& h, half8& l) {
@@ -106,66 +106,36 @@ struct FinalArgs {
 typedef const void __attribute__((address_space(1))) * global_ptr;
 typedef void __attribute__((address_space(3))) * shared_ptr;
 
-// A tile of SIDE by SIDE sums, by DOWN x ACROSS waves, BLOCKS blocks of columns at a time in shared memory, and as many on their way;
-// without blocks each wave loads what it needs for itself.
-template <int SIDE_, int DOWN_, int ACROSS_, int BLOCKS_> struct Tile {
-    static constexpr int SIDE = SIDE_, DOWN = DOWN_, ACROSS = ACROSS_, BLOCKS = BLOCKS_;
-    static constexpr int THREADS = DOWN * ACROSS * LD_WAVE, WAVES = BLOCKS == 1 ? 2 : 1;  // waves of a SIMD
+// A tile of SIDE by SIDE sums, by DOWN x ACROSS waves. STAGES blocks of columns have room in shared memory: one that is multiplied, the others on
+// their way.
+template <int SIDE_, int DOWN_, int ACROSS_, int STAGES_> struct Tile {
+    static constexpr int SIDE = SIDE_, DOWN = DOWN_, ACROSS = ACROSS_, STAGES = STAGES_;
+    static constexpr int THREADS = DOWN * ACROSS * LD_WAVE;
+    static constexpr int WAVES = SIDE == 64 ? 3 : 2;             // of a SIMD
+    // Consecutive tiles, which share rows and columns, that an XCD has at a time: as many as it runs, so that its cache loads them once.
+    static constexpr int RUN = SIDE == 256 ? 32 : SIDE == 64 ? 96 : 64;
     static constexpr int R = SIDE / DOWN / 32, C = SIDE / ACROSS / 32;            // MFMA tiles of a wave
     static constexpr int BLOCK_BYTES = SIDE * static_cast<int>(kMuonRowBytes);     // an operand's, of a block
-    static constexpr int STAGE_BYTES = 2 * BLOCKS * BLOCK_BYTES;
-    static constexpr int ROWS = SIDE < 64 ? SIDE : 64;                             // rows of sums laid out at a time
+    static constexpr int FETCHES = BLOCK_BYTES / 1024 / (DOWN * ACROSS);           // loads of a wave for it
+    static constexpr int ROWS = 64;                                                // rows of sums laid out at a time
     static constexpr int STRIDE = SIDE + 2;                                        // floats of one: rows and columns read by eights lie in different banks
-    static constexpr int SHARED = 2 * STAGE_BYTES > ROWS * STRIDE * 4 ? 2 * STAGE_BYTES : ROWS * STRIDE * 4;
+    static constexpr int OPERANDS = 2 * STAGES * BLOCK_BYTES, SUMS = ROWS * STRIDE * 4, HELD = ROWS * SIDE * 4;
+    static constexpr int SHARED = OPERANDS > SUMS + HELD ? OPERANDS : SUMS + HELD;
 };
 
 // A block of an operand's rows into shared memory, 16 bytes a lane, as they lie.
 template <typename T>
 __device__ __forceinline__ void fetch(const char* from, char* to) {
-    constexpr int kEach = T::BLOCK_BYTES / 1024 / (T::THREADS / LD_WAVE);
     const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LD_WAVE);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int32_t at = (wave * kEach + i) * 1024;
+    for (int i = 0; i < T::FETCHES; ++i) {
+        const int32_t at = (wave * T::FETCHES + i) * 1024;
         __builtin_amdgcn_global_load_lds((global_ptr)(from + at + ld_lane() * 16), (shared_ptr)(to + at), 16, 0, 0);
     }
 }
 
 __device__ __forceinline__ half8 fragment(const char* tile, int32_t row, int32_t piece) {
-    return *reinterpret_cast<const half8*>(tile + row * kMuonRowBytes + ((piece ^ (row & 7)) << 4));
-}
-
-// One wave's tile, straight from memory: kAhead blocks' operands on their way while one is multiplied.
-template <typename T>
-__device__ __forceinline__ void multiply_alone(const char* left, int64_t left_rows, const char* right, int64_t right_rows, int32_t blocks,
-                                               f32x16 (&acc)[T::R][T::C]) {
-    constexpr int kAhead = 8;
-    const int32_t row = ld_lane() & 31, half = ld_lane() >> 5;
-    const int64_t left_step = left_rows * kMuonRowBytes, right_step = right_rows * kMuonRowBytes;
-    half8 x[kAhead][2][2], y[kAhead][2][2];  // [block][lower][16 columns]
-    const auto load = [&](int32_t k, int at) {
-#pragma unroll
-        for (int l = 0; l < 2; ++l)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                x[at][l][s] = fragment(left + k * left_step, row, 4 * l + 2 * s + half);
-                y[at][l][s] = fragment(right + k * right_step, row, 4 * l + 2 * s + half);
-            }
-    };
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-        if (u < blocks) load(u, u);
-    for (int32_t k = 0; k < blocks; k += kAhead) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (k + u >= blocks) break;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int l = 0; l < 3; ++l) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[u][l == 0][s], y[u][l == 1][s], acc[0][0], 0, 0, 0);
-            if (k + u + kAhead < blocks) load(k + u + kAhead, u);
-        }
-    }
+    return *reinterpret_cast<const half8*>(tile + row * kMuonRowBytes + ((piece ^ (row >> 1 & 7)) << 4));
 }
 
 template <typename T>
@@ -174,56 +144,78 @@ __device__ __forceinline__ void multiply(const char* left, int64_t left_rows, co
     const int32_t lane = ld_lane(), wave = threadIdx.x / LD_WAVE;
     const int32_t row = wave / T::ACROSS * (T::SIDE / T::DOWN) + (lane & 31), col = wave % T::ACROSS * (T::SIDE / T::ACROSS) + (lane & 31);
     const int64_t left_step = left_rows * kMuonRowBytes, right_step = right_rows * kMuonRowBytes;
-    const auto fetch_stage = [&](int32_t k, char* to) {
-#pragma unroll
-        for (int b = 0; b < T::BLOCKS; ++b)
-            if (k + b < blocks) {
-                fetch<T>(left + (k + b) * left_step, to + 2 * b * T::BLOCK_BYTES);
-                fetch<T>(right + (k + b) * right_step, to + (2 * b + 1) * T::BLOCK_BYTES);
-            }
+    constexpr int kStages = T::STAGES;
+    constexpr int kLoads = 2 * T::FETCHES;                   // of a wave for a block
+    const auto fetch_block = [&](int32_t k, int32_t stage) {
+        char* to = shared + stage * 2 * T::BLOCK_BYTES;
+        fetch<T>(left + k * left_step, to);
+        fetch<T>(right + k * right_step, to + T::BLOCK_BYTES);
     };
-    if constexpr (T::BLOCKS == 0) {
-        multiply_alone<T>(left, left_rows, right, right_rows, blocks, acc);
-        return;
-    }
-    fetch_stage(0, shared);
-    __syncthreads();
-    int32_t stage = 0;
-    for (int32_t k = 0; k < blocks; k += T::BLOCKS ? T::BLOCKS : 1) {
-        char* now = shared + stage * T::STAGE_BYTES;
-        stage ^= 1;
-        if (k + T::BLOCKS < blocks) fetch_stage(k + T::BLOCKS, shared + stage * T::STAGE_BYTES);
-        const int32_t held = T::BLOCKS == 1 ? 1 : blocks - k < T::BLOCKS ? blocks - k : T::BLOCKS;
-        for (int32_t b = 0; b < held; ++b, now += 2 * T::BLOCK_BYTES) {
+    // The operands of 16 columns are read while those before them are multiplied, and waited for before the next are read: the compiler
+    // would wait for both.
+    constexpr int kSharedRead = 0xC07F;  // lgkmcnt(0), nothing else
+    half8 x[2][T::R][2], y[2][T::C][2];
+    const auto read = [&](int s, int32_t stage) {
+        const char* now = shared + stage * 2 * T::BLOCK_BYTES;
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                half8 x[T::R][2], y[T::C][2];
+        for (int l = 1; l >= 0; --l) {
 #pragma unroll
-                for (int l = 0; l < 2; ++l) {
+            for (int i = 0; i < T::R; ++i) x[s][i][l] = fragment(now, row + 32 * i, 4 * l + 2 * s + (lane >> 5));
 #pragma unroll
-                    for (int i = 0; i < T::R; ++i) x[i][l] = fragment(now, row + 32 * i, 4 * l + 2 * s + (lane >> 5));
-#pragma unroll
-                    for (int j = 0; j < T::C; ++j) y[j][l] = fragment(now + T::BLOCK_BYTES, col + 32 * j, 4 * l + 2 * s + (lane >> 5));
-                }
-                // lower halves first; one after another for every sum, whatever the tile
-#pragma unroll
-                for (int l = 0; l < 3; ++l)
-#pragma unroll
-                    for (int i = 0; i < T::R; ++i)
-#pragma unroll
-                        for (int j = 0; j < T::C; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][l == 0], y[j][l == 1], acc[i][j], 0, 0, 0);
-            }
+            for (int j = 0; j < T::C; ++j) y[s][j][1 - l] = fragment(now + T::BLOCK_BYTES, col + 32 * j, 4 * (1 - l) + 2 * s + (lane >> 5));
         }
-        __syncthreads();
+    };
+    const auto use = [&](int s) {  // lower halves first; one after another for every sum, whatever the tile
+#pragma unroll
+        for (int l = 0; l < 3; ++l)
+#pragma unroll
+            for (int i = 0; i < T::R; ++i)
+#pragma unroll
+                for (int j = 0; j < T::C; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[s][i][l == 0], y[s][j][l == 1], acc[i][j], 0, 0, 0);
+    };
+    for (int32_t k = 0; k < kStages && k < blocks; ++k) fetch_block(k, k);
+    if (blocks >= kStages) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 1) * kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    read(0, 0);
+    int32_t stage = 0;
+    for (int32_t k = 0; k < blocks; ++k) {
+        const int32_t next = stage + 1 == kStages ? 0 : stage + 1;
+        __builtin_amdgcn_s_waitcnt(kSharedRead);
+        read(1, stage);
+        __builtin_amdgcn_sched_barrier(0);
+        use(0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(kSharedRead);
+        if (k + 1 < blocks) {
+            // This wave's loads of the next block have arrived when no more are left than those of the blocks behind it; the barrier then
+            // says it of all waves, and that all have read this block, whose room is filled anew.
+            if (k + kStages <= blocks) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            if (k + kStages < blocks) fetch_block(k + kStages, stage);
+            read(0, next);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        use(1);
+        __builtin_amdgcn_sched_barrier(0);
+        stage = next;
     }
+    __syncthreads();
+}
+
+// A barrier for what goes through shared memory alone: what is on its way to memory is not waited for, as __syncthreads does. With
+// `loads` what the wave loads into shared memory is.
+template <bool LOADS = false>
+__device__ __forceinline__ void shared_barrier() {
+    if (LOADS) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // The sums of the `part`-th T::ROWS rows, times `inv`, as rows of 32-bit values in shared memory.
 template <typename T>
-__device__ __forceinline__ void lay_out(const f32x16 (&acc)[T::R][T::C], int32_t part, float inv, float* sums, int32_t stride = T::STRIDE) {
+__device__ __forceinline__ void lay_out(const f32x16 (&acc)[T::R][T::C], int32_t part, float inv, float* sums, int32_t stride, bool loads) {
     const int32_t lane = ld_lane(), wave = threadIdx.x / LD_WAVE, first = wave / T::ACROSS * (T::SIDE / T::DOWN);
-    if (part > 0) __syncthreads();
+    if (part > 0) shared_barrier();
 #pragma unroll
     for (int i = 0; i < T::R; ++i) {
         if ((first + 32 * i) / T::ROWS != part) continue;
@@ -236,8 +228,44 @@ __device__ __forceinline__ void lay_out(const f32x16 (&acc)[T::R][T::C], int32_t
                 sums[r * stride + c] = acc[i][j][q] * inv;
             }
     }
-    __syncthreads();
+    if (loads) shared_barrier<true>();
+    else shared_barrier();
 }
+
+// A value's two halves side by side, as shared memory holds them between a row's way out and a column's.
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ u32x8 pack(const half8& h, const half8& l) {
+    return __builtin_bit_cast(u32x8, __builtin_shufflevector(h, l, 0, 8, 1, 9, 2, 10, 3, 11, 4, 12, 5, 13, 6, 14, 7, 15));
+}
+__device__ __forceinline__ void store_packed(char* upper, char* lower, const u32x8& x) {
+    ld_u32x4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        h[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x05040100u);
+        l[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x07060302u);
+    }
+    *reinterpret_cast<ld_u32x4*>(upper) = h;
+    *reinterpret_cast<ld_u32x4*>(lower) = l;
+}
+
+// A tile's way out as halves. Four lanes write those of 32 columns of a row, which lie side by side, the next four those of the row behind
+// it. A thread's pieces all have the same permutation.
+template <typename T>
+struct WayOut {
+    static constexpr int EACH = T::ROWS * T::SIDE / 8 / T::THREADS, STEP = T::THREADS / 4;
+    int32_t piece, along;
+    __device__ __forceinline__ WayOut() : piece(threadIdx.x & 3), along(threadIdx.x >> 2) {}
+    // of the part, row r and the first of eight columns c
+    __device__ __forceinline__ void straight(int p, int32_t& r, int32_t& c) const {
+        const int32_t n = along + p * STEP;
+        r = n % T::ROWS, c = n / T::ROWS * 32 + piece * 8;
+    }
+    // the first of eight rows r, and column c
+    __device__ __forceinline__ void turned(int p, int32_t& r, int32_t& c) const {
+        const int32_t n = along + p * STEP;
+        r = n / T::SIDE * 32 + piece * 8, c = n % T::SIDE;
+    }
+};
 
 // Which problem a tile is of, and its number there.
 __device__ __forceinline__ int32_t problem_of(const Batch& b, int32_t& tile) {
@@ -254,7 +282,8 @@ __device__ __forceinline__ int32_t problem_of(const Batch& b, int32_t& tile) {
 template <typename T>
 __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_symmetric(Batch batch, Plans plans) {
     __shared__ __attribute__((aligned(16))) char shared[T::SHARED];
-    int32_t tile = blockIdx.x;
+    int32_t tile = static_cast<int32_t>(ld_xcd_piece<T::RUN>(blockIdx.x, gridDim.x));
+    if (tile >= batch.first[batch.count]) return;
     const int32_t i = problem_of(batch, tile);
     const Plan a = plans.of[batch.kind[i]];
     const int32_t side = tiles_of(padded(batch.m[i]), T::SIDE), tiles = side * (side + 1) / 2, second = tile >= tiles;
@@ -271,38 +300,71 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_symmetric(Batch batch,
     multiply<T>(buffer_of(batch, i, prod.left) + r0 * kMuonRowBytes, rows, buffer_of(batch, i, prod.right) + c0 * kMuonRowBytes, rows,
                 static_cast<int32_t>((a.long_sum ? padded(batch.n[i]) : rows) / kMuonBlock), shared, acc);
     float* sums = reinterpret_cast<float*>(shared);
-    constexpr int S = T::STRIDE, kPieces = T::SIDE / 8;
+    constexpr int S = T::STRIDE;
     char* out = buffer_of(batch, i, prod.out);
     const char* gram = buffer_of(batch, i, prod.left);
-    const auto keep = [&](f32x8 x, int32_t r, int32_t c) {  // eight columns from c on of row r, of the whole matrix
-        if (a.poly) {
-            x = a.cc * x + a.cb * load_split(gram, rows, r, c >> 3);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (r == c + e && r < m) x[e] += a.ca;
-        }
-        store_split(out, rows, r, c >> 3, x * scale);
-    };
-    // Only sums on and below the diagonal are kept, and mirrored, in squares of eight by eight. Four lanes write the halves of 32 columns
-    // of a row, which lie side by side, the next four those of the row behind it.
+    // Only sums on and below the diagonal are kept, and mirrored, in squares of eight by eight. What is needed of A comes into shared memory
+    // behind the sums.
+    const WayOut<T> way;
+    char* held = shared + T::SUMS;
     for (int32_t h = 0; h < T::SIDE / T::ROWS; ++h) {
-        lay_out<T>(acc, h, a.inv, sums);
         const int32_t h0 = r0 + T::ROWS * h;
-        for (int32_t p = threadIdx.x; p < T::ROWS * kPieces; p += T::THREADS) {
-            const int32_t r = (p >> 2) % T::ROWS, c = (p >> 2) / T::ROWS * 32 + (p & 3) * 8, at = h0 + r - c0;  // at: the row's number among the columns
-            if (h0 + r >= rows || c0 + c >= rows || c > at) continue;
-            f32x8 x;
+        if (a.poly) {
+            const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LD_WAVE);
+            if (h > 0) shared_barrier();
+            for (int32_t k = wave; k < T::SIDE / kMuonBlock && c0 + k * kMuonBlock < rows; k += T::THREADS / LD_WAVE)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = sums[c + e > at ? (c + e - at + r) * S + at : r * S + c + e];
-            keep(x, h0 + r, c0 + c);
+                for (int n = 0; n < T::ROWS / 8; ++n)
+                    __builtin_amdgcn_global_load_lds((global_ptr)(gram + ((c0 / kMuonBlock + k) * rows + h0 + 8 * n) * kMuonRowBytes + ld_lane() * 16),
+                                                     (shared_ptr)(held + (k * T::ROWS + 8 * n) * kMuonRowBytes), 16, 0, 0);
         }
-        for (int32_t p = threadIdx.x; p < T::ROWS / 8 * T::SIDE; p += T::THREADS) {
-            const int32_t c = (p >> 2) % T::SIDE, r = (p >> 2) / T::SIDE * 32 + (p & 3) * 8;
-            if (h0 + r >= rows || c0 + c >= rows || (h0 + r) / 8 <= (c0 + c) / 8) continue;
+        lay_out<T>(acc, h, a.inv, sums, S, a.poly != 0);
+#pragma unroll 2
+        for (int p = 0; p < WayOut<T>::EACH; ++p) {
+            int32_t r, c;
+            way.straight(p, r, c);
+            const int32_t row = h0 + r, col = c0 + c;
+            if (row >= rows || col >= rows || col > row) continue;
+            float* from = sums + r * S + c;
             f32x8 x;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = sums[(r + e) * S + c];
-            keep(x, c0 + c, h0 + r);
+            for (int e = 0; e < 8; ++e) x[e] = from[e];
+            const bool diagonal = tr == tc && row / 8 == col / 8;
+            if (diagonal) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (col + e > row) x[e] = sums[(col + e - h0) * S + row - c0];
+            }
+            if (a.poly) {
+                const char* block = held + (c >> 5) * T::ROWS * kMuonRowBytes;
+                const f32x8 g = __builtin_convertvector(fragment(block, r, way.piece), f32x8) + __builtin_convertvector(fragment(block, r, way.piece | 4), f32x8);
+                x = a.cc * x + a.cb * g;
+                if (diagonal) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (row == col + e && row < m) x[e] += a.ca;
+                }
+            }
+            half8 upper, lower;
+            split(x * scale, upper, lower);
+            *reinterpret_cast<half8*>(out + piece_at(rows, row, col >> 3, 0)) = upper;
+            *reinterpret_cast<half8*>(out + piece_at(rows, row, col >> 3, 1)) = lower;
+            if (!diagonal) {  // to be mirrored; the squares on the diagonal are read by one another's rows
+                const u32x8 both = pack(upper, lower);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) reinterpret_cast<uint32_t*>(from)[e] = both[e];
+            }
+        }
+        shared_barrier();
+#pragma unroll 2
+        for (int p = 0; p < WayOut<T>::EACH; ++p) {
+            int32_t r, c;
+            way.turned(p, r, c);
+            if (h0 + r >= rows || c0 + c >= rows || (h0 + r) / 8 <= (c0 + c) / 8) continue;
+            u32x8 x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = reinterpret_cast<const uint32_t*>(sums)[(r + e) * S + c];
+            store_packed(out + piece_at(rows, c0 + c, (h0 + r) >> 3, 0), out + piece_at(rows, c0 + c, (h0 + r) >> 3, 1), x);
         }
     }
 }
@@ -311,7 +373,8 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_symmetric(Batch batch,
 template <typename T, bool FINAL, int OT>
 __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Plans plans, FinalArgs f) {
     __shared__ __attribute__((aligned(16))) char shared[T::SHARED];
-    int32_t tile = blockIdx.x;
+    int32_t tile = static_cast<int32_t>(ld_xcd_piece<T::RUN>(blockIdx.x, gridDim.x));
+    if (tile >= batch.first[batch.count]) return;
     const int32_t i = problem_of(batch, tile);
     const Plan a = plans.of[batch.kind[i]];
     const int32_t m = batch.m[i], n = batch.n[i], down = tiles_of(padded(m), T::SIDE);
@@ -323,6 +386,8 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Pla
     float* sums = reinterpret_cast<float*>(shared);
     constexpr int S = T::STRIDE, kPieces = T::SIDE / 8;
     typedef typename LdElem<OT>::type elem;
+    char* straight = FINAL ? nullptr : buffer_of(batch, i, a.prod[0].out);
+    char* turned = FINAL ? nullptr : buffer_of(batch, i, a.prod[0].out_t);
     elem* final_out = FINAL ? static_cast<elem*>(f.out[i]) : nullptr;
     const int64_t stride = FINAL ? f.stride[i] : 0;
     const auto write = [&](const f32x8& x, int32_t r, int32_t c, int32_t width) {
@@ -346,7 +411,7 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Pla
         if (FINAL && batch.flipped[i]) {
             // an odd stride, and the lanes along the columns that are rows of the update: what they write lies side by side
             constexpr int kOdd = T::SIDE + 1, kDeep = T::ROWS / 8;
-            lay_out<T>(acc, h, a.inv, sums, kOdd);
+            lay_out<T>(acc, h, a.inv, sums, kOdd, false);
             for (int32_t p = threadIdx.x; p < kDeep * T::SIDE; p += T::THREADS) {
                 const int32_t c = p / kDeep, r = p % kDeep * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
                 f32x8 x;
@@ -356,24 +421,47 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Pla
             }
             continue;
         }
-        lay_out<T>(acc, h, a.inv, sums);
-        for (int32_t p = threadIdx.x; p < T::ROWS * kPieces; p += T::THREADS) {
-            const int32_t r = FINAL ? p / kPieces : (p >> 2) % T::ROWS, c = FINAL ? p % kPieces * 8 : (p >> 2) / T::ROWS * 32 + (p & 3) * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
-            f32x8 x;
+        lay_out<T>(acc, h, FINAL ? a.inv : a.inv * a.scale[0], sums, S, false);
+        if (FINAL) {
+            for (int32_t p = threadIdx.x; p < T::ROWS * kPieces; p += T::THREADS) {
+                const int32_t r = p / kPieces, c = p % kPieces * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
+                f32x8 x;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = sums[r * S + c + e];
-            if (FINAL) {
+                for (int e = 0; e < 8; ++e) x[e] = sums[r * S + c + e];
                 if (ri < m) write(x, ri, ci, n);
-            } else if (ri < rows && ci < cols) {
-                store_split(buffer_of(batch, i, a.prod[0].out), rows, ri, ci >> 3, x * a.scale[0]);
             }
+            continue;
         }
-        for (int32_t p = threadIdx.x; !FINAL && p < T::ROWS / 8 * T::SIDE; p += T::THREADS) {
-            const int32_t c = (p >> 2) % T::SIDE, r = (p >> 2) / T::SIDE * 32 + (p & 3) * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
+        const WayOut<T> way;
+#pragma unroll 2
+        for (int p = 0; p < WayOut<T>::EACH; ++p) {
+            int32_t r, c;
+            way.straight(p, r, c);
+            const int32_t row = r0 + T::ROWS * h + r, col = c0 + c;
+            if (row >= rows || col >= cols) continue;
+            float* from = sums + r * S + c;
             f32x8 x;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = sums[(r + e) * S + c];
-            if (ri < rows && ci < cols) store_split(buffer_of(batch, i, a.prod[0].out_t), cols, ci, ri >> 3, x * a.scale[0]);
+            for (int e = 0; e < 8; ++e) x[e] = from[e];
+            half8 upper, lower;
+            split(x, upper, lower);
+            *reinterpret_cast<half8*>(straight + piece_at(rows, row, col >> 3, 0)) = upper;
+            *reinterpret_cast<half8*>(straight + piece_at(rows, row, col >> 3, 1)) = lower;
+            const u32x8 both = pack(upper, lower);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) reinterpret_cast<uint32_t*>(from)[e] = both[e];
+        }
+        shared_barrier();
+#pragma unroll 2
+        for (int p = 0; p < WayOut<T>::EACH; ++p) {
+            int32_t r, c;
+            way.turned(p, r, c);
+            const int32_t row = r0 + T::ROWS * h + r, col = c0 + c;
+            if (row >= rows || col >= cols) continue;
+            u32x8 x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = reinterpret_cast<const uint32_t*>(sums)[(r + e) * S + c];
+            store_packed(turned + piece_at(cols, col, row >> 3, 0), turned + piece_at(cols, col, row >> 3, 1), x);
         }
     }
 }
@@ -639,10 +727,9 @@ size_t workspace_of(const int64_t* rows, const int64_t* cols, int32_t n, int64_t
     return most == 0 ? 0 : static_cast<size_t>(kSumBytes + most);
 }
 
-typedef Tile<32, 1, 1, 0> Least;
-typedef Tile<64, 2, 2, 4> Small;
-typedef Tile<128, 2, 2, 1> Middle;
-typedef Tile<256, 2, 4, 1> Large;
+typedef Tile<64, 2, 2, 3> Small;
+typedef Tile<128, 2, 2, 2> Middle;
+typedef Tile<256, 2, 4, 2> Large;
 
 void program_of(const Polynomial& p, int32_t kind, Program& out) {
     const auto scale = [](double bound) { return ld_muon_scale(bound); };
@@ -725,35 +812,36 @@ ld_status run_steps(Batch& b, const Polynomial& p, const FinalArgs& out, int32_t
             tiles += a.of[b.kind[i]].products * (apply ? down * across : down * (down + 1) / 2);
         }
         for (int32_t i = b.count; i <= kMost; ++i) b.first[i] = tiles;
-        const dim3 grid(tiles), threads(T::THREADS);
+        const dim3 grid((tiles + 7) / 8 * 8), threads(T::THREADS);
         if (!apply) k_symmetric<T><<<grid, threads, 0, s>>>(b, a);
         else if (final) ld_with_type(out_type, [&](auto type) { k_apply<T, true, type><<<grid, threads, 0, s>>>(b, a, out); });
         else k_apply<T, false, LD_F32><<<grid, threads, 0, s>>>(b, a, out);
         return ld_launch_status();
     };
-    // Which tile: the one that is done first, by what blocks of 32 columns take a CU (ns) with each, as measured. 256: a tile at a time;
-    // 128: two, or one, at a time; 64: one; 32: eight at a time, of which few wait on memory alone.
+    // Which tile: the one that is done first, by fits to what launches of 1 to 64 square matrices of 64 to 4096 took (us; within some 10 %).
+    // x: tiles a CU has; a block: 32 columns. A CU works on one tile of 256, two of 128, three of 64. (4096 x 4096, one and four of
+    // them, A^2: 320 and 1200 by 64, 271 and 837 by 128, 298 and 920 by 256; six: 1841, 1256, 1280. 768 x 768, one and 32: 13 and 71, 26 and
+    // 73, 64 and 79. Tiles of 32, each wave for itself, were no faster than 64 for any.)
     const auto launch = [&](const Plans& a) {
         bool apply = false;
         for (const Plan& plan : a.of) apply |= plan.apply != 0;
-        const int32_t sides[4] = {32, 64, 128, 256};
+        const int32_t sides[3] = {64, 128, 256};
         double best = 0.0;
         int32_t side = 0;
-        for (int32_t k = 0; k < 4; ++k) {
-            double tiles = 0.0, blocks = 0.0;
+        for (int32_t k = 0; k < 3; ++k) {
+            double tiles = 0.0, all_blocks = 0.0;
             for (int32_t i = 0; i < b.count; ++i) {
                 const Plan& plan = a.of[b.kind[i]];
                 const int32_t down = tiles_of(ld_muon_padded(b.m[i]), sides[k]), across = tiles_of(ld_muon_padded(b.n[i]), sides[k]);
                 const double mine = static_cast<double>(plan.products) * (apply ? static_cast<double>(down) * across : 0.5 * down * (down + 1.0));
-                tiles += mine, blocks += mine * (ld_muon_padded(plan.long_sum ? b.n[i] : b.m[i]) / kMuonBlock);
+                tiles += mine, all_blocks += mine * (ld_muon_padded(plan.long_sum ? b.n[i] : b.m[i]) / kMuonBlock);
             }
-            const double each = blocks / tiles, rounds = ceil(tiles / kCUs), pairs = floor(rounds / 2.0);
-            const double time = sides[k] == 256 ? 20000.0 + each * 2700.0 * rounds
-                                : sides[k] == 128 ? 10000.0 + each * (1600.0 * pairs + 900.0 * (rounds - 2.0 * pairs))
-                                : sides[k] == 64 ? 5000.0 + each * 400.0 * rounds : 4000.0 + each * fmax(200.0, 220.0 * rounds);
+            const double blocks = all_blocks / tiles, x = tiles / kCUs, rounds = ceil(x);
+            const double time = sides[k] == 256 ? 10.0 + rounds * (6.0 + 2.4 * blocks)
+                                : sides[k] == 128 ? 8.0 + blocks * fmax(0.87, 0.73 * x + 0.45) : 5.0 + blocks * fmax(0.34, 0.28 * x + 0.1);
             if (k == 0 || time < best) best = time, side = sides[k];
         }
-        return side == 256 ? launch_as(Large(), a) : side == 128 ? launch_as(Middle(), a) : side == 64 ? launch_as(Small(), a) : launch_as(Least(), a);
+        return side == 256 ? launch_as(Large(), a) : side == 128 ? launch_as(Middle(), a) : launch_as(Small(), a);
     };
     for (;;) {
         const auto sort_of = [](const Plan& plan) { return plan.final ? 0 : plan.apply ? 2 : 1; };
