@@ -19,7 +19,7 @@ constexpr int kWide = 256, kNarrow = 64;       // threads of a workgroup: one ro
 constexpr int32_t kNarrowElems = 4096;         // up to here a row is one wave's
 constexpr int32_t kMostPart = 65536;           // elements of a part: 32 KB of group maxima for the alternatives
 constexpr int32_t kPartStep = kWide * kGroup;
-constexpr int64_t kWorkgroups = 1024;          // rows are split until there are as many
+constexpr int64_t kWorkgroups = 1024;          // rows are split until there are as many, where they are fewer than half
 constexpr int kMostTop = LD_MAX_TOP;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // Powers of two by which a value may pass the reference before that is moved: an exponent is rounded in proportion to it.
@@ -121,73 +121,122 @@ __device__ __forceinline__ void write_top(const ScoreArgs& a, int64_t t, int32_t
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
+// N elements that lie on a 16-byte boundary, or on that of all of them, as loaded.
+template <int DT, int N> struct Raw {
+    typedef typename LdElem<DT>::type elem;
+    typedef elem type __attribute__((ext_vector_type(N)));
+    static __device__ __forceinline__ type load(const elem* p) {
+        if constexpr (DT == LD_F32 && N == 8) {
+            typedef float half __attribute__((ext_vector_type(4)));
+            const half lo = *reinterpret_cast<const half*>(p), hi = *reinterpret_cast<const half*>(p + 4);
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            return *reinterpret_cast<const type*>(p);
+        }
+    }
+    // n < N of them, minus infinity behind
+    static __device__ __forceinline__ type load_some(const elem* p, int32_t n) {
+        type x;
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = e < n ? p[e] : static_cast<elem>(-__builtin_huge_valf());
+        return x;
+    }
+};
+// The largest of eight; a NaN only where all are.
 template <int DT>
-__device__ __forceinline__ f32x8 load_group(const typename LdElem<DT>::type* p) {
-    if constexpr (DT == LD_F32) {
-        typedef typename LdVec<LD_F32, 4>::type half;
-        const half lo = *reinterpret_cast<const half*>(p), hi = *reinterpret_cast<const half*>(p + 4);
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+__device__ __forceinline__ float largest(const typename Raw<DT, kGroup>::type& x) {
+    if constexpr (DT == LD_F16) {  // two at a time
+        typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+        typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+        const half4 a = __builtin_elementwise_max(__builtin_shufflevector(x, x, 0, 1, 2, 3), __builtin_shufflevector(x, x, 4, 5, 6, 7));
+        const half2 b = __builtin_elementwise_max(__builtin_shufflevector(a, a, 0, 1), __builtin_shufflevector(a, a, 2, 3));
+        return fmaxf(static_cast<float>(b[0]), static_cast<float>(b[1]));
     } else {
-        typedef LdVec<DT, 8> V;
-        return V::widen(*reinterpret_cast<const typename V::type*>(p));
+        const f32x8 y = __builtin_convertvector(x, f32x8);
+        return fmaxf(fmaxf(fmaxf(fmaxf(y[0], y[1]), y[2]), fmaxf(fmaxf(y[3], y[4]), y[5])), fmaxf(y[6], y[7]));
     }
 }
-// The same at the end of a row, minus infinity behind it.
-template <int DT>
-__device__ __forceinline__ f32x8 load_ragged(const typename LdElem<DT>::type* p, int32_t n) {
-    f32x8 x;
-#pragma unroll
-    for (int e = 0; e < kGroup; ++e) x[e] = e < n ? static_cast<float>(p[e]) : -__builtin_huge_valf();
-    return x;
+// Elements from p on up to the first on a boundary of N.
+template <typename E>
+__device__ __forceinline__ int32_t to_boundary(const E* p, int32_t N) {
+    return static_cast<int32_t>(-static_cast<int64_t>(reinterpret_cast<uintptr_t>(p) / sizeof(E)) & (N - 1));
 }
 
-// A part of a row: its sums, and with TOP its best elements. `groups`: the order of every group's largest element.
+// The rank of every lane's key among the wave's, 0 for the largest. Equal keys are 0 and nothing.
+__device__ __forceinline__ int32_t rank_in_wave(uint64_t key) {
+    int32_t rank = 0;
+    for (int j = 0; j < LD_WAVE; ++j) {
+        const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(key), j), hi = __builtin_amdgcn_readlane(static_cast<int>(key >> 32), j);
+        rank += (static_cast<uint64_t>(hi) << 32 | lo) > key;
+    }
+    return rank;
+}
+// How many of 64 keys in falling order are larger than `key`.
+__device__ __forceinline__ int32_t larger_among(const uint64_t* sorted, uint64_t key) {
+    int32_t n = 0;
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1)
+        if (sorted[n + step - 1] > key) n += step;
+    return n + (n == 63 && sorted[63] > key);
+}
+
+// A part of a row: its sums, and with TOP its best elements. Groups of eight begin at 16-byte boundaries (odd rows of 16-bit logits
+// loaded as they lie took a fifth longer: 16384 x 50257 338 us, now 280): up to seven elements before the first are one too,
+// and those behind the last. `groups`: every group's largest element.
 template <int DT, int THREADS, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
     typedef typename LdElem<DT>::type elem;
+    typedef Raw<DT, kGroup> R;
     constexpr int kWaves = THREADS / LD_WAVE;
-    extern __shared__ uint32_t groups[];
+    extern __shared__ float groups[];
     __shared__ Sums wave_sums[kWaves];
-    __shared__ uint32_t wave_high[kWaves];
+    __shared__ float wave_high[kWaves];
     __shared__ uint64_t keys[TOP ? kMostTop * kGroup : 1];
-    __shared__ uint32_t list_count, picked_groups[TOP ? kMostTop : 1];
+    __shared__ uint32_t counts[2], picked_groups[TOP ? kMostTop : 1];
     __shared__ uint64_t kth;
     const int64_t t = a.row0 + blockIdx.x / a.parts;
-    const int32_t p = blockIdx.x % a.parts, begin = p * a.part, n = min(a.V - begin, a.part);
-    const int32_t n_groups = (n + kGroup - 1) / kGroup, whole = n / kGroup, tid = threadIdx.x;
+    const int32_t p = blockIdx.x % a.parts, begin = p * a.part, n = min(a.V - begin, a.part), tid = threadIdx.x;
     const elem* row = static_cast<const elem*>(a.logits) + t * a.stride + begin;
-    const float c = a.scale * kLog2e;
+    const int32_t head = min(to_boundary(row, kGroup), n), headed = head > 0;
+    const elem* body = row + head;
+    const int32_t whole = (n - head) / kGroup, rest = (n - head) % kGroup, n_body = whole + (rest > 0), n_groups = headed + n_body;
+    const float c = a.scale * kLog2e, infinity = __builtin_huge_valf();
 
-    const float lowest = -kLowest / c;
-    float ref = lowest, ref_c = -kLowest, z = 0.0f, s = 0.0f;
-    uint32_t high = 0, at = 0;  // order of this thread's largest element, and its group
-    const auto take = [&](const f32x8& x, int32_t g) {
-        float m = fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(fmaxf(x[3], x[4]), x[5])), fmaxf(x[6], x[7]));
-        const uint32_t o = order_of(m);
-        if (o > high) high = o, at = g;
-        if (TOP) groups[g] = o;
-        if (m * c > ref_c + kFar) {
+    // Sums against a reference, which moves to a value that lies beyond `limit`.
+    const float lowest = -kLowest / c, far = kFar / c;
+    float ref = lowest, ref_c = -kLowest, limit = lowest + far, z = 0.0f, s = 0.0f;
+    float high = -infinity;  // this thread's largest element, and its group
+    int32_t at = tid == 0 ? 0 : tid + headed;
+    const auto take = [&](const typename R::type& x, int32_t g) {
+        const float m = largest<DT>(x);
+        if (TOP) {
+            groups[g] = m;
+            if (m > high) at = g;
+        }
+        high = fmaxf(high, m);
+        if (m > limit) {
             const Sums r = moved({ref, z, s}, m, c);
-            ref = m, ref_c = m * c, z = r.z, s = r.s;
+            ref = m, ref_c = m * c, limit = m + far, z = r.z, s = r.s;
         }
 #pragma unroll
         for (int e = 0; e < kGroup; ++e) {
-            const float d = __fmaf_rn(x[e], c, -ref_c), y = __builtin_amdgcn_exp2f(d);
+            const float d = __fmaf_rn(static_cast<float>(x[e]), c, -ref_c), y = __builtin_amdgcn_exp2f(d);
             z += y;
             if (ENTROPY) s = __fmaf_rn(y, fmaxf(d, -200.0f), s);
         }
     };
+    if (headed && tid == 0) take(R::load_some(row, head), 0);
     constexpr int kUnroll = 4;
     int32_t g = tid;
     for (; g + (kUnroll - 1) * THREADS < whole; g += kUnroll * THREADS) {
-        f32x8 x[kUnroll];
+        typename R::type x[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) x[u] = load_group<DT>(row + static_cast<int64_t>(g + u * THREADS) * kGroup);
+        for (int u = 0; u < kUnroll; ++u) x[u] = R::load(body + (g + u * THREADS) * kGroup);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) take(x[u], g + u * THREADS);
+        for (int u = 0; u < kUnroll; ++u) take(x[u], headed + g + u * THREADS);
     }
-    for (; g < whole; g += THREADS) take(load_group<DT>(row + static_cast<int64_t>(g) * kGroup), g);
-    if (g < n_groups) take(load_ragged<DT>(row + static_cast<int64_t>(g) * kGroup, n - whole * kGroup), g);
+    for (; g < whole; g += THREADS) take(R::load(body + g * kGroup), headed + g);
+    if (g < n_body) take(R::load_some(body + g * kGroup, rest), headed + g);
 
     // What rounding ref_c has moved all exponents by.
     if (ref != lowest) {
@@ -196,15 +245,14 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
         z *= f;
     }
     const int32_t wave = tid / LD_WAVE;
-    uint32_t top_order = wave_max(high);
+    float most = value_of(wave_max(order_of(high)));
     if (kWaves > 1) {
-        if (ld_lane() == 0) wave_high[wave] = top_order;
+        if (ld_lane() == 0) wave_high[wave] = most;
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w) top_order = max(top_order, wave_high[w]);
+        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, wave_high[w]);
     }
-    const float most = value_of(top_order);
     Sums r = moved({ref, z, s}, most, c);
-    if (most != -__builtin_huge_valf() && !(fabsf(most) * c < kSteady)) {
+    if (most != -infinity && !(fabsf(most) * c < kSteady)) {
         r.z = r.s = 0.0f;
         for (int32_t i = tid; i < n; i += THREADS) {
             const float d = (static_cast<float>(row[i]) - most) * c, y = __builtin_amdgcn_exp2f(d);
@@ -230,56 +278,75 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
     }
     if (!TOP) return;
 
+    const auto first_of = [&](int32_t q) { return headed && q == 0 ? 0 : head + (q - headed) * kGroup; };  // a group's elements
+    const auto end_of = [&](int32_t q) { return headed && q == 0 ? head : min(head + (q - headed + 1) * kGroup, n); };
+    const auto own_groups = [&](auto f) {  // of this thread, in order
+        if (headed && tid == 0) f(0);
+        for (int32_t q = tid; q < n_body; q += THREADS) f(headed + q);
+    };
     // The maxima above passed NaN over: where there is one, or an infinity, all groups are ordered once more, one element at a time.
+    uint32_t order = order_of(high);
     if (r.z != r.z) {
-        high = 0;
-        for (int32_t q = tid; q < n_groups; q += THREADS) {
+        order = 0;
+        own_groups([&](int32_t q) {
             uint32_t o = 0;
-            for (int32_t e = q * kGroup; e < min(q * kGroup + kGroup, n); ++e) o = max(o, order_of(static_cast<float>(row[e])));
-            groups[q] = o;
-            if (o > high) high = o, at = q;
-        }
+            for (int32_t e = first_of(q); e < end_of(q); ++e) o = max(o, order_of(static_cast<float>(row[e])));
+            groups[q] = value_of(o);
+            if (o > order) order = o, at = q;
+        });
     }
     // The best K elements lie in the K groups whose largest elements are the best K (of equal ones the lower), and those in the K
-    // threads of which the same holds.
+    // threads of which the same holds. First the K-th of those threads' best.
     const int32_t K = a.top;
+    const uint64_t mine = tid < n_body || (headed && tid == 0) ? key_of(order, at) : 0;
+    if (tid == 0) counts[0] = counts[1] = 0, kth = 0;
+    int32_t rank = rank_in_wave(mine);
     __syncthreads();
-    const uint64_t mine = high ? key_of(high, at) : 0;
-    keys[tid] = mine;
-    if (tid == 0) list_count = 0, kth = 0;
-    __syncthreads();
-    int32_t rank = 0;
-    for (int j = 0; j < THREADS; ++j) rank += keys[j] > mine;
+    if (kWaves > 1) {
+        if (mine) keys[wave * LD_WAVE + rank] = mine;
+        else keys[tid] = 0;  // lanes without a group are a wave's last
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w)
+            if (w != wave) rank += larger_among(keys + w * LD_WAVE, mine);
+    }
     if (rank == K - 1 && mine) kth = mine;
     __syncthreads();
-    // Groups of those threads that are no worse than the K-th thread's best, behind the maxima.
+    // Groups of those threads that are no worse, behind the maxima; of them the K best.
     const uint64_t least = kth;
-    uint32_t* list = groups + n_groups;
-    if (mine >= least)
-        for (int32_t q = tid; q < n_groups; q += THREADS)
-            if (key_of(groups[q], q) >= least) list[atomicAdd(&list_count, 1u)] = q;
+    uint64_t* list = reinterpret_cast<uint64_t*>(groups + (n_groups + 1) / 2 * 2);
+    if (mine >= least && mine)
+        own_groups([&](int32_t q) {
+            const uint64_t k = key_of(order_of(groups[q]), q);
+            if (k >= least) list[atomicAdd(&counts[0], 1u)] = k;
+        });
     __syncthreads();
-    const int32_t listed = list_count, kept = min(listed, K);
+    const int32_t listed = counts[0], kept = min(listed, K);
     for (int32_t i = tid; i < listed; i += THREADS) {
-        const uint64_t k = key_of(groups[list[i]], list[i]);
+        const uint64_t k = list[i];
         int32_t better = 0;
-        for (int32_t j = 0; j < listed; ++j) better += key_of(groups[list[j]], list[j]) > k;
-        if (better < K) picked_groups[better] = list[i];
-    }
-    __syncthreads();
-    for (int32_t i = tid; i < kept * kGroup; i += THREADS) {
-        const int32_t e = static_cast<int32_t>(picked_groups[i / kGroup]) * kGroup + i % kGroup;
-        keys[i] = e < n ? key_of(order_of(static_cast<float>(row[e])), begin + e) : 0;
+        for (int32_t j = 0; j < listed; ++j) better += list[j] > k;
+        if (better < K) picked_groups[better] = ~static_cast<uint32_t>(k);
     }
     if (tid == 0) wave_sums[0] = {r.high, log_z, 0.0f};
     __syncthreads();
     log_z = wave_sums[0].z;
-    uint64_t* best = a.best ? a.best + (a.row0 * a.parts + blockIdx.x) * K : nullptr;
+    // Their elements that are no worse than the K-th group's largest, wherever that lies in it; of those the K best.
+    const int32_t last = picked_groups[kept - 1];
+    const uint64_t bar = kept < K ? 1 : key_of(order_of(groups[last]), begin + end_of(last) - 1);
     for (int32_t i = tid; i < kept * kGroup; i += THREADS) {
+        const int32_t q = picked_groups[i / kGroup], e = first_of(q) + i % kGroup;
+        if (e >= end_of(q)) continue;
+        const uint64_t k = key_of(order_of(static_cast<float>(row[e])), begin + e);
+        if (k >= bar) keys[atomicAdd(&counts[1], 1u)] = k;
+    }
+    __syncthreads();
+    const int32_t found = counts[1];
+    uint64_t* best = a.best ? a.best + (a.row0 * a.parts + blockIdx.x) * K : nullptr;
+    for (int32_t i = tid; i < found; i += THREADS) {
         const uint64_t k = keys[i];
         int32_t better = 0;
-        for (int32_t j = 0; j < kept * kGroup; ++j) better += keys[j] > k;
-        if (better >= K || !k) continue;
+        for (int32_t j = 0; j < found; ++j) better += keys[j] > k;
+        if (better >= K) continue;
         if (best) best[better] = k;
         else write_top(a, t, better, k, r.high, log_z);
     }
@@ -287,7 +354,9 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
         for (int32_t i = n + tid; i < K; i += THREADS) best[i] = 0;
 }
 
-// A wave joins the parts of a row.
+// A wave joins the parts of a row, their lists in shared memory unless there are too many.
+constexpr int32_t kJoinHeld = 8192;
+static_assert(kMostTop <= LD_WAVE, "a lane writes an alternative");
 template <int DT>
 __global__ __launch_bounds__(LD_WAVE) void k_score_join(ScoreArgs a) {
     constexpr int kEach = (LD_MAX_VOCAB / kMostPart + LD_WAVE - 1) / LD_WAVE;
@@ -314,15 +383,23 @@ __global__ __launch_bounds__(LD_WAVE) void k_score_join(ScoreArgs a) {
     if (a.top == 0) return;
     log_z = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(log_z)));
     // Every lane holds the next of up to kEach parts' lists; the best of all is written, and its list moves on.
-    const uint64_t* best = a.best + t * a.parts * a.top;
+    extern __shared__ uint64_t lists[];
+    const int32_t all = a.parts * a.top;
+    const uint64_t* best = a.best + t * all;
+    const bool held = all <= kJoinHeld;
+    if (held)
+        for (int32_t i = lane; i < all; i += LD_WAVE) lists[i] = best[i];
+    __syncthreads();
+    const auto entry = [&](int32_t i) { return held ? lists[i] : best[i]; };
     uint64_t next[kEach];
     int32_t used[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int32_t p = lane + i * LD_WAVE;
         used[i] = 0;
-        next[i] = p < a.parts ? best[static_cast<int64_t>(p) * a.top] : 0;
+        next[i] = p < a.parts ? entry(p * a.top) : 0;
     }
+    uint64_t kept = 0;
     for (int32_t k = 0; k < a.top; ++k) {
         uint64_t mine = next[0];
 #pragma unroll
@@ -330,14 +407,15 @@ __global__ __launch_bounds__(LD_WAVE) void k_score_join(ScoreArgs a) {
         const uint32_t hi = wave_max(static_cast<uint32_t>(mine >> 32));
         const uint32_t lo = wave_max(static_cast<uint32_t>(mine >> 32) == hi ? static_cast<uint32_t>(mine) : 0u);
         const uint64_t winner = static_cast<uint64_t>(hi) << 32 | lo;
-        if (lane == 0) write_top(a, t, k, winner, most, log_z);
+        if (lane == k) kept = winner;
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (next[i] == winner && winner) {
+            if (next[i] == winner) {
                 const int32_t p = lane + i * LD_WAVE;
-                next[i] = ++used[i] < a.top ? best[static_cast<int64_t>(p) * a.top + used[i]] : 0;
+                next[i] = ++used[i] < a.top ? entry(p * a.top + used[i]) : 0;
             }
     }
+    if (lane < a.top) write_top(a, t, lane, kept, most, log_z);
 }
 
 struct GradArgs {
@@ -350,66 +428,89 @@ struct GradArgs {
     void* out;
     int64_t stride, out_stride, d_logprob_stride, d_entropy_stride;
     int64_t row0;
-    int32_t V, chunks;
+    uint32_t pieces, chunks;   // of the launch, and of a row
+    int32_t V;
     float scale;
     int32_t wide_ids;
 };
 
-constexpr int kGradUnroll = 4;
+// A thread's elements side by side: 16 bytes of the gradient, so that a wave writes whole lines.
+template <int OT> constexpr int grad_group() { return OT == LD_F32 ? 4 : 8; }
+// Elements of a thread: few, of many threads (16384 x 50257 in bf16 529 us with 16, 576 with 32, 605 with 64, 647 with 8; fp32 to fp32 1138
+// with 16, 1045 with 8).
+template <int DT, int OT> constexpr int grad_elems() { return DT == LD_F32 && OT == LD_F32 ? 8 : 16; }
+// Consecutive chunks that an XCD takes: 517 us in runs of 16 and 64, 527 of 4, 534 one by one.
+constexpr uint32_t kGradRun = 16;
+constexpr int32_t kLine = 128;
 
 template <int OT>
-__device__ __forceinline__ void store_group(typename LdElem<OT>::type* p, const f32x8& y) {
-    if constexpr (OT == LD_F32) {
-        typedef LdVec<LD_F32, 4> V;
-        __builtin_nontemporal_store(typename V::type(__builtin_shufflevector(y, y, 0, 1, 2, 3)), reinterpret_cast<typename V::type*>(p));
-        __builtin_nontemporal_store(typename V::type(__builtin_shufflevector(y, y, 4, 5, 6, 7)), reinterpret_cast<typename V::type*>(p + 4));
-    } else {
-        typedef LdVec<OT, 8> V;
-        __builtin_nontemporal_store(V::narrow(y), reinterpret_cast<typename V::type*>(p));
-    }
+__device__ __forceinline__ void store_streamed(typename LdElem<OT>::type* p, const float (&y)[grad_group<OT>()]) {
+    typedef float wide __attribute__((ext_vector_type(grad_group<OT>())));
+    typedef typename LdElem<OT>::type narrow __attribute__((ext_vector_type(grad_group<OT>())));
+    wide x;
+#pragma unroll
+    for (int e = 0; e < grad_group<OT>(); ++e) x[e] = y[e];
+    __builtin_nontemporal_store(__builtin_convertvector(x, narrow), reinterpret_cast<narrow*>(p));
 }
 
-// A chunk of a row. Every element is read and written by one thread, so that the gradient may take the logits' place.
+// A chunk of a row. Every element is read and written by one thread, so that the gradient may take the logits' place. Groups begin where
+// the gradient's lines do: those elements before the first and behind the last that are fewer go one by one.
 template <int DT, int OT, int THREADS, bool ENTROPY>
 __global__ __launch_bounds__(THREADS) void k_score_grad(GradArgs a) {
     typedef typename LdElem<DT>::type elem;
     typedef typename LdElem<OT>::type out_elem;
-    constexpr int32_t kChunk = THREADS * kGroup * kGradUnroll;
-    const int64_t t = a.row0 + blockIdx.x / a.chunks;
-    const int32_t begin = blockIdx.x % a.chunks * kChunk, n = min(a.V - begin, kChunk);
-    const elem* row = static_cast<const elem*>(a.logits) + t * a.stride + begin;
-    out_elem* out = static_cast<out_elem*>(a.out) + t * a.out_stride + begin;
+    constexpr int N = grad_group<OT>(), kUnroll = grad_elems<DT, OT>() / N, kChunk = THREADS * grad_elems<DT, OT>();
+    typedef LdVec<DT, N> V;
+    const uint32_t piece = ld_xcd_piece<kGradRun>(blockIdx.x, gridDim.x);
+    if (piece >= a.pieces) return;
+    const int64_t t = a.row0 + piece / a.chunks;
+    out_elem* out = static_cast<out_elem*>(a.out) + t * a.out_stride;
+    const elem* row = static_cast<const elem*>(a.logits) + t * a.stride;
+    const int32_t head = min(to_boundary(out, kLine / static_cast<int32_t>(sizeof(out_elem))), a.V), chunk = piece % a.chunks, begin = head + chunk * kChunk;
     const float high = a.stats[2 * t], log_z = a.stats[2 * t + 1];  // the largest logit, L
-    const bool empty = high == -__builtin_huge_valf();
-    int64_t id = a.ids ? id_at(a.ids, t, a.wide_ids) : -1;
+    const int64_t id = a.ids ? id_at(a.ids, t, a.wide_ids) : -1;
     const bool inside = id >= 0 && id < a.V;
     const float g = inside ? a.scale * a.d_logprob[t * a.d_logprob_stride] : 0.0f;
-    const int32_t named = inside && id >= begin && id < begin + n ? static_cast<int32_t>(id - begin) : -1;
+    const int32_t named = inside ? static_cast<int32_t>(id) : -1;
     const float h = ENTROPY ? a.scale * a.d_entropy[t * a.d_entropy_stride] : 0.0f, entropy = ENTROPY ? a.entropy[t] : 0.0f;
-    const auto at = [&](float x, int32_t i) {
+    const auto at = [&](float x) {  // without what the token named gets
         const float logp = __fmaf_rn(x - high, a.scale, -log_z), p = __builtin_amdgcn_exp2f(logp * kLog2e);
-        float d = (i == named ? g : 0.0f) - p * g;
-        if (ENTROPY) d -= p > 0.0f ? h * (p * (logp + entropy)) : 0.0f;
-        return empty ? 0.0f : d;
+        if (ENTROPY) return p > 0.0f ? -p * __fmaf_rn(h, logp + entropy, g) : -p * g;
+        return -p * g;
     };
-    const int32_t whole = n / kGroup;
-    f32x8 x[kGradUnroll];
+    const auto one = [&](int32_t i) {
+        float y = at(static_cast<float>(row[i]));
+        if (i == named) y += g;
+        out[i] = static_cast<out_elem>(y);
+    };
+    if (high == -__builtin_huge_valf()) {  // nothing is left
+        for (int32_t i = (chunk == 0 ? 0 : begin) + threadIdx.x; i < min(a.V, begin + kChunk); i += THREADS) out[i] = static_cast<out_elem>(0.0f);
+        return;
+    }
+    if (chunk == 0 && static_cast<int32_t>(threadIdx.x) < head) one(threadIdx.x);
+    const int32_t whole = min(a.V - begin, kChunk) / N;
+    typename V::type x[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kGradUnroll; ++u) {
+    for (int u = 0; u < kUnroll; ++u) {
         const int32_t q = threadIdx.x + u * THREADS;
-        if (q < whole) x[u] = load_group<DT>(row + q * kGroup);
+        if (q < whole) x[u] = *reinterpret_cast<const typename V::type*>(row + begin + q * N);
     }
 #pragma unroll
-    for (int u = 0; u < kGradUnroll; ++u) {
-        const int32_t q = threadIdx.x + u * THREADS;
+    for (int u = 0; u < kUnroll; ++u) {
+        const int32_t q = threadIdx.x + u * THREADS, first = begin + q * N;
         if (q >= whole) continue;
-        f32x8 y;
+        float y[N];
 #pragma unroll
-        for (int e = 0; e < kGroup; ++e) y[e] = at(x[u][e], q * kGroup + e);
-        store_group<OT>(out + q * kGroup, y);
+        for (int e = 0; e < N; ++e) y[e] = at(static_cast<float>(x[u][e]));
+        const int32_t own = named - first;
+        if (static_cast<uint32_t>(own) < static_cast<uint32_t>(N)) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = e == own ? y[e] + g : y[e];
+        }
+        store_streamed<OT>(out + first, y);
     }
-    const int32_t rest = whole * kGroup + static_cast<int32_t>(threadIdx.x);
-    if (rest < n) out[rest] = static_cast<out_elem>(at(static_cast<float>(row[rest]), rest));
+    const int32_t end = begin + whole * N + static_cast<int32_t>(threadIdx.x);
+    if (whole < kChunk / N && end < a.V) one(end);
 }
 
 // How a call splits its rows.
@@ -418,9 +519,9 @@ struct Split {
     bool narrow;
 };
 Split split_of(int64_t T, int32_t V) {
-    if (V <= kNarrowElems && T >= kWorkgroups) return {V, 1, true};
+    if (V <= kNarrowElems && T >= kWorkgroups / 2) return {V, 1, true};
     const int32_t most = (V + kPartStep - 1) / kPartStep, least = (V + kMostPart - 1) / kMostPart;
-    int64_t parts = T > 0 ? (kWorkgroups + T - 1) / T : 1;
+    int64_t parts = T > 0 && T < kWorkgroups / 2 ? (kWorkgroups + T - 1) / T : 1;
     parts = parts > most ? most : parts < least ? least : parts;
     if (parts > LD_MAX_VOCAB / kMostPart) parts = LD_MAX_VOCAB / kMostPart;  // few rows of very many columns
     const int32_t part = static_cast<int32_t>((most + parts - 1) / parts) * kPartStep;
@@ -462,9 +563,10 @@ extern "C" ld_status ld_token_logprob(const void* logits, int64_t T, int32_t V, 
     float4* sums = sp.parts > 1 ? static_cast<float4*>(workspace) : nullptr;
     uint64_t* best = sums && top ? reinterpret_cast<uint64_t*>(sums + T * sp.parts) : nullptr;
     const int32_t threads = sp.narrow ? kNarrow : kWide;
-    // maxima of the groups, and the list of those that `top` threads hold
-    const int32_t n_groups = (sp.part + kGroup - 1) / kGroup, of_thread = (n_groups + threads - 1) / threads;
-    const size_t shared = top ? (n_groups + static_cast<size_t>(n_groups < top * of_thread ? n_groups : top * of_thread)) * sizeof(uint32_t) : 0;
+    // maxima of the groups, with one more where rows do not begin at a boundary, and the list of those that `top` threads hold
+    const int32_t n_groups = sp.part / kGroup + 2, of_thread = (n_groups + threads - 1) / threads + 1;
+    const size_t shared = top ? (n_groups + 1) / 2 * 2 * sizeof(float) + static_cast<size_t>(n_groups < top * of_thread ? n_groups : top * of_thread) * sizeof(uint64_t) : 0;
+    const size_t join_shared = sp.parts * top <= kJoinHeld ? static_cast<size_t>(sp.parts) * top * sizeof(uint64_t) : 0;
     const int64_t most = ld_workgroups(static_cast<int64_t>(1) << 40, threads) / sp.parts;  // rows of a launch
     for (int64_t t = 0; t < T; t += most) {
         const int64_t rows = T - t < most ? T - t : most;
@@ -487,7 +589,7 @@ extern "C" ld_status ld_token_logprob(const void* logits, int64_t T, int32_t V, 
         });
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
         if (sp.parts == 1) continue;
-        ld_with_type(dtype, [&](auto type) { k_score_join<type><<<dim3(static_cast<uint32_t>(rows)), dim3(LD_WAVE), 0, st>>>(a); });
+        ld_with_type(dtype, [&](auto type) { k_score_join<type><<<dim3(static_cast<uint32_t>(rows)), dim3(LD_WAVE), join_shared, st>>>(a); });
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
     }
     return LD_OK;
@@ -510,14 +612,16 @@ extern "C" ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_
         return LD_ERR_ALIGN;
     ld_begin_call();
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const bool narrow = V <= kNarrow * kGroup * kGradUnroll;
-    const int32_t threads = narrow ? kNarrow : kWide, chunk = threads * kGroup * kGradUnroll, chunks = (V + chunk - 1) / chunk;
-    const int64_t most = ld_workgroups(static_cast<int64_t>(1) << 40, threads) / chunks;
+    const int32_t elems = dtype == LD_F32 && out_dtype == LD_F32 ? grad_elems<LD_F32, LD_F32>() : grad_elems<LD_BF16, LD_BF16>();
+    const bool narrow = V <= kNarrow * elems;
+    const int32_t threads = narrow ? kNarrow : kWide, chunk = threads * elems, chunks = (V + chunk - 1) / chunk;
+    const int64_t most = (ld_workgroups(static_cast<int64_t>(1) << 40, threads) - 7) / chunks;
     for (int64_t t = 0; t < T; t += most) {
         const int64_t rows = T - t < most ? T - t : most;
+        const uint32_t pieces = static_cast<uint32_t>(rows * chunks);
         const GradArgs a = {logits, ids, stats, d_logprob, entropy, d_entropy, d_logits, stride, out_stride, d_logprob_stride,
-                            d_entropy_stride, t, V, chunks, scale, id_dtype == LD_I64};
-        const dim3 grid(static_cast<uint32_t>(rows * chunks));
+                            d_entropy_stride, t, pieces, static_cast<uint32_t>(chunks), V, scale, id_dtype == LD_I64};
+        const dim3 grid((pieces + 7) / 8 * 8);
         ld_with_type(dtype, [&](auto type) {
             ld_with_type(out_dtype, [&](auto out_type) {
                 if (narrow && entropy) k_score_grad<type, out_type, kNarrow, true><<<grid, dim3(kNarrow), 0, st>>>(a);
