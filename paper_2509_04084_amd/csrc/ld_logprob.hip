@@ -171,6 +171,36 @@ __device__ __forceinline__ int32_t rank_in_wave(uint64_t key) {
     }
     return rank;
 }
+// The K-th largest of all threads' keys (0: nothing), in every thread. Up to kFewTop the K largest of every wave one after
+// another, and of those by counting (16384 x 32000 with five alternatives 213 -> 204 us); else every key's rank. `keys`: 256 of them.
+constexpr int32_t kFewTop = 8;
+template <int THREADS>
+__device__ __forceinline__ uint64_t kth_of_few(uint64_t key, int32_t K, uint64_t* keys) {
+    constexpr int kWaves = THREADS / LD_WAVE;
+    uint64_t kept = 0;  // of lane k the wave's k-th largest
+    for (int32_t k = 0; k < K; ++k) {
+        const uint32_t hi = wave_max(static_cast<uint32_t>(key >> 32));
+        const uint32_t lo = wave_max(static_cast<uint32_t>(key >> 32) == hi ? static_cast<uint32_t>(key) : 0u);
+        const uint64_t best = static_cast<uint64_t>(hi) << 32 | lo;
+        if (ld_lane() == k) kept = best;
+        if (key == best) key = 0;
+    }
+    if (kWaves == 1) return static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<int>(kept >> 32), K - 1)) << 32 |
+                            static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(kept), K - 1));
+    if (ld_lane() < K) keys[threadIdx.x / LD_WAVE * K + ld_lane()] = kept;
+    __syncthreads();
+    // Each wave for itself: lane i holds the i-th of the kWaves K candidates.
+    const int32_t n = kWaves * K;
+    const uint64_t mine = ld_lane() < n ? keys[ld_lane()] : 0;
+    int32_t rank = 0;
+    for (int32_t j = 0; j < n; ++j) rank += keys[j] > mine;
+    const uint64_t found = __ballot(mine != 0 && rank == K - 1);
+    if (!found) return 0;
+    const int32_t lane = __builtin_ctzll(found);
+    return static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<int>(mine >> 32), lane)) << 32 |
+           static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(mine), lane));
+}
+
 // How many of 64 keys in falling order are larger than `key`.
 __device__ __forceinline__ int32_t larger_among(const uint64_t* sorted, uint64_t key) {
     int32_t n = 0;
@@ -300,32 +330,45 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
     const int32_t K = a.top;
     const uint64_t mine = tid < n_body || (headed && tid == 0) ? key_of(order, at) : 0;
     if (tid == 0) counts[0] = counts[1] = 0, kth = 0;
-    int32_t rank = rank_in_wave(mine);
-    __syncthreads();
-    if (kWaves > 1) {
-        if (mine) keys[wave * LD_WAVE + rank] = mine;
-        else keys[tid] = 0;  // lanes without a group are a wave's last
+    const bool single = n_groups <= THREADS && !headed;  // a thread has one group at most: its rank is the group's
+    uint64_t least;
+    if (K <= kFewTop && !single) {
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w)
-            if (w != wave) rank += larger_among(keys + w * LD_WAVE, mine);
+        least = kth_of_few<THREADS>(mine, K, keys);
+    } else {
+        int32_t rank = rank_in_wave(mine);
+        __syncthreads();
+        if (kWaves > 1) {
+            if (mine) keys[wave * LD_WAVE + rank] = mine;
+            else keys[tid] = 0;  // lanes without a group are a wave's last
+            __syncthreads();
+            rank = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) rank += larger_among(keys + w * LD_WAVE, mine);
+        }
+        if (single && rank < K && mine) picked_groups[rank] = at;
+        if (rank == K - 1 && mine) kth = mine;
+        __syncthreads();
+        least = kth;
     }
-    if (rank == K - 1 && mine) kth = mine;
-    __syncthreads();
     // Groups of those threads that are no worse, behind the maxima; of them the K best.
-    const uint64_t least = kth;
     uint64_t* list = reinterpret_cast<uint64_t*>(groups + (n_groups + 1) / 2 * 2);
-    if (mine >= least && mine)
-        own_groups([&](int32_t q) {
-            const uint64_t k = key_of(order_of(groups[q]), q);
-            if (k >= least) list[atomicAdd(&counts[0], 1u)] = k;
-        });
-    __syncthreads();
-    const int32_t listed = counts[0], kept = min(listed, K);
-    for (int32_t i = tid; i < listed; i += THREADS) {
-        const uint64_t k = list[i];
-        int32_t better = 0;
-        for (int32_t j = 0; j < listed; ++j) better += list[j] > k;
-        if (better < K) picked_groups[better] = ~static_cast<uint32_t>(k);
+    int32_t kept = min(n_groups, K);
+    if (!single) {
+        if (mine >= least && mine)
+            own_groups([&](int32_t q) {
+                const uint64_t k = key_of(order_of(groups[q]), q);
+                if (k >= least) list[atomicAdd(&counts[0], 1u)] = k;
+            });
+        __syncthreads();
+        const int32_t listed = counts[0];
+        kept = min(listed, K);
+        for (int32_t i = tid; i < listed; i += THREADS) {
+            const uint64_t k = list[i];
+            int32_t better = 0;
+            for (int32_t j = 0; j < listed; ++j) better += list[j] > k;
+            if (better < K) picked_groups[better] = ~static_cast<uint32_t>(k);
+        }
     }
     if (tid == 0) wave_sums[0] = {r.high, log_z, 0.0f};
     __syncthreads();
@@ -362,33 +405,47 @@ __global__ __launch_bounds__(LD_WAVE) void k_score_join(ScoreArgs a) {
     constexpr int kEach = (LD_MAX_VOCAB / kMostPart + LD_WAVE - 1) / LD_WAVE;
     const int64_t t = a.row0 + blockIdx.x;
     const float4* sums = a.sums + t * a.parts;
-    const int32_t lane = threadIdx.x;
+    const int32_t lane = threadIdx.x, all = a.parts * a.top;
     const float c = a.scale * kLog2e;
+    // All that is read is on its way before any of it is used.
+    extern __shared__ uint64_t lists[];
+    const uint64_t* best = a.best + t * all;
+    const bool held = all <= kJoinHeld;
+    constexpr int kHeldEach = 8;
+    uint64_t some[kHeldEach];
+    if (held)
+#pragma unroll
+        for (int i = 0; i < kHeldEach; ++i) some[i] = lane + i * LD_WAVE < all ? best[lane + i * LD_WAVE] : 0;
+    float4 part[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int32_t p = lane + i * LD_WAVE;
+        part[i] = p < a.parts ? sums[p] : make_float4(-__builtin_huge_valf(), 0.0f, 0.0f, 0.0f);
+    }
+    bool inside;
+    const float picked = picked_of<DT>(a, t, inside);
+    if (held) {
+#pragma unroll
+        for (int i = 0; i < kHeldEach; ++i)
+            if (lane + i * LD_WAVE < all) lists[lane + i * LD_WAVE] = some[i];
+        for (int32_t i = lane + kHeldEach * LD_WAVE; i < all; i += LD_WAVE) lists[i] = best[i];
+    }
     uint32_t high = 0;
-    for (int32_t p = lane; p < a.parts; p += LD_WAVE) high = max(high, order_of(sums[p].x));
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) high = max(high, order_of(part[i].x));
     const float most = value_of(wave_max(high));
     float z = 0.0f, s = 0.0f;
-    for (int32_t p = lane; p < a.parts; p += LD_WAVE) {
-        const float4 x = sums[p];
-        const Sums r = moved({x.x, x.y, x.z}, most, c);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const Sums r = moved({part[i].x, part[i].y, part[i].z}, most, c);
         z += r.z, s += r.s;
     }
     const Sums r = {most, wave_sum(z), wave_sum(s)};
     float log_z = 0.0f;
-    if (lane == 0) {
-        bool inside;
-        const float x = picked_of<DT>(a, t, inside);
-        log_z = finish(a, t, r, x, inside);
-    }
+    if (lane == 0) log_z = finish(a, t, r, picked, inside);
     if (a.top == 0) return;
     log_z = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(log_z)));
     // Every lane holds the next of up to kEach parts' lists; the best of all is written, and its list moves on.
-    extern __shared__ uint64_t lists[];
-    const int32_t all = a.parts * a.top;
-    const uint64_t* best = a.best + t * all;
-    const bool held = all <= kJoinHeld;
-    if (held)
-        for (int32_t i = lane; i < all; i += LD_WAVE) lists[i] = best[i];
     __syncthreads();
     const auto entry = [&](int32_t i) { return held ? lists[i] : best[i]; };
     uint64_t next[kEach];
