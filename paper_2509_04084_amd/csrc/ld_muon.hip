@@ -540,38 +540,50 @@ __global__ __launch_bounds__(kThreads) void k_squares(Batch b, Source s) {
     if (threadIdx.x == 0) s.sums[i * kSumParts + blockIdx.x] = sum;
 }
 
-// X and its transposed from the update: 64 by 64 elements a workgroup, zeros behind its edges.
+// X and its transposed from the update: 64 by 64 elements a workgroup, zeros behind its edges. Rows are written as they are loaded,
+// columns by way of shared memory; the elements are on their way while the partial sums are added up.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void k_lay_out(Batch b, Source s, float scale) {
-    __shared__ float tile[kMuonPad][kMuonPad + 1];
+    constexpr int kStride = kMuonPad + 2, kEach = kMuonPad * kMuonPad / 8 / kThreads;
+    __shared__ float tile[kMuonPad * kStride];
     __shared__ double sh[kThreads / LD_WAVE];
     typedef typename LdElem<DT>::type elem;
     const int32_t i = blockIdx.y, rows = user_rows(b, i), cols = user_cols(b, i);
     const int32_t across = (cols + kMuonPad - 1) / kMuonPad, r0 = static_cast<int32_t>(blockIdx.x) / across * kMuonPad, c0 = static_cast<int32_t>(blockIdx.x) % across * kMuonPad;
     if (r0 >= rows) return;
+    const elem* src = static_cast<const elem*>(s.src[i]);
+    const int64_t stride = s.stride[i];
+    f32x8 x[kEach];
+#pragma unroll
+    for (int p = 0; p < kEach; ++p) {
+        const int32_t n = p * kThreads + threadIdx.x, r = r0 + n / 8, c = c0 + n % 8 * 8;
+        x[p] = r < rows && c < cols ? load_eight<DT>(src + r * stride + c, cols - c) : f32x8(0.0f);
+    }
     const int32_t parts = sum_parts(static_cast<int64_t>(rows) * cols);
     const double total = block_sum(static_cast<int32_t>(threadIdx.x) < parts ? s.sums[i * kSumParts + threadIdx.x] : 0.0, sh);
     const double norm = sqrt(total);
     const double f = norm == 0.0 ? 0.0 : static_cast<double>(scale) / (norm + static_cast<double>(s.eps));
-    const elem* src = static_cast<const elem*>(s.src[i]);
-    const int64_t stride = s.stride[i];
-    for (int32_t e = threadIdx.x; e < kMuonPad * kMuonPad; e += kThreads) {
-        const int32_t r = e / kMuonPad, c = e % kMuonPad;
-        float x = 0.0f;
-        if (r0 + r < rows && c0 + c < cols) x = static_cast<float>(static_cast<double>(static_cast<float>(src[(r0 + r) * stride + c0 + c])) * f);
-        tile[r][c] = x;
-    }
-    __syncthreads();
     char* straight = buffer_of(b, i, b.flipped[i] ? kXT : kX);
     char* turned = buffer_of(b, i, b.flipped[i] ? kX : kXT);
     const int64_t all_rows = padded(rows), all_cols = padded(cols);
-    for (int32_t p = threadIdx.x; p < kMuonPad * kMuonPad / 8; p += kThreads) {
-        const int32_t r = p / 8, c = p % 8 * 8;
-        f32x8 x, y;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = tile[r][c + e], y[e] = tile[c + e][r];
-        store_split(straight, all_rows, r0 + r, (c0 + c) >> 3, x);
-        store_split(turned, all_cols, c0 + r, (r0 + c) >> 3, y);
+    for (int p = 0; p < kEach; ++p) {
+        const int32_t n = p * kThreads + threadIdx.x, r = n / 8, c = n % 8 * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[p][e] = static_cast<float>(static_cast<double>(x[p][e]) * f);
+            tile[r * kStride + c + e] = x[p][e];
+        }
+        store_split(straight, all_rows, r0 + r, (c0 + c) >> 3, x[p]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < kEach; ++p) {
+        const int32_t n = p * (kThreads / 4) + (threadIdx.x >> 2), c = n % kMuonPad, r = n / kMuonPad * 32 + (threadIdx.x & 3) * 8;
+        f32x8 y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = tile[(r + e) * kStride + c];
+        store_split(turned, all_cols, c0 + c, (r0 + r) >> 3, y);
     }
 }
 
@@ -597,6 +609,7 @@ struct MomentumArgs {
     float mu;
     int32_t nesterov;
 };
+constexpr int kTogether = 4;  // steps between which the momentum stays in registers
 template <int DT>
 __global__ __launch_bounds__(kThreads) void k_momentum(Batch b, MomentumArgs a) {
     __shared__ double sh[kThreads / LD_WAVE];
@@ -607,25 +620,34 @@ __global__ __launch_bounds__(kThreads) void k_momentum(Batch b, MomentumArgs a) 
     if (static_cast<int32_t>(blockIdx.x) >= parts) return;
     float* momentum = a.momentum[blockIdx.y];
     const int64_t from = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 8, step = static_cast<int64_t>(parts) * kThreads * 8;
-    for (int32_t t = 0; t < steps; ++t) {
-        const elem* grad = static_cast<const elem*>(a.grad[p0 + t]);
-        float* update = reinterpret_cast<float*>(buffer_of(b, p0 + t, kYT));
-        double sum = 0.0;
+    for (int32_t t0 = 0; t0 < steps; t0 += kTogether) {
+        double sum[kTogether] = {};
         for (int64_t e = from; e < elems; e += step) {
             const int32_t n = elems - e < 8 ? static_cast<int32_t>(elems - e) : 8;
-            const f32x8 g = load_eight<DT>(grad + e, n);
-            f32x8 m = load_eight<LD_F32>(momentum + e, n), u;
+            f32x8 m = load_eight<LD_F32>(momentum + e, n), g[kTogether];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                m[k] = __fmaf_rn(a.mu, m[k], g[k]);
-                u[k] = a.nesterov ? __fmaf_rn(a.mu, m[k], g[k]) : m[k];
-                if (k < n) sum = fma(static_cast<double>(u[k]), static_cast<double>(u[k]), sum);
+            for (int k = 0; k < kTogether; ++k)
+                if (t0 + k < steps) g[k] = load_eight<DT>(static_cast<const elem*>(a.grad[p0 + t0 + k]) + e, n);
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {
+                if (t0 + k >= steps) break;
+                f32x8 u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    m[i] = __fmaf_rn(a.mu, m[i], g[k][i]);
+                    u[i] = a.nesterov ? __fmaf_rn(a.mu, m[i], g[k][i]) : m[i];
+                    if (i < n) sum[k] = fma(static_cast<double>(u[i]), static_cast<double>(u[i]), sum[k]);
+                }
+                store_eight(reinterpret_cast<float*>(buffer_of(b, p0 + t0 + k, kYT)) + e, u, n);
             }
             store_eight(momentum + e, m, n);
-            store_eight(update + e, u, n);
         }
-        sum = block_sum(sum, sh);
-        if (threadIdx.x == 0) a.sums[(p0 + t) * kSumParts + blockIdx.x] = sum;
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            if (t0 + k >= steps) break;
+            const double all = block_sum(sum[k], sh);
+            if (threadIdx.x == 0) a.sums[(p0 + t0 + k) * kSumParts + blockIdx.x] = all;
+        }
     }
 }
 
