@@ -2,7 +2,8 @@
 
 Token and position table lie in one flat parameter, the token table is the output head as well. A step is
 
-    lookup -> head and loss (torch) -> gradient of both tables -> clipping -> top-k with error feedback -> update
+    lookup -> head (torch) -> log probabilities and their gradient -> gradient of both tables -> clipping
+    -> top-k with error feedback -> update
 
 and what the last two make is the differential checkpoint of the step. At the end the model is recovered from the
 initial weights and the differentials, and compared with the trained one bit for bit:
@@ -34,6 +35,7 @@ def train(steps=40, vocab=499, width=96, context=32, batch=16, lr=4.0, max_norm=
     scale = math.sqrt(width)
     positions = torch.arange(context, device=device).repeat(batch, 1)
     norm, losses, norms, idx, val = torch.zeros(1, device=device), [], [], [], []
+    weight = torch.tensor(-1.0 / (batch * context), device=device)
     for step in range(steps):
         ids = torch.empty(batch, context + 1, dtype=torch.int64, device=device)
         ids[:, 0] = torch.randint(0, vocab, (batch,), generator=gen, device=device)
@@ -42,12 +44,13 @@ def train(steps=40, vocab=499, width=96, context=32, batch=16, lr=4.0, max_norm=
         tokens, wanted = ids[:, :-1].contiguous(), ids[:, 1:].reshape(-1)
 
         x = ld.ld_embed_lookup(wte, tokens, scale, wpe, positions).view(-1, width)
-        p = torch.softmax(x @ wte.t(), dim=1)
-        losses.append(float(-p.gather(1, wanted[:, None]).clamp_min(1e-30).log().mean()))
-        p[torch.arange(p.shape[0], device=device), wanted] -= 1.0
-        p /= p.shape[0]
-        dx = p @ wte
-        torch.mm(p.t(), x, out=d_wte)                                        # the head's share,
+        logits = x @ wte.t()
+        said = ld.ld_token_logprob(logits, wanted)
+        losses.append(-float(said.logprob.mean()))
+        # of the mean's negative; in the logits' place
+        dy = ld.ld_token_logprob_grad(logits, said.stats, wanted, weight.expand_as(wanted), out=logits)
+        dx = dy @ wte
+        torch.mm(dy.t(), x, out=d_wte)                                       # the head's share,
         ld.ld_embed_grad(dx, tokens.view(-1), d_wte, scale, accumulate=True)  # and the lookup's on top of it
         ld.ld_embed_grad(dx, positions.view(-1), d_wpe)
 

@@ -923,6 +923,10 @@ def ld_orthogonalize(mats: Sequence[torch.Tensor], outs: Optional[Sequence[torch
         dp[i], _, ds[i] = _rows(t, "outs", written=True)
         if dp[i] == sp[i] and t.numel() and (t.dtype != first.dtype or ds[i] != ss[i]):
             raise ValueError("outs: in place a matrix keeps its type and stride")
+    source = {int(p): i for i, p in enumerate(sp) if mats[i].numel()}
+    written = [int(p) for i, p in enumerate(dp) if mats[i].numel()]
+    if len(set(written)) < len(written) or any(int(p) in source and dp[i] != sp[i] for i, p in enumerate(dp) if mats[i].numel()):
+        raise ValueError("outs: a tensor stands for two matrices")
     if workspace is None and (need := lib.ld_orthogonalize_workspace(_hp(rows), _hp(cols), n)) > 0:
         workspace = _scratch(need, first.device, stream)
     st = lib.ld_orthogonalize(_hp(sp), _hp(ss), _hp(dp), _hp(ds), _hp(rows), _hp(cols), n, code, _elem(outs[0], "outs"), int(steps),
@@ -965,6 +969,9 @@ def ld_merge_dense_muon(ws: Sequence[torch.Tensor], ms: Sequence[torch.Tensor], 
     _one_device(ws[0], (workspace,), w, m, g)
     wp, mp, gp = w.checked("ws"), m.checked("ms"), g.checked("grads")
     _on_device_of(stream, ws[0])
+    written = [a for p in (wp, mp) for a, k in zip(np.frombuffer(p, np.uint64).tolist(), w.numel().tolist()) if k]
+    if len(set(written)) < len(written):
+        raise ValueError("ws, ms: a tensor stands for two matrices")
     factor = None
     if scale is not None:
         factor = np.ascontiguousarray(np.broadcast_to(np.asarray(scale, dtype=np.float32), (n,)))

@@ -301,6 +301,26 @@ def test_rows_beyond_2_31_elements():
     assert abs(float(x[0, V - 1]) - 1.0) <= 2 ** -7 and abs(float(x[T - 1, 0].float()) + 1 / (V - 1 + math.exp(3.0))) <= 1e-7
 
 
+@pytest.mark.parametrize("V,top", [(1 << 24, 64), (1 << 24, 1), ((1 << 24) - 77, 20), (3000001, 33)])
+def test_the_largest_vocabularies(V, top):
+    """Rows of up to 256 parts; lists that the join holds in shared memory, and more. Against 64 bits on the GPU: L within 28 + 8 A + 280
+    roundings as above, A below 20 here."""
+    g = torch.Generator(device=DEV).manual_seed(V + top)
+    x = (torch.randn(2, V, generator=g, device=DEV) * 2).half()
+    x[1, V - 1] = 11.0
+    ids = torch.tensor([V - 1, 5], device=DEV)
+    got = ld.ld_token_logprob(x, ids, entropy=True, top=top)
+    wide = x.double()
+    lse = torch.logsumexp(wide, dim=1)
+    eL = U * (28 + 160 + 280 + 2 * 20)
+    assert bool(((got.logprob.double() - (wide.gather(1, ids[:, None])[:, 0] - lse)).abs() <= eL + 64 * U).all())
+    p = torch.softmax(wide, dim=1)
+    H = -torch.special.xlogy(p, p).sum(dim=1)
+    assert bool(((got.entropy.double() - H).abs() <= 60 * eL).all())
+    order = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(got.top_ids.long(), order)
+
+
 def test_another_stream_and_a_graph():
     g, T, V = gen(29), 40, 30011
     x, ids = make(T, V, BF16, g).to(DEV), torch.randint(0, V, (T,), generator=g).to(DEV)

@@ -379,6 +379,14 @@ def test_refusals_on_the_gpu():
         ld.ld_orthogonalize([a], [a.t()])
     with pytest.raises(ValueError, match="in place"):
         ld.ld_orthogonalize([torch.zeros(4, 6, device=DEV, dtype=BF16)[:2]] * 0 + [a[:, :3]], [a.view(-1)[:12].view(4, 3)])
+    with pytest.raises(ValueError, match="two matrices"):
+        ld.ld_orthogonalize([a, a.clone()], [a, a])
+    with pytest.raises(ValueError, match="two matrices"):
+        ld.ld_orthogonalize([a, a.clone()], [a.clone(), a])
+    with pytest.raises(ValueError, match="two matrices"):
+        ld.ld_merge_dense_muon([a, a], [a.clone(), a.clone()], [[a.clone(), a.clone()]], 0.1)
+    with pytest.raises(ValueError, match="two matrices"):
+        ld.ld_merge_dense_muon([a], [a], [[a.clone()]], 0.1)
     with pytest.raises(ld.LowDiffError):
         ld.ld_orthogonalize([a], workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
     with pytest.raises(TypeError):
