@@ -8,7 +8,7 @@
 // coefficients bound. A run of steps works on the Gram matrix alone: with P = a I + b A + c A^2, A' = P A P and Q' = P Q, all of m by
 // m, symmetric and commuting, so that half of each is computed and mirrored; X is read for its Gram matrix and multiplied by Q once a
 // run (ld_muon_shape.h says when a run ends, and why): 6 m^2 n + 14 m^3 products' operations for five steps of a wide matrix instead of
-// 15 m^2 n + 5 m^3 (symmetric halves there too).
+// 15 m^2 n + 5 m^3 (symmetric halves there too). Matrices of up to 64 rows go a way of their own, in 64 bits.
 //
 // In memory a matrix lies as blocks of 32 columns, in each of them row after row: 32 upper halves, 32 lower halves, 128 bytes, whose eight
 // 16-byte pieces are permuted by the row, as shared memory wants them: a tile's block is contiguous, and is copied into shared memory as it is.
@@ -338,12 +338,9 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_symmetric(Batch batch,
             if (a.poly) {
                 const char* block = held + (c >> 5) * T::ROWS * kMuonRowBytes;
                 const f32x8 g = __builtin_convertvector(fragment(block, r, way.piece), f32x8) + __builtin_convertvector(fragment(block, r, way.piece | 4), f32x8);
-                x = a.cc * x + a.cb * g;
-                if (diagonal) {
+                // the terms nearly cancel at singular values of 1: one rounding each, the smaller sums first
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (row == col + e && row < m) x[e] += a.ca;
-                }
+                for (int e = 0; e < 8; ++e) x[e] = __fmaf_rn(a.cc, x[e], __fmaf_rn(a.cb, g[e], diagonal && row == col + e && row < m ? a.ca : 0.0f));
             }
             half8 upper, lower;
             split(x * scale, upper, lower);
@@ -525,7 +522,7 @@ __global__ __launch_bounds__(kThreads) void k_squares(Batch b, Source s) {
     typedef typename LdElem<DT>::type elem;
     const int32_t i = blockIdx.y, rows = user_rows(b, i), cols = user_cols(b, i);
     const int32_t parts = sum_parts(static_cast<int64_t>(rows) * cols);
-    if (static_cast<int32_t>(blockIdx.x) >= parts) return;
+    if (static_cast<int32_t>(blockIdx.x) >= parts || b.kind[i] == kMuonFew) return;
     const elem* src = static_cast<const elem*>(s.src[i]);
     const int64_t stride = s.stride[i];
     const int32_t lanes_log2 = lanes_log2_of(cols), lanes = 1 << lanes_log2, at_once = kThreads >> lanes_log2;
@@ -550,7 +547,7 @@ __global__ __launch_bounds__(kThreads) void k_lay_out(Batch b, Source s, float s
     typedef typename LdElem<DT>::type elem;
     const int32_t i = blockIdx.y, rows = user_rows(b, i), cols = user_cols(b, i);
     const int32_t across = (cols + kMuonPad - 1) / kMuonPad, r0 = static_cast<int32_t>(blockIdx.x) / across * kMuonPad, c0 = static_cast<int32_t>(blockIdx.x) % across * kMuonPad;
-    if (r0 >= rows) return;
+    if (r0 >= rows || b.kind[i] == kMuonFew) return;
     const elem* src = static_cast<const elem*>(s.src[i]);
     const int64_t stride = s.stride[i];
     f32x8 x[kEach];
@@ -584,6 +581,234 @@ __global__ __launch_bounds__(kThreads) void k_lay_out(Batch b, Source s, float s
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = tile[(r + e) * kStride + c];
         store_split(turned, all_cols, c0 + c, (r0 + r) >> 3, y);
+    }
+}
+
+// -------------------------------------------------------------------------------------------------------------------- few rows
+
+// Matrices of at most kMuonFewSide rows, in 64 bits. All steps work on the Gram matrix, which one workgroup holds: a launch for the parts of
+// X X^T, one for all P and Q (the norm is the root of the trace), and one for Q U. In so few rows roundings do not average out before
+// the steps grow them: halves left 4 x 600 up to 5.5e-6 off (relative, Frobenius; products in 32 bits 7.5e-7), this 5e-8, the rounding of
+// the result. Latency is what bounds it, of 3 launches and some 17 products in turn rather than of 17 launches. By halves and so, us:
+// 1 x 768 109 and 31, 32 x 1024 113 and 29, 64 x 64 81 and 65, 64 x 2048 129 and 71, 64 x 65536 1160 and 128, 32 of 64 x 2048 173
+// and 133 (the steps 50 of those of 64 rows, 12 of 16). 128 rows would take eight times the products, and do not fit.
+// An MFMA of 16 by 16 by 4: lane l has row (or column) l & 15 of both operands at column l >> 4, and of the sums column l & 15 and rows
+// (l >> 4) + 4 q.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+constexpr int kFewThreads = 512;
+constexpr int kFewBand = 16, kFewBands = kMuonFewSide / kFewBand, kFewTiles = kFewBands * (kFewBands + 1) / 2;  // tiles on and above the diagonal
+constexpr int kFewTile = kFewBand * kFewBand;
+
+// Columns of X that a part of its Gram matrix is of, by its columns alone: what is added up then does not depend on the rest of a call.
+__host__ __device__ __forceinline__ int32_t few_columns(int32_t n) { return n <= 64 * 128 ? 128 : (n + 64 * 128 - 1) / (64 * 128) * 128; }
+__device__ __forceinline__ char* few_parts(const Batch& b, int32_t i) { return buffer_of(b, i, kXT); }
+__device__ __forceinline__ char* few_q(const Batch& b, int32_t i) { return buffer_of(b, i, kA); }
+// Both fit what a matrix's scratch has for X transposed and for A.
+static_assert(kMuonFewSide == kMuonPad && kFewTiles * kFewTile * 8 <= 128 * kMuonFewSide * 4 && kFewTiles * kFewTile * 8 <= kMuonPad * kMuonPad * 4 + 3 * kMuonPad * kMuonRowBytes &&
+              kMuonFewSide * kMuonFewSide * 8 <= kMuonPad * kMuonPad * 4 + 3 * kMuonPad * kMuonRowBytes, "scratch");
+
+// Eight columns of X from c on, of row r.
+template <int DT>
+__device__ __forceinline__ f32x8 few_load(const typename LdElem<DT>::type* src, int64_t stride, int32_t flipped, int32_t m, int32_t n, int32_t r, int32_t c) {
+    f32x8 x(0.0f);
+    if (r >= m || c >= n) return x;
+    if (!flipped) return load_eight<DT>(src + r * stride + c, n - c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (c + e < n) x[e] = static_cast<float>(src[(c + e) * stride + r]);
+    return x;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void k_few_gram(Batch b, Source s) {
+    constexpr int kWaves = kThreads / LD_WAVE;
+    __shared__ double sums[kWaves][kFewTiles * kFewTile];
+    typedef typename LdElem<DT>::type elem;
+    const int32_t i = blockIdx.y, m = b.m[i], n = b.n[i], lane = ld_lane(), wave = threadIdx.x / LD_WAVE;
+    if (b.kind[i] != kMuonFew) return;
+    const int32_t columns = few_columns(n), from = blockIdx.x * columns, to = n - from < columns ? n : from + columns;
+    if (from >= n) return;
+    const int32_t bands = (m + kFewBand - 1) / kFewBand;
+    f64x4 acc[kFewTiles] = {};
+    for (int32_t c0 = from + wave * 32; c0 < to; c0 += kWaves * 32) {
+        f32x8 x[kFewBands];
+#pragma unroll
+        for (int t = 0; t < kFewBands; ++t)
+            if (t < bands) x[t] = few_load<DT>(static_cast<const elem*>(s.src[i]), s.stride[i], b.flipped[i], m, n, kFewBand * t + (lane & 15), c0 + 8 * (lane >> 4));
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int t = 0, k = 0; t < kFewBands; ++t)
+#pragma unroll
+                for (int u = 0; u <= t; ++u, ++k)
+                    if (t < bands) acc[k] = __builtin_amdgcn_mfma_f64_16x16x4f64(static_cast<double>(x[u][e]), static_cast<double>(x[t][e]), acc[k], 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kFewTiles; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sums[wave][k * kFewTile + q * LD_WAVE + lane] = acc[k][q];
+    __syncthreads();
+    double* out = reinterpret_cast<double*>(few_parts(b, i)) + static_cast<int64_t>(blockIdx.x) * kFewTiles * kFewTile;
+    for (int32_t e = threadIdx.x; e < bands * (bands + 1) / 2 * kFewTile; e += kThreads) {
+        double sum = 0.0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += sums[w][e];
+        out[e] = sum;
+    }
+}
+
+struct FewArgs {
+    int32_t steps;
+    float eps;
+    float coeff[3 * kMuonMaxSteps];
+};
+// Matrices are symmetric: an operand's column is read for its row, so that lanes read side by side, and rows two apart use the same banks.
+__device__ __forceinline__ int32_t few_at(int32_t r, int32_t c) { return r * kMuonFewSide + (c ^ ((r & 1) << 4)); }
+__global__ __launch_bounds__(kFewThreads) void k_few_steps(Batch b, FewArgs a) {
+    constexpr int kWaves = kFewThreads / LD_WAVE, kMine = (2 * kFewTiles + kWaves - 1) / kWaves;
+    __shared__ double A[kMuonFewSide * kMuonFewSide], P[kMuonFewSide * kMuonFewSide], Q[kMuonFewSide * kMuonFewSide], R[kMuonFewSide * kMuonFewSide];
+    const int32_t i = blockIdx.x, m = b.m[i], n = b.n[i], lane = ld_lane(), wave = threadIdx.x / LD_WAVE;
+    if (b.kind[i] != kMuonFew) return;
+    const int32_t bands = (m + kFewBand - 1) / kFewBand, tiles = bands * (bands + 1) / 2;
+    const auto place = [](int32_t k, int32_t& u, int32_t& t) {  // tile k's bands, u <= t
+        t = k < 1 ? 0 : k < 3 ? 1 : k < 6 ? 2 : 3;
+        u = k - t * (t + 1) / 2;
+    };
+    const auto product = [&](const double* left, const double* right, int32_t k) {
+        int32_t u, t;
+        place(k, u, t);
+        f64x4 acc = {};
+        for (int32_t band = 0; band < bands; ++band) {
+            double x[4], y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int32_t c = kFewBand * band + 4 * e + (lane >> 4);
+                x[e] = left[few_at(c, kFewBand * u + (lane & 15))], y[e] = right[few_at(c, kFewBand * t + (lane & 15))];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[e], y[e], acc, 0, 0, 0);
+        }
+        return acc;
+    };
+    // f(value, row, column) of a tile's elements, to both sides of the diagonal
+    const auto keep = [&](double* to, int32_t k, const f64x4& x, auto f) {
+        int32_t u, t;
+        place(k, u, t);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int32_t r = kFewBand * u + (lane >> 4) + 4 * q, c = kFewBand * t + (lane & 15);
+            const double y = f(x[q], r, c);
+            to[few_at(r, c)] = y;
+            if (u != t) to[few_at(c, r)] = y;
+        }
+    };
+    const auto same = [](double x, int32_t, int32_t) { return x; };
+
+    const int32_t columns = few_columns(n), parts = (n + columns - 1) / columns;
+    const double* sums = reinterpret_cast<const double*>(few_parts(b, i));
+    for (int32_t k = wave; k < tiles; k += kWaves) {
+        f64x4 x = {};
+#pragma unroll 4
+        for (int32_t p = 0; p < parts; ++p)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] += sums[(static_cast<int64_t>(p) * kFewTiles + k) * kFewTile + q * LD_WAVE + lane];
+        keep(A, k, x, same);
+    }
+    __syncthreads();
+    double trace = lane < m ? A[few_at(lane, lane)] : 0.0;
+    for (int d = LD_WAVE / 2; d > 0; d >>= 1) trace += __shfl_xor(trace, d);
+    const double norm = sqrt(trace), f = norm == 0.0 ? 0.0 : 1.0 / (norm + static_cast<double>(a.eps));
+    __syncthreads();
+    for (int32_t e = threadIdx.x; e < bands * kFewBand * kMuonFewSide; e += kFewThreads) A[e] *= f * f;
+    __syncthreads();
+    for (int32_t step = 0; step < a.steps; ++step) {
+        const bool first = step == 0, last = step + 1 == a.steps;
+        const double ca = a.coeff[3 * step], cb = a.coeff[3 * step + 1], cc = a.coeff[3 * step + 2];
+        for (int32_t k = wave; k < tiles; k += kWaves) {
+            const auto poly = [&](double x, int32_t r, int32_t c) { return fma(cc, x, fma(cb, A[few_at(r, c)], r == c ? ca : 0.0)); };
+            const f64x4 x = product(A, A, k);
+            keep(P, k, x, poly);
+            if (first) keep(Q, k, x, poly);
+        }
+        __syncthreads();
+        f64x4 x[kMine];  // P A, then P Q, which takes Q's place when all have read it
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+            const int32_t k = wave + j * kWaves;
+            if (k < tiles && !last) x[j] = product(P, A, k);
+            else if (k >= tiles && k < 2 * tiles && !first) x[j] = product(P, Q, k - tiles);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+            const int32_t k = wave + j * kWaves;
+            if (k < tiles && !last) keep(R, k, x[j], same);
+            else if (k >= tiles && k < 2 * tiles && !first) keep(Q, k - tiles, x[j], same);
+        }
+        __syncthreads();
+        if (last) break;
+        for (int32_t k = wave; k < tiles; k += kWaves) keep(A, k, product(P, R, k), same);
+        __syncthreads();
+    }
+    double* out = reinterpret_cast<double*>(few_q(b, i));
+    for (int32_t e = threadIdx.x; e < bands * kFewBand * kMuonFewSide; e += kFewThreads) out[e] = Q[few_at(e / kMuonFewSide, e % kMuonFewSide)] * f;
+}
+
+// Q U, which holds the norm: a wave takes 16 columns, a lane's at the eight rows that few_load takes side by side where U is transposed.
+constexpr int kFewColumns = kThreads / LD_WAVE * kFewBand;
+template <int DT, int OT>
+__global__ __launch_bounds__(kThreads) void k_few_apply(Batch b, Source s, FinalArgs out) {
+    __shared__ double Q[kMuonFewSide * kMuonFewSide];
+    typedef typename LdElem<DT>::type elem;
+    typedef typename LdElem<OT>::type out_elem;
+    const int32_t i = blockIdx.y, m = b.m[i], n = b.n[i], lane = ld_lane(), wave = threadIdx.x / LD_WAVE;
+    if (b.kind[i] != kMuonFew || static_cast<int32_t>(blockIdx.x) * kFewColumns >= n) return;
+    const int32_t bands = (m + kFewBand - 1) / kFewBand;
+    const double* q = reinterpret_cast<const double*>(few_q(b, i));
+    const int32_t c = blockIdx.x * kFewColumns + wave * kFewBand + (lane & 15), flipped = b.flipped[i];
+    const elem* src = static_cast<const elem*>(s.src[i]);
+    const int64_t stride = s.stride[i];
+    // rows 32 h + 8 (lane >> 4) + e of column c
+    float x[kMuonFewSide / 32][8];
+#pragma unroll
+    for (int h = 0; h < kMuonFewSide / 32; ++h) {
+        const int32_t k = 32 * h + 8 * (lane >> 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[h][e] = k + e < m && c < n ? static_cast<float>(flipped ? src[c * stride + k + e] : src[(k + e) * stride + c]) : 0.0f;
+    }
+    constexpr int kRowsAtOnce = kThreads / kMuonFewSide;
+    for (int32_t band = 0; band < bands; ++band) {  // a band's loads side by side
+        double y[kFewBand / kRowsAtOnce];
+#pragma unroll
+        for (int e = 0; e < kFewBand / kRowsAtOnce; ++e) y[e] = q[band * kFewBand * kMuonFewSide + e * kThreads + threadIdx.x];
+#pragma unroll
+        for (int e = 0; e < kFewBand / kRowsAtOnce; ++e)
+            Q[few_at(band * kFewBand + e * kRowsAtOnce + threadIdx.x / kMuonFewSide, threadIdx.x % kMuonFewSide)] = y[e];
+    }
+    __syncthreads();
+    out_elem* to = static_cast<out_elem*>(out.out[i]);
+    const int64_t to_stride = out.stride[i];
+#pragma unroll
+    for (int t = 0; t < kFewBands; ++t) {
+        if (t >= bands) break;
+        f64x4 acc = {};
+#pragma unroll
+        for (int h = 0; h < kMuonFewSide / 32; ++h) {
+            if (32 * h >= m) break;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int32_t k = 32 * h + 8 * (lane >> 4) + e;
+                const double y = k < bands * kFewBand ? Q[few_at(k, kFewBand * t + (lane & 15))] : 0.0, z = static_cast<double>(x[h][e]);
+                acc = flipped ? __builtin_amdgcn_mfma_f64_16x16x4f64(z, y, acc, 0, 0, 0) : __builtin_amdgcn_mfma_f64_16x16x4f64(y, z, acc, 0, 0, 0);
+            }
+        }
+        // lanes along the rows of what is written
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int32_t across = lane & 15, down = (lane >> 4) + 4 * w;
+            const int32_t r = kFewBand * t + (flipped ? across : down), col = blockIdx.x * kFewColumns + wave * kFewBand + (flipped ? down : across);
+            if (r < m && col < n) to[flipped ? col * to_stride + r : r * to_stride + col] = static_cast<out_elem>(static_cast<float>(acc[w]));
+        }
     }
 }
 
@@ -714,9 +939,9 @@ bool append(Batch& b, int64_t& used, char* scratch, int64_t room, int64_t rows, 
     const int32_t i = b.count++;
     b.base[i] = scratch + used;
     b.flipped[i] = rows > cols;
-    b.kind[i] = ld_muon_kind(rows > cols ? cols : rows, rows > cols ? rows : cols);
     b.m[i] = static_cast<int32_t>(rows > cols ? cols : rows);
     b.n[i] = static_cast<int32_t>(rows > cols ? rows : cols);
+    b.kind[i] = b.m[i] <= kMuonFewSide ? kMuonFew : ld_muon_kind(b.m[i], b.n[i]);
     used += need;
     return true;
 }
@@ -822,7 +1047,7 @@ ld_status run_steps(Batch& b, const Polynomial& p, const FinalArgs& out, int32_t
     int32_t at[kMuonKinds] = {};
     for (int32_t k = 0; k < kMuonKinds; ++k) prog[k].count = 0;
     for (int32_t i = 0; i < b.count; ++i)
-        if (prog[b.kind[i]].count == 0) program_of(p, b.kind[i], prog[b.kind[i]]);
+        if (b.kind[i] != kMuonFew && prog[b.kind[i]].count == 0) program_of(p, b.kind[i], prog[b.kind[i]]);
     const auto launch_as = [&](auto tile, const Plans& a) {
         typedef decltype(tile) T;
         bool apply = false, final = false;
@@ -878,6 +1103,12 @@ ld_status run_steps(Batch& b, const Polynomial& p, const FinalArgs& out, int32_t
     }
 }
 
+bool has(const Batch& b, bool few) {
+    for (int32_t i = 0; i < b.count; ++i)
+        if ((b.kind[i] == kMuonFew) == few) return true;
+    return false;
+}
+
 int32_t most_parts(const Batch& b) {
     int32_t most = 1;
     for (int32_t i = 0; i < b.count; ++i) {
@@ -887,14 +1118,29 @@ int32_t most_parts(const Batch& b) {
     return most;
 }
 
-ld_status lay_out_group(const Batch& b, const Source& src, int32_t dtype, const Polynomial& p, hipStream_t s) {
-    int32_t most = 1;
+// All of a group but its updates' squares, which `source` has the sums of.
+ld_status orthogonalize_group(Batch& b, const Source& src, int32_t dtype, const Polynomial& p, const FinalArgs& out, int32_t out_type, hipStream_t s) {
+    int32_t tiles = 1, parts = 1, columns = 1;
     for (int32_t i = 0; i < b.count; ++i) {
-        const int32_t tiles = tiles_of(b.m[i], kMuonPad) * tiles_of(b.n[i], kMuonPad);
-        if (tiles > most) most = tiles;
+        const auto most = [](int32_t& x, int32_t y) { x = y > x ? y : x; };
+        if (b.kind[i] == kMuonFew) most(parts, tiles_of(b.n[i], few_columns(b.n[i]))), most(columns, tiles_of(b.n[i], kFewColumns));
+        else most(tiles, tiles_of(b.m[i], kMuonPad) * tiles_of(b.n[i], kMuonPad));
     }
-    ld_with_type(dtype, [&](auto type) { k_lay_out<type><<<dim3(most, b.count), dim3(kThreads), 0, s>>>(b, src, ld_muon_scale(p.bounds.x[0])); });
-    return ld_launch_status();
+    if (has(b, true)) {
+        FewArgs a = {};
+        a.steps = p.steps, a.eps = src.eps;
+        memcpy(a.coeff, p.coeff, sizeof(a.coeff));
+        ld_with_type(dtype, [&](auto type) { k_few_gram<type><<<dim3(parts, b.count), dim3(kThreads), 0, s>>>(b, src); });
+        k_few_steps<<<dim3(b.count), dim3(kFewThreads), 0, s>>>(b, a);
+        ld_with_type(dtype, [&](auto type) {
+            ld_with_type(out_type, [&](auto to) { k_few_apply<type, to><<<dim3(columns, b.count), dim3(kThreads), 0, s>>>(b, src, out); });
+        });
+        if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
+    }
+    if (!has(b, false)) return LD_OK;
+    ld_with_type(dtype, [&](auto type) { k_lay_out<type><<<dim3(tiles, b.count), dim3(kThreads), 0, s>>>(b, src, ld_muon_scale(p.bounds.x[0])); });
+    if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
+    return run_steps(b, p, out, out_type, s);
 }
 
 }  // namespace
@@ -941,8 +1187,8 @@ extern "C" ld_status ld_orthogonalize(const void* const* src, const int64_t* src
         }
         if (b.count == 0) break;
         source.sums = static_cast<double*>(workspace), source.eps = eps;
-        ld_with_type(dtype, [&](auto type) { k_squares<type><<<dim3(most_parts(b), b.count), dim3(kThreads), 0, s>>>(b, source); });
-        if (ld_launch_status() != LD_OK || lay_out_group(b, source, dtype, p, s) != LD_OK || run_steps(b, p, out, out_dtype, s) != LD_OK) return LD_ERR_HIP;
+        if (has(b, false)) ld_with_type(dtype, [&](auto type) { k_squares<type><<<dim3(most_parts(b), b.count), dim3(kThreads), 0, s>>>(b, source); });
+        if (ld_launch_status() != LD_OK || orthogonalize_group(b, source, dtype, p, out, out_dtype, s) != LD_OK) return LD_ERR_HIP;
     }
     return LD_OK;
 }
@@ -1022,7 +1268,7 @@ extern "C" ld_status ld_merge_dense_muon(float* const* w, float* const* m, const
         up.keep = static_cast<float>(1.0 - static_cast<double>(lr) * static_cast<double>(weight_decay));
         const dim3 grid(most_parts(b), mats);
         ld_with_type(dtype, [&](auto type) { k_momentum<type><<<grid, dim3(kThreads), 0, s>>>(b, mom); });
-        if (ld_launch_status() != LD_OK || lay_out_group(b, source, LD_F32, p, s) != LD_OK || run_steps(b, p, out, LD_F32, s) != LD_OK) return LD_ERR_HIP;
+        if (ld_launch_status() != LD_OK || orthogonalize_group(b, source, LD_F32, p, out, LD_F32, s) != LD_OK) return LD_ERR_HIP;
         k_update<<<dim3(4 * most_parts(b), mats), dim3(kThreads), 0, s>>>(b, up);
         if (ld_launch_status() != LD_OK) return LD_ERR_HIP;
     }

@@ -183,6 +183,73 @@ def test_larger(r, c):
     check(ld.ld_orthogonalize([u])[0], u, (r, c))
 
 
+# Up to 64 rows everything is in 64 bits until the result is rounded: half a step of its type, and half one of 32 bits on the way to less. What
+# 64 bits lose, 2^-53 at each of a few hundred sums and products whose errors usual steps grow no more than 2^12 times (in both
+# sides of the comparison), stays below 2^-30 of the largest element.
+def check_few(got, u, tag, **kw):
+    want = orthogonal64(u, **kw)
+    assert got.shape == want.shape and not bool(got.isnan().any()), tag
+    room = (UNIT[got.dtype] + (U if got.dtype != F32 else 0.0)) * want.abs() + 0.5 * STEP[got.dtype] + 2.0 ** -30 * want.abs().max()
+    off = (got.double() - want).abs()
+    assert bool((off <= room).all()), (tag, float((off - room).max()), float(want.abs().max()))
+
+
+@pytest.mark.parametrize("r", [1, 2, 15, 16, 17, 32, 33, 48, 49, 63, 64])
+@pytest.mark.parametrize("c", [1, 64, 127, 128, 129, 1000, 8192, 8193, 20011])
+def test_few_rows(r, c):
+    print(f"[orthogonalize] {r} x {c}", flush=True)
+    for rows, cols in ((r, c), (c, r)):
+        for kind in ("plain", "lower rank"):
+            u = matrix(rows, cols, gen(r * 10 + c), kind).to(F32)
+            check_few(ld.ld_orthogonalize([u])[0], u, (rows, cols, kind))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("out_dtype", [F32, BF16, F16])
+def test_few_rows_of_every_type_and_stride(dtype, out_dtype):
+    print(f"[orthogonalize] {dtype} to {out_dtype}", flush=True)
+    for r, c in ((5, 77), (77, 5), (64, 333), (333, 64), (20, 20)):
+        wide = matrix(r + 3, c + 7, gen(c)).to(dtype)
+        u, room = wide[1:r + 1, 3:c + 3], torch.full((r + 2, c + 9), 7.0, dtype=out_dtype, device=DEV)
+        ld.ld_orthogonalize([u], outs=[room[1:r + 1, 5:c + 5]])
+        check_few(room[1:r + 1, 5:c + 5], u, (r, c))
+        room[1:r + 1, 5:c + 5] = 7.0
+        assert bool((room == 7.0).all())
+        if dtype == out_dtype:
+            want = ld.ld_orthogonalize([u])[0]
+            before = wide.clone()
+            before[1:r + 1, 3:c + 3] = want
+            ld.ld_orthogonalize([u], outs=[u])
+            assert same_bits(wide, before)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 16])
+def test_few_rows_by_any_steps(steps):
+    print(f"[orthogonalize] {steps} steps", flush=True)
+    coeffs = [(1.5, -0.5, 0.0), (15 / 8, -10 / 8, 3 / 8)] * 8  # these bring singular values to 1, and errors to nothing
+    for r, c in ((1, 40), (33, 70), (70, 64)):
+        u = matrix(r, c, gen(steps)).to(F32)
+        check_few(ld.ld_orthogonalize([u], steps=steps, coeffs=coeffs[:steps])[0], u, (r, c), steps=steps, coeffs=coeffs[:steps])
+
+
+def test_few_rows_that_are_zeros_or_no_numbers():
+    print("[orthogonalize] few rows of zeros, infinities and NaN", flush=True)
+    us = [matrix(r, c, gen(c)).to(F32) for r, c in ((3, 50), (50, 3), (40, 200), (1, 9), (64, 64), (100, 200))]
+    want = ld.ld_orthogonalize(us)
+    us[0][:] = 0.0
+    us[1][7, 2], us[2][39, 150], us[3][0, 0] = math.nan, math.inf, -math.inf
+    us[3][0, 1:] = 0.0
+    got = ld.ld_orthogonalize(us)
+    assert bool((got[0] == 0.0).all()) and all(bool(g.isnan().all()) for g in got[1:4])
+    assert all(same_bits(a, b) for a, b in zip(got[4:], want[4:]))
+    us[2][39, 150] = 0.0
+    us[2][:39] = 0.0
+    check_few(ld.ld_orthogonalize(us[2:3])[0], us[2], "one row")
+    for size in (1e-44, 1e-30, 1e38):
+        u = (matrix(7, 90, gen(1)).clamp(-3, 3) * size).to(F32)
+        check_few(ld.ld_orthogonalize([u], eps=0.0)[0], u, size, eps=0.0)
+
+
 @pytest.mark.parametrize("size", [1e-44, 1e-30, 1e30, 1e38])
 def test_magnitudes(size):
     u = torch.sign(matrix(40, 50, gen(1))).mul(size).to(F32) if size < 1e-40 else matrix(40, 50, gen(1)).clamp(-3, 3).mul(size).to(F32)
