@@ -54,15 +54,17 @@ inline bool ld_muon_bounds(LdMuonBounds& m, int32_t steps, const float* coeff) {
 
 // A run of steps works on one Gram matrix; X is multiplied by what they amount to, and its Gram matrix formed anew, between runs. The
 // Gram matrix loses directions of small singular values, the more the further a run grows them (each usual step 3.4 times), and
-// a matrix that is about square has more of those than a wide one. So a run of a wide matrix (kind 2) ends at three steps or 48 times,
-// counted from the last step on, of a less wide one (1) at two steps or 16 times, counted from the first, and one that is about square
+// a matrix that is about square has more of those than a wide one, and one of many rows, whose values are scaled to a norm of 1 in all,
+// smaller ones. So a run of a wide matrix of up to kMuonThreeSide rows (kind 2) ends at three steps or 48 times,
+// counted from the last step on, of a less wide or a larger one (1) at two steps or 16 times, counted from the first, and one that is about square
 // (0), to which a run's matrices of m x m are no smaller than X, has runs of one step: 2 + 3, 2 + 2 + 1 and five times 1 of five usual
 // steps, 6 m^2 n + 14 m^3, 9 m^2 n + 11 m^3 and 15 m^2 n + 5 m^3 operations of products, in 17, 18 and 15 launches. Errors against 64 bits
 // (relative, Frobenius) of products in 32 bits in the order of the formula, and of these three: 768 x 768 2.3e-6, 4.3e-6, 1.9e-6, 1.7e-6;
-// 1000 x 2000 2.9e-6, 2.9e-6, 2.3e-6, 2.1e-6; 1600 x 6400 4.0e-6, 2.6e-6, 2.9e-6, 2.5e-6. Up to kMuonFewSide rows a matrix goes another
+// 1000 x 2000 2.9e-6, 2.9e-6, 2.3e-6, 2.1e-6; 1600 x 6400 4.0e-6, 2.6e-6, 2.9e-6, 2.5e-6; 5120 x 2048 with rows of
+// different scales 4.4e-6, 5.4e-6, 3.3e-6; 11008 x 4096 of them 4.8e-6, 6.6e-6, 3.3e-6, 3.3e-6. Up to kMuonFewSide rows a matrix goes another
 // way, in 64 bits (kMuonFew).
-constexpr int32_t kMuonKinds = 4, kMuonFew = 3, kMuonFewSide = 64;
-inline int32_t ld_muon_kind(int64_t m, int64_t n) { return 2 * n >= 5 * m ? 2 : 4 * n >= 5 * m ? 1 : 0; }
+constexpr int32_t kMuonKinds = 4, kMuonFew = 3, kMuonFewSide = 64, kMuonThreeSide = 2048;
+inline int32_t ld_muon_kind(int64_t m, int64_t n) { return 2 * n >= 5 * m && m <= kMuonThreeSide ? 2 : 4 * n >= 5 * m ? 1 : 0; }
 // First steps of the runs, and behind them the number of steps; returns the number of runs.
 inline int32_t ld_muon_runs(const LdMuonBounds& b, int32_t steps, int32_t kind, int32_t* begin) {
     const bool wide = kind == 2;

@@ -55,7 +55,7 @@ def orthogonal64(u, steps=5, coeffs=None, eps=1e-7):
 def runs_of(coeffs, m, n):
     """Numbers of steps that go by one Gram matrix: up to three or a growth of 48, counted from the last, of wide matrices, two or 16 of
     less wide ones, and one of those that are about square."""
-    kind = 2 if 2 * n >= 5 * m else 1 if 4 * n >= 5 * m else 0
+    kind = 2 if 2 * n >= 5 * m and m <= 2048 else 1 if 4 * n >= 5 * m else 0
     top, grows, longest, most = 1.0, [], kind + 1, 48 if kind == 2 else 16
     for a, b, c in coeffs:
         x = np.linspace(0, top, 10001)

@@ -78,7 +78,7 @@ def test_runs_of_the_usual_steps(shim):
         for steps, begin in want.items():
             assert bounds(shim, steps, usual(steps), kind)[4] == begin + [steps], (kind, steps)
     i64 = ctypes.c_int64
-    assert [shim.kind(i64(m), i64(n)) for m, n in ((1, 1), (100, 124), (100, 125), (100, 249), (100, 250), (65536, 65536), (1, 65536))] == [0, 0, 1, 1, 2, 0, 2]
+    assert [shim.kind(i64(m), i64(n)) for m, n in ((1, 1), (100, 124), (100, 125), (100, 249), (100, 250), (65536, 65536), (1, 65536), (2048, 5120), (2049, 65536))] == [0, 0, 1, 1, 2, 0, 2, 2, 1]
 
 
 def test_bounds_hold_for_every_singular_value(shim):
