@@ -114,6 +114,7 @@ template <int SIDE_, int DOWN_, int ACROSS_, int STAGES_> struct Tile {
     static constexpr int WAVES = SIDE == 64 ? 3 : 2;             // of a SIMD
     // Consecutive tiles, which share rows and columns, that an XCD has at a time: as many as it runs, so that its cache loads them once.
     static constexpr int RUN = SIDE == 256 ? 32 : SIDE == 64 ? 96 : 64;
+    static constexpr int BAND = 8;
     static constexpr int R = SIDE / DOWN / 32, C = SIDE / ACROSS / 32;            // MFMA tiles of a wave
     static constexpr int BLOCK_BYTES = SIDE * static_cast<int>(kMuonRowBytes);     // an operand's, of a block
     static constexpr int FETCHES = BLOCK_BYTES / 1024 / (DOWN * ACROSS);           // loads of a wave for it
@@ -290,11 +291,9 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_symmetric(Batch batch,
     if (second) tile -= tiles;
     const Product prod = a.prod[second];
     const float scale = a.scale[second];
-    // row by row of the lower triangle
-    int32_t tr = static_cast<int32_t>((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
-    while (tr * (tr + 1) / 2 > tile) --tr;
-    while ((tr + 1) * (tr + 2) / 2 <= tile) ++tr;
-    const int32_t tc = tile - tr * (tr + 1) / 2, m = batch.m[i], r0 = tr * T::SIDE, c0 = tc * T::SIDE;
+    int32_t tr, tc;
+    ld_muon_lower_tile(tile, side, T::BAND, tr, tc);
+    const int32_t m = batch.m[i], r0 = tr * T::SIDE, c0 = tc * T::SIDE;
     const int64_t rows = padded(m);
     f32x16 acc[T::R][T::C] = {};
     multiply<T>(buffer_of(batch, i, prod.left) + r0 * kMuonRowBytes, rows, buffer_of(batch, i, prod.right) + c0 * kMuonRowBytes, rows,
@@ -375,7 +374,9 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Pla
     const int32_t i = problem_of(batch, tile);
     const Plan a = plans.of[batch.kind[i]];
     const int32_t m = batch.m[i], n = batch.n[i], down = tiles_of(padded(m), T::SIDE);
-    const int32_t r0 = tile % down * T::SIDE, c0 = tile / down * T::SIDE;
+    int32_t tr, tc;
+    ld_muon_tile(tile, down, tiles_of(padded(n), T::SIDE), T::BAND, tr, tc);
+    const int32_t r0 = tr * T::SIDE, c0 = tc * T::SIDE;
     const int64_t rows = padded(m), cols = padded(n);
     f32x16 acc[T::R][T::C] = {};
     multiply<T>(buffer_of(batch, i, a.prod[0].left) + r0 * kMuonRowBytes, rows, buffer_of(batch, i, a.prod[0].right) + c0 * kMuonRowBytes, cols,

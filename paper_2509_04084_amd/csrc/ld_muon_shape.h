@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "ld_map.h"
+
 constexpr int32_t kMuonMaxSteps = 16;
 constexpr int32_t kMuonPad = 64;        // rows and columns are padded to whole tiles of the smallest kind
 constexpr int32_t kMuonBlock = 32;      // elements of a row side by side, their upper halves before their lower
@@ -98,6 +100,31 @@ inline float ld_muon_scale(double bound) {
     int e = 0;
     frexp(bound, &e);  // bound < 2^e
     return static_cast<float>(ldexp(1.0, 15 - (e < 0 ? 0 : e)));
+}
+
+// Which tile a workgroup has. Consecutive ones, which an XCD has at a time, are to share rows and columns: bands of `band` rows of tiles, in each
+// of them column after column.
+LD_HD void ld_muon_tile(int32_t tile, int32_t down, int32_t across, int32_t band, int32_t& r, int32_t& c) {
+    const int32_t first = tile / (band * across) * band, rows = down - first < band ? down - first : band;
+    const int32_t t = tile - first * across;
+    r = first + t % rows, c = t / rows;
+}
+// The same of the tiles on and below the diagonal: what a band has left of its diagonal tiles first, these then row by row.
+LD_HD int32_t ld_muon_triangle_row(int32_t tile) {
+    int32_t r = static_cast<int32_t>((sqrtf(8.0f * static_cast<float>(tile) + 1.0f) - 1.0f) * 0.5f);
+    while (r * (r + 1) / 2 > tile) --r;
+    while ((r + 1) * (r + 2) / 2 <= tile) ++r;
+    return r;
+}
+LD_HD void ld_muon_lower_tile(int32_t tile, int32_t side, int32_t band, int32_t& r, int32_t& c) {
+    const int32_t first = ld_muon_triangle_row(tile) / band * band, rows = side - first < band ? side - first : band;
+    const int32_t t = tile - first * (first + 1) / 2;
+    if (t < first * rows) {
+        r = first + t % rows, c = t / rows;
+        return;
+    }
+    const int32_t d = t - first * rows, down = ld_muon_triangle_row(d);
+    r = first + down, c = first + d - down * (down + 1) / 2;
 }
 
 inline int64_t ld_muon_padded(int64_t n) { return (n + kMuonPad - 1) / kMuonPad * kMuonPad; }

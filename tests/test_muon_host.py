@@ -35,6 +35,12 @@ int32_t bounds(int32_t steps, const float* coeff, int32_t kind, double* x, doubl
 int32_t kind(int64_t m, int64_t n) { return ld_muon_kind(m, n); }
 float scale(double bound) { return ld_muon_scale(bound); }
 int64_t scratch(int32_t m, int32_t n) { return ld_muon_scratch(m, n); }
+void tiles(int32_t down, int32_t across, int32_t band, int32_t* r, int32_t* c) {
+    for (int32_t t = 0; t < down * across; ++t) ld_muon_tile(t, down, across, band, r[t], c[t]);
+}
+void lower_tiles(int32_t side, int32_t band, int32_t* r, int32_t* c) {
+    for (int32_t t = 0; t < side * (side + 1) / 2; ++t) ld_muon_lower_tile(t, side, band, r[t], c[t]);
+}
 }
 """
 
@@ -238,3 +244,20 @@ def test_binding_refuses_before_any_launch():
     with pytest.raises(TypeError):
         ld.ld_merge_dense_muon([a], [a.clone()], [[a.clone()]], 0.1)
     ld.ld_merge_dense_muon([], [], [], 0.1)
+
+
+def test_every_tile_is_one_workgroups(shim):
+    rs = np.random.RandomState(5)
+    for down, across, band in [(1, 1, 8), (1, 9, 8), (9, 1, 8), (8, 8, 8), (12, 12, 8), (1024, 1024, 8)] + [tuple(rs.randint(1, (70, 70, 12))) for _ in range(60)]:
+        r, c = np.empty((2, down * across), np.int32)
+        shim.tiles(int(down), int(across), int(band), _p(r), _p(c))
+        assert r.min() >= 0 and r.max() < down and c.min() >= 0 and c.max() < across
+        assert np.unique(r.astype(np.int64) * across + c).size == down * across, (down, across, band)
+        n = down * (down + 1) // 2
+        r, c = np.empty((2, n), np.int32)
+        shim.lower_tiles(int(down), int(band), _p(r), _p(c))
+        assert c.min() >= 0 and r.max() < down and (c <= r).all()
+        assert np.unique(r.astype(np.int64) * down + c).size == n, (down, band)
+        if down >= 32 and band == 8:  # 64 in a row, of eight rows and eight columns
+            t = 24 * 25 // 2
+            assert np.unique(r[t:t + 64]).size == 8 and np.unique(c[t:t + 64]).size == 8
