@@ -26,8 +26,12 @@
  * what stands between a model's tokens and those gradients: ld_embed_lookup and
  * ld_embed_grad (the token embedding, the largest tensor of the models that are
  * checkpointed, and its gradient), ld_grad_norm, ld_clip_grads and
- * ld_clip_grad_norm (the norm over all gradients of a step, and clipping by it);
- * and two helpers of the recovery path: ld_merge_sparse_from_host (the merge fed
+ * ld_clip_grad_norm (the norm over all gradients of a step, and clipping by it),
+ * ld_token_logprob and ld_token_logprob_grad (log probabilities of given tokens,
+ * entropy and the most probable tokens of rows of logits, and the gradient: where a
+ * step's gradients begin, and how a recovered model is compared); the optimizer
+ * that orthogonalises its updates, ld_orthogonalize and ld_merge_dense_muon (dense
+ * diffs replayed through it, or a training step); and two helpers of the recovery path: ld_merge_sparse_from_host (the merge fed
  * from page-locked host memory, copies and merges pipelined) and ld_check_diff
  * (counts what is wrong with a diff before it is merged).
  *
@@ -538,7 +542,8 @@ ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_t dtype,
  *   entropy[t]     = L - sum_j exp(x_j - L) x_j
  *   top_ids[t], top_logprob[t] = the `top` tokens of the largest logits, in that order, the
  *                    lower index first among equal ones (-0 and +0 are), and x_j - L of each
- * in 32 bits.  Masked tokens are minus infinity: their probability is 0.  A row in which
+ * in 32 bits.  Few rows are split, and L, and the entropy, may then differ in their last bits
+ * from what the same row has in a call of more; the same call gives the same bits.  Masked tokens are minus infinity: their probability is 0.  A row in which
  * nothing is left (all minus infinity) has M = -inf, L = 0, entropy 0 and log probabilities of
  * -inf.  An infinite logit or a NaN makes a row's L, entropy and log probabilities NaN; a NaN
  * counts as the largest of all logits among the alternatives.
@@ -587,8 +592,8 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
  * vectors and singular values near 1, by Newton-Schulz steps:
  *   X = U / (|U|_F + eps);  `steps` times  X <- (a I + b A + c A^2) X,  A = X X^T
  * (the steps run on the smaller side: for U with more rows than columns, on its transposed, which
- * is the same map).  Everything is as precise as products in 32 bits are, and rounded once to
- * out_dtype; U's squares are summed in 64 bits.  A matrix of zeros stays zeros.  An infinity or a
+ * is the same map).  Everything is as precise as products in 32 bits are (of up to 64 rows or
+ * columns: in 64), and rounded once to out_dtype; U's squares are summed in 64 bits.  A matrix of zeros stays zeros.  An infinity or a
  * NaN anywhere in a matrix makes all of it NaN; other matrices of the call are not touched by it.
  * What a matrix becomes depends on nothing but itself: not on the others of the call.
  *
@@ -613,7 +618,8 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
  *   u  = nesterov ? fl(mu m + g_t) : m
  *   w <- fl(fl(w keep) - rate O(u)),  keep = fl(1 - lr weight_decay),  rate = fl(lr scale[i])
  * with O the map above, its result in 32 bits.  One call with W gradients gives the same bits as
- * W calls with one.
+ * W calls with one.  An infinity or a NaN in a gradient stays in that momentum and makes all of
+ * that matrix NaN, from its step on: gradients are checked (ld_grad_norm) before.
  *
  *   w, m       host arrays of n_mats dev pointers, fp32 [rows][cols] contiguous, in/out; no two
  *              overlap

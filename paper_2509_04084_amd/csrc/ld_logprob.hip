@@ -16,10 +16,16 @@ namespace {
 
 constexpr int kGroup = 8;                      // elements side by side that a thread takes at a time
 constexpr int kWide = 256, kNarrow = 64;       // threads of a workgroup: one row, or a part of one
-constexpr int32_t kNarrowElems = 4096;         // up to here a row is one wave's
+// Up to here a row is one wave's, where there are at least as many rows as would fill the chip with waves: it meets no barrier (five
+// alternatives of 16384 x 1000 in bf16 19 us, by workgroups of 256 threads 76; x 4096 38 and 60; x 8000 71 and 82, but fp32 98 and
+// 90; 1000 x 4096 7.8 and 8.3, 512 x 4096 7.4 and 7.0, 1000 x 8000 11.4 and 10.4).
+constexpr int32_t kNarrowElems = 4096;
+constexpr int64_t kNarrowRows = 512;
 constexpr int32_t kMostPart = 65536;           // elements of a part: 32 KB of group maxima for the alternatives
 constexpr int32_t kPartStep = kWide * kGroup;
-constexpr int64_t kWorkgroups = 1024;          // rows are split until there are as many, where they are fewer than half
+// Rows are split until there are as many, where they are fewer than half: by 256, 512 and 1024, us with five alternatives of 50257: 8 rows 10.2,
+// 10.1, 9.9; 64 rows 12.0, 12.5, 12.7; 255 rows 13.2, 15.8, 16.4; 511 rows 17.8, 17.8, 22.3.
+constexpr int64_t kWorkgroups = 256;
 constexpr int kMostTop = LD_MAX_TOP;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // Powers of two by which a value may pass the reference before that is moved: an exponent is rounded in proportion to it.
@@ -576,7 +582,7 @@ struct Split {
     bool narrow;
 };
 Split split_of(int64_t T, int32_t V) {
-    if (V <= kNarrowElems && T >= kWorkgroups / 2) return {V, 1, true};
+    if (V <= kNarrowElems && T >= kNarrowRows) return {V, 1, true};
     const int32_t most = (V + kPartStep - 1) / kPartStep, least = (V + kMostPart - 1) / kMostPart;
     int64_t parts = T > 0 && T < kWorkgroups / 2 ? (kWorkgroups + T - 1) / T : 1;
     parts = parts > most ? most : parts < least ? least : parts;
@@ -670,7 +676,7 @@ extern "C" ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_
     ld_begin_call();
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int32_t elems = dtype == LD_F32 && out_dtype == LD_F32 ? grad_elems<LD_F32, LD_F32>() : grad_elems<LD_BF16, LD_BF16>();
-    const bool narrow = V <= kNarrow * elems;
+    const bool narrow = V <= kNarrow * elems;  // a wave's: 16384 x 1000 in bf16 11 us, by 256 threads 17
     const int32_t threads = narrow ? kNarrow : kWide, chunk = threads * elems, chunks = (V + chunk - 1) / chunk;
     const int64_t most = (ld_workgroups(static_cast<int64_t>(1) << 40, threads) - 7) / chunks;
     for (int64_t t = 0; t < T; t += most) {
