@@ -108,13 +108,18 @@ typedef void __attribute__((address_space(3))) * shared_ptr;
 
 // A tile of SIDE by SIDE sums, by DOWN x ACROSS waves. STAGES blocks of columns have room in shared memory: one that is multiplied, the others on
 // their way.
+// Tiles of 64 and 128 are bound by shared memory (of 128, a block's 64 KB of fragments and 32 KB of loads take as long as its MFMA), those of
+// 256 by the matrix cores and their power. Five steps of 32 matrices of 768 x 768 and of four of 2048 x 2048, us: 64 by 2 x 2 waves, three
+// stages 1460 and 2660, by two waves 1570 and 2890, by one 1610 and 2770; 128 by 2 x 2, two stages 1290 and 2410, by two waves 1485
+// and 2640, by eight 1300 and 2510; 256 by 2 x 4, two stages 1425 and 2290, by four 1640 and 2460, by sixteen 2260 and 3690. Blocks of 16
+// columns, as many bytes and more on their way, took 3 to 8 % longer in all: twice the barriers.
 template <int SIDE_, int DOWN_, int ACROSS_, int STAGES_> struct Tile {
     static constexpr int SIDE = SIDE_, DOWN = DOWN_, ACROSS = ACROSS_, STAGES = STAGES_;
     static constexpr int THREADS = DOWN * ACROSS * LD_WAVE;
     static constexpr int WAVES = SIDE == 64 ? 3 : 2;             // of a SIMD
     // Consecutive tiles, which share rows and columns, that an XCD has at a time: as many as it runs, so that its cache loads them once.
     static constexpr int RUN = SIDE == 256 ? 32 : SIDE == 64 ? 96 : 64;
-    static constexpr int BAND = 8;
+    static constexpr int BAND = 8;                               // rows of tiles that they are taken from (rows of all: 64 3030 us, not 2760)
     static constexpr int R = SIDE / DOWN / 32, C = SIDE / ACROSS / 32;            // MFMA tiles of a wave
     static constexpr int BLOCK_BYTES = SIDE * static_cast<int>(kMuonRowBytes);     // an operand's, of a block
     static constexpr int FETCHES = BLOCK_BYTES / 1024 / (DOWN * ACROSS);           // loads of a wave for it
@@ -152,8 +157,8 @@ __device__ __forceinline__ void multiply(const char* left, int64_t left_rows, co
         fetch<T>(left + k * left_step, to);
         fetch<T>(right + k * right_step, to + T::BLOCK_BYTES);
     };
-    // The operands of 16 columns are read while those before them are multiplied, and waited for before the next are read: the compiler
-    // would wait for both.
+    // The operands of 16 columns are read while those before them are multiplied (in what order, is the compiler's: 1 % faster than the
+    // reads first), and waited for before the next are read: the compiler would wait for both.
     constexpr int kSharedRead = 0xC07F;  // lgkmcnt(0), nothing else
     half8 x[2][T::R][2], y[2][T::C][2];
     const auto read = [&](int s, int32_t stage) {
@@ -184,7 +189,6 @@ __device__ __forceinline__ void multiply(const char* left, int64_t left_rows, co
         const int32_t next = stage + 1 == kStages ? 0 : stage + 1;
         __builtin_amdgcn_s_waitcnt(kSharedRead);
         read(1, stage);
-        __builtin_amdgcn_sched_barrier(0);
         use(0);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(kSharedRead);
@@ -196,7 +200,6 @@ __device__ __forceinline__ void multiply(const char* left, int64_t left_rows, co
             if (k + kStages < blocks) fetch_block(k + kStages, stage);
             read(0, next);
         }
-        __builtin_amdgcn_sched_barrier(0);
         use(1);
         __builtin_amdgcn_sched_barrier(0);
         stage = next;

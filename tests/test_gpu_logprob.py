@@ -146,7 +146,8 @@ def check(x, ids, scale, top, id_dtype=torch.int64, dev=None, tag=""):
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("T,V,top", [(1, 1, 1), (1, 7, 7), (3, 8, 2), (2, 64, 64), (5, 499, 20), (70, 2047, 5), (3, 2048, 64), (3, 2049, 64), (9, 4096, 50),
-                                     (2, 4097, 1), (1, 50257, 20), (8, 32003, 64), (300, 8191, 3), (1, 65537, 10), (2, 160001, 33)])
+                                     (2, 4097, 1), (1, 50257, 20), (8, 32003, 64), (300, 8191, 3), (1, 65537, 10), (2, 160001, 33), (64, 50257, 11),
+                                     (127, 8191, 64), (128, 9001, 5), (511, 4000, 4), (512, 4000, 4)])
 def test_scores_and_gradients(T, V, top, dtype):
     print(f"[score] T={T} V={V} top={top} {dtype}", flush=True)
     g = gen(T * 31 + V)
