@@ -108,11 +108,12 @@ typedef void __attribute__((address_space(3))) * shared_ptr;
 
 // A tile of SIDE by SIDE sums, by DOWN x ACROSS waves. STAGES blocks of columns have room in shared memory: one that is multiplied, the others on
 // their way.
-// Tiles of 64 and 128 are bound by shared memory (of 128, a block's 64 KB of fragments and 32 KB of loads take as long as its MFMA), those of
-// 256 by the matrix cores and their power. Five steps of 32 matrices of 768 x 768 and of four of 2048 x 2048, us: 64 by 2 x 2 waves, three
+// Tiles of 64 and 128 are bound by their loads into shared memory next to the products (of 128, below, 2410 us; 1480 without the loads, 1790
+// with a third of the products), those of 256 by the matrix cores and their power. Five steps of 32 matrices of 768 x 768 and of four of 2048 x 2048, us: 64 by 2 x 2 waves, three
 // stages 1460 and 2660, by two waves 1570 and 2890, by one 1610 and 2770; 128 by 2 x 2, two stages 1290 and 2410, by two waves 1485
 // and 2640, by eight 1300 and 2510; 256 by 2 x 4, two stages 1425 and 2290, by four 1640 and 2460, by sixteen 2260 and 3690. Blocks of 16
-// columns, as many bytes and more on their way, took 3 to 8 % longer in all: twice the barriers.
+// columns, as many bytes and more on their way, took 3 to 8 % longer in all: twice the barriers; loads among the products rather than before them
+// 2 to 7 %; asking for lines four blocks early 1 to 8 %.
 template <int SIDE_, int DOWN_, int ACROSS_, int STAGES_> struct Tile {
     static constexpr int SIDE = SIDE_, DOWN = DOWN_, ACROSS = ACROSS_, STAGES = STAGES_;
     static constexpr int THREADS = DOWN * ACROSS * LD_WAVE;
