@@ -49,6 +49,7 @@ struct ScoreArgs {
     int32_t V, part, parts, top;
     float scale;
     int32_t wide_ids;
+    int32_t listed;            // groups that shared memory has room for behind the maxima
 };
 
 __device__ __forceinline__ int64_t id_at(const void* ids, int64_t t, int32_t wide) {
@@ -178,7 +179,7 @@ __device__ __forceinline__ int32_t rank_in_wave(uint64_t key) {
     return rank;
 }
 // The K-th largest of all threads' keys (0: nothing), in every thread. Up to kFewTop the K largest of every wave one after
-// another, and of those by counting (16384 x 32000 with five alternatives 213 -> 204 us); else every key's rank. `keys`: 256 of them.
+// another, and of those by counting; else every key's rank. `keys`: 256 of them.
 constexpr int32_t kFewTop = 8;
 template <int THREADS>
 __device__ __forceinline__ uint64_t kth_of_few(uint64_t key, int32_t K, uint64_t* keys) {
@@ -223,12 +224,12 @@ template <int DT, int THREADS, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
     typedef typename LdElem<DT>::type elem;
     typedef Raw<DT, kGroup> R;
-    constexpr int kWaves = THREADS / LD_WAVE;
+    constexpr int kWaves = THREADS / LD_WAVE, kOfSet = THREADS / 16;
     extern __shared__ float groups[];
     __shared__ Sums wave_sums[kWaves];
     __shared__ float wave_high[kWaves];
     __shared__ uint64_t keys[TOP ? kMostTop * kGroup : 1];
-    __shared__ uint32_t counts[2], picked_groups[TOP ? kMostTop : 1];
+    __shared__ uint32_t counts[3], picked_groups[TOP ? kMostTop : 1];
     __shared__ uint64_t kth;
     const int64_t t = a.row0 + blockIdx.x / a.parts;
     const int32_t p = blockIdx.x % a.parts, begin = p * a.part, n = min(a.V - begin, a.part), tid = threadIdx.x;
@@ -331,11 +332,73 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
             if (o > order) order = o, at = q;
         });
     }
+    const int32_t K = a.top;
+    uint64_t* list = reinterpret_cast<uint64_t*>(groups + (n_groups + 1) / 2 * 2);  // behind the maxima
+    uint64_t* best = a.best ? a.best + (a.row0 * a.parts + blockIdx.x) * K : nullptr;
+    const auto rank_and_write = [&](int32_t many) {  // the best of the keys
+        for (int32_t i = tid; i < many; i += THREADS) {
+            const uint64_t k = keys[i];
+            int32_t better = 0;
+            for (int32_t j = 0; j < many; ++j) better += keys[j] > k;
+            if (better >= K) continue;
+            if (best) best[better] = k;
+            else write_top(a, t, better, k, r.high, log_z);
+        }
+        if (best)  // a part of fewer elements
+            for (int32_t i = n + tid; i < K; i += THREADS) best[i] = 0;
+    };
+    const uint64_t mine = tid < n_body || (headed && tid == 0) ? key_of(order, at) : 0;
+    // Few alternatives: no better bar than the K-th of what 16 sets of threads have best is passed by at least K elements, and usually by few
+    // more, which are ranked (five of 16384 x 32000 212 -> 204 us, eight of 1023 x 32003 28.3 -> 27.0; with 64 sets fifty take 33.4, not 31.7).
+    if (K <= kFewTop) {
+        uint32_t set = static_cast<uint32_t>(mine >> 32);
+        set = max(set, ld_dpp0<0xB1>(set));  // of two, of four lanes
+        set = max(set, ld_dpp0<0x4E>(set));
+        if (kWaves > 1) {                    // of sixteen, in the last
+            set = max(set, ld_dpp0<kDppShr + 4>(set));
+            set = max(set, ld_dpp0<kDppShr + 8>(set));
+        }
+        if (tid == 0) counts[0] = counts[1] = 0;
+        if (tid % kOfSet == kOfSet - 1) picked_groups[tid / kOfSet] = set;
+        __syncthreads();
+        set = ld_lane() < 16 ? picked_groups[ld_lane()] : 0;
+        int32_t rank = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const uint32_t other = __builtin_amdgcn_readlane(set, j);
+            rank += other > set || (other == set && j < ld_lane());
+        }
+        const uint32_t bar = __builtin_amdgcn_readlane(set, __builtin_ctzll(__ballot(rank == K - 1)));
+        if (mine >> 32 >= bar && mine)
+            own_groups([&](int32_t q) {
+                if (order_of(groups[q]) < bar) return;
+                const int32_t i = atomicAdd(&counts[0], 1u);
+                if (i < a.listed) list[i] = q;
+            });
+        if (tid == 0) wave_sums[0] = {r.high, log_z, 0.0f};
+        __syncthreads();
+        const int32_t listed = counts[0];
+        if (listed <= a.listed) {
+            log_z = wave_sums[0].z;
+            for (int32_t i = tid; i < listed * kGroup; i += THREADS) {
+                const int32_t q = static_cast<int32_t>(list[i / kGroup]), e = first_of(q) + i % kGroup;
+                if (e >= end_of(q)) continue;
+                const uint32_t o = order_of(static_cast<float>(row[e]));
+                if (o < bar) continue;
+                const int32_t place = atomicAdd(&counts[1], 1u);
+                if (place < kMostTop * kGroup) keys[place] = key_of(o, begin + e);
+            }
+            __syncthreads();
+            if (counts[1] <= kMostTop * kGroup) {
+                rank_and_write(counts[1]);
+                return;
+            }
+        }
+        __syncthreads();
+    }
     // The best K elements lie in the K groups whose largest elements are the best K (of equal ones the lower), and those in the K
     // threads of which the same holds. First the K-th of those threads' best.
-    const int32_t K = a.top;
-    const uint64_t mine = tid < n_body || (headed && tid == 0) ? key_of(order, at) : 0;
-    if (tid == 0) counts[0] = counts[1] = 0, kth = 0;
+    if (tid == 0) counts[0] = counts[1] = counts[2] = 0, kth = 0;
     const bool single = n_groups <= THREADS && !headed;  // a thread has one group at most: its rank is the group's
     uint64_t least;
     if (K <= kFewTop && !single) {
@@ -357,8 +420,9 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
         __syncthreads();
         least = kth;
     }
-    // Groups of those threads that are no worse, behind the maxima; of them the K best.
-    uint64_t* list = reinterpret_cast<uint64_t*>(groups + (n_groups + 1) / 2 * 2);
+    if (tid == 0) wave_sums[0] = {r.high, log_z, 0.0f};
+    // Groups of those threads that are no worse, behind the maxima. Usually few of their elements are no worse than the K-th thread's best,
+    // and those are ranked at once; where many are, as in rows of equal ones, first the K best groups are found.
     int32_t kept = min(n_groups, K);
     if (!single) {
         if (mine >= least && mine)
@@ -368,6 +432,20 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
             });
         __syncthreads();
         const int32_t listed = counts[0];
+        log_z = wave_sums[0].z;
+        for (int32_t i = tid; i < listed * kGroup; i += THREADS) {
+            const int32_t q = ~static_cast<uint32_t>(list[i / kGroup]), e = first_of(q) + i % kGroup;
+            if (e >= end_of(q)) continue;
+            const uint32_t o = order_of(static_cast<float>(row[e]));
+            if (o < least >> 32) continue;
+            const int32_t at = atomicAdd(&counts[2], 1u);
+            if (at < kMostTop * kGroup) keys[at] = key_of(o, begin + e);
+        }
+        __syncthreads();
+        if (counts[2] <= kMostTop * kGroup) {
+            rank_and_write(counts[2]);
+            return;
+        }
         kept = min(listed, K);
         for (int32_t i = tid; i < listed; i += THREADS) {
             const uint64_t k = list[i];
@@ -376,7 +454,6 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
             if (better < K) picked_groups[better] = ~static_cast<uint32_t>(k);
         }
     }
-    if (tid == 0) wave_sums[0] = {r.high, log_z, 0.0f};
     __syncthreads();
     log_z = wave_sums[0].z;
     // Their elements that are no worse than the K-th group's largest, wherever that lies in it; of those the K best.
@@ -389,18 +466,7 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
         if (k >= bar) keys[atomicAdd(&counts[1], 1u)] = k;
     }
     __syncthreads();
-    const int32_t found = counts[1];
-    uint64_t* best = a.best ? a.best + (a.row0 * a.parts + blockIdx.x) * K : nullptr;
-    for (int32_t i = tid; i < found; i += THREADS) {
-        const uint64_t k = keys[i];
-        int32_t better = 0;
-        for (int32_t j = 0; j < found; ++j) better += keys[j] > k;
-        if (better >= K) continue;
-        if (best) best[better] = k;
-        else write_top(a, t, better, k, r.high, log_z);
-    }
-    if (best)  // a part of fewer elements
-        for (int32_t i = n + tid; i < K; i += THREADS) best[i] = 0;
+    rank_and_write(counts[1]);
 }
 
 // A wave joins the parts of a row, their lists in shared memory unless there are too many.
@@ -628,13 +694,14 @@ extern "C" ld_status ld_token_logprob(const void* logits, int64_t T, int32_t V, 
     const int32_t threads = sp.narrow ? kNarrow : kWide;
     // maxima of the groups, with one more where rows do not begin at a boundary, and the list of those that `top` threads hold
     const int32_t n_groups = sp.part / kGroup + 2, of_thread = (n_groups + threads - 1) / threads + 1;
-    const size_t shared = top ? (n_groups + 1) / 2 * 2 * sizeof(float) + static_cast<size_t>(n_groups < top * of_thread ? n_groups : top * of_thread) * sizeof(uint64_t) : 0;
+    const int32_t listed = n_groups < top * of_thread ? n_groups : top * of_thread;
+    const size_t shared = top ? (n_groups + 1) / 2 * 2 * sizeof(float) + listed * sizeof(uint64_t) : 0;
     const size_t join_shared = sp.parts * top <= kJoinHeld ? static_cast<size_t>(sp.parts) * top * sizeof(uint64_t) : 0;
     const int64_t most = ld_workgroups(static_cast<int64_t>(1) << 40, threads) / sp.parts;  // rows of a launch
     for (int64_t t = 0; t < T; t += most) {
         const int64_t rows = T - t < most ? T - t : most;
         const ScoreArgs a = {logits, ids, logprob, entropy, stats, top_ids, top_logprob, sums, best, stride, t,
-                             V, sp.part, sp.parts, top, scale, id_dtype == LD_I64};
+                             V, sp.part, sp.parts, top, scale, id_dtype == LD_I64, listed};
         const dim3 grid(static_cast<uint32_t>(rows * sp.parts));
         ld_with_type(dtype, [&](auto type) {
             const auto launch = [&](auto wide, auto with_entropy, auto with_top) {

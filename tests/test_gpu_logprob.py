@@ -166,19 +166,35 @@ def test_many_rows(T, V, top):
     check(make(T, V, BF16, g), make_ids(T, V, g), 1.3, top)
 
 
-@pytest.mark.parametrize("T", [3, 1100])
-@pytest.mark.parametrize("kind", ["equal", "ascending", "descending", "two", "zeros", "one thread", "peaked", "lowest", "huge", "far mask"])
-def test_rows_that_sorting_and_exponentials_find_hard(kind, T):
-    print(f"[score] {kind} T={T}", flush=True)
-    g, V = gen(7), 6001
+HARD = ["equal", "ascending", "descending", "two", "zeros", "one thread", "peaked", "lowest", "huge", "far mask"]
+
+
+def hard_rows(kind, T, V, g):
     j = torch.arange(V, dtype=torch.float64)
     row = {"equal": torch.full((V,), -3.25, dtype=torch.float64), "ascending": j * 2.0 ** -6, "descending": -j * 2.0 ** -6,
            "two": (j % 2) * 4.0, "zeros": torch.where(j % 3 == 0, -0.0, 0.0), "one thread": (j % 2048 < 8) * 5.0 + torch.rand(V, generator=g),
-           "peaked": torch.where(j == 4444, 90.0, -j * 1e-3), "lowest": torch.full((V,), torch.finfo(F32).min, dtype=torch.float64),
-           "huge": torch.where(j > 5990, 3.0e38, -3.0e38), "far mask": torch.where(j % 5 == 1, torch.randn(V, generator=g).double(), -1e9)}[kind]
+           "peaked": torch.where(j == V * 4444 // 6001, 90.0, -j * 1e-3), "lowest": torch.full((V,), torch.finfo(F32).min, dtype=torch.float64),
+           "huge": torch.where(j > V - 11, 3.0e38, -3.0e38), "far mask": torch.where(j % 5 == 1, torch.randn(V, generator=g).double(), -1e9)}[kind]
     x = row.to(F32).repeat(T, 1)
     x[T // 2] = x[T // 2].roll(1234)
+    return x
+
+
+@pytest.mark.parametrize("T", [3, 1100])
+@pytest.mark.parametrize("kind", HARD)
+def test_rows_that_sorting_and_exponentials_find_hard(kind, T):
+    print(f"[score] {kind} T={T}", flush=True)
+    g, V = gen(7), 6001
+    x = hard_rows(kind, T, V, g)
     check(x, make_ids(T, V, g), 1.0, 64, tag=kind)
+
+
+@pytest.mark.parametrize("T,V,top", [(3, 6001, 1), (3, 70001, 8), (600, 6001, 5), (600, 4001, 8), (600, 4001, 9), (600, 1001, 3), (200, 20011, 33)])
+@pytest.mark.parametrize("kind", HARD)
+def test_few_alternatives_of_hard_rows(kind, T, V, top):
+    print(f"[score] {kind} T={T} V={V} top={top}", flush=True)
+    g = gen(T + V)
+    check(hard_rows(kind, T, V, g), make_ids(T, V, g), 1.0, top, tag=kind)
 
 
 @pytest.mark.parametrize("T,V", [(4, 300), (1200, 300), (4, 9001), (1100, 9001)])
