@@ -624,7 +624,8 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
  *   w, m       host arrays of n_mats dev pointers, fp32 [rows][cols] contiguous, in/out; no two
  *              overlap
  *   grad       host array of W n_mats dev pointers, gradient t of matrix i at [t n_mats + i],
- *              [rows][cols] contiguous elements of `dtype`
+ *              [rows][cols] contiguous elements of `dtype`; the same one may stand in several
+ *              places, and overlaps no w and no m
  *   scale      host [n_mats] fp32, or NULL: sqrt(max(1, rows / cols))
  *   0 <= W <= LD_MAX_WINDOW
  *   workspace  dev, 256-byte aligned, ld_merge_dense_muon_workspace() bytes, or fewer, as above

@@ -16,11 +16,10 @@ namespace {
 
 constexpr int kGroup = 8;                      // elements side by side that a thread takes at a time
 constexpr int kWide = 256, kNarrow = 64;       // threads of a workgroup: one row, or a part of one
-// Up to here a row is one wave's, where there are at least as many rows as would fill the chip with waves: it meets no barrier (five
-// alternatives of 16384 x 1000 in bf16 19 us, by workgroups of 256 threads 76; x 4096 38 and 60; x 8000 71 and 82, but fp32 98 and
-// 90; 1000 x 4096 7.8 and 8.3, 512 x 4096 7.4 and 7.0, 1000 x 8000 11.4 and 10.4).
+// Up to here a row that is not split is one wave's: it meets no barrier (five alternatives of 16384 x 1000 in bf16 19 us, by workgroups of
+// 256 threads 76; 16384 x 4096 38 and 60, 1000 x 4096 7.8 and 8.3, 256 x 4096 7.2 and 6.6; 16384 x 8000 71 and 82, but in fp32 98
+// and 90, and 1000 x 8000 11.4 and 10.4).
 constexpr int32_t kNarrowElems = 4096;
-constexpr int64_t kNarrowRows = 512;
 constexpr int32_t kMostPart = 65536;           // elements of a part: 32 KB of group maxima for the alternatives
 constexpr int32_t kPartStep = kWide * kGroup;
 // Rows are split until there are as many, where they are fewer than half: by 256, 512 and 1024, us with five alternatives of 50257: 8 rows 10.2,
@@ -648,7 +647,6 @@ struct Split {
     bool narrow;
 };
 Split split_of(int64_t T, int32_t V) {
-    if (V <= kNarrowElems && T >= kNarrowRows) return {V, 1, true};
     const int32_t most = (V + kPartStep - 1) / kPartStep, least = (V + kMostPart - 1) / kMostPart;
     int64_t parts = T > 0 && T < kWorkgroups / 2 ? (kWorkgroups + T - 1) / T : 1;
     parts = parts > most ? most : parts < least ? least : parts;
