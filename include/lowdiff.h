@@ -545,8 +545,9 @@ ld_status ld_embed_grad(const void* dout, int64_t dout_stride, int32_t dtype,
  * in 32 bits.  Few rows are split, and L, and the entropy, may then differ in their last bits
  * from what the same row has in a call of more; the same call gives the same bits.  Masked tokens are minus infinity: their probability is 0.  A row in which
  * nothing is left (all minus infinity) has M = -inf, L = 0, entropy 0 and log probabilities of
- * -inf.  An infinite logit or a NaN makes a row's L, entropy and log probabilities NaN; a NaN
- * counts as the largest of all logits among the alternatives.
+ * -inf.  An infinite logit or a NaN makes a row's L, entropy and log probabilities NaN, and its
+ * gradient (M passes NaN over, and is NaN where nothing else is left: such a row is not taken for
+ * a masked one).  A NaN counts as the largest of all logits among the alternatives.
  *
  *   logits     dev [T] rows of V elements of `dtype`, stride >= 0 elements apart
  *   ids        dev [T] of `id_dtype` (LD_I32 or LD_I64); NULL together with logprob

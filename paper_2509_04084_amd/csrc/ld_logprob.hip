@@ -98,6 +98,10 @@ __device__ __forceinline__ Sums moved(Sums a, float high, float c) {
     return {high, a.z == 0.0f ? 0.0f : a.z * f, a.z == 0.0f || f == 0.0f ? 0.0f : f * __fmaf_rn(d, a.z, a.s)};
 }
 
+// A row's sums, of all its parts. Maxima pass NaN over, sums do not: a row of nothing but NaN and minus infinities has a sum that is NaN and is
+// no row in which nothing is left (whose sum is 0), and so that none takes it for one, its largest logit is NaN as well.
+__device__ __forceinline__ Sums whole_row(Sums r) { return {r.z != r.z && r.high == -__builtin_huge_valf() ? r.z : r.high, r.z, r.s}; }
+
 // What a row's sums say, written by one thread.
 __device__ __forceinline__ float finish(const ScoreArgs& a, int64_t t, Sums r, float picked, bool inside) {
     const bool empty = r.high == -__builtin_huge_valf();
@@ -304,13 +308,14 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
         r.z = r.s = 0.0f;
         for (int w = 0; w < kWaves; ++w) r.z += wave_sums[w].z, r.s += wave_sums[w].s;
     }
+    const Sums row_sums = whole_row(r);
     float log_z = 0.0f;
     if (a.sums) {
         if (tid == 0) a.sums[blockIdx.x + a.row0 * a.parts] = make_float4(r.high, r.z, r.s, 0.0f);
     } else if (tid == 0) {
         bool inside;
         const float x = picked_of<DT>(a, t, inside);
-        log_z = finish(a, t, r, x, inside);
+        log_z = finish(a, t, row_sums, x, inside);
     }
     if (!TOP) return;
 
@@ -341,7 +346,7 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
             for (int32_t j = 0; j < many; ++j) better += keys[j] > k;
             if (better >= K) continue;
             if (best) best[better] = k;
-            else write_top(a, t, better, k, r.high, log_z);
+            else write_top(a, t, better, k, row_sums.high, log_z);
         }
         if (best)  // a part of fewer elements
             for (int32_t i = n + tid; i < K; i += THREADS) best[i] = 0;
@@ -511,7 +516,7 @@ __global__ __launch_bounds__(LD_WAVE) void k_score_join(ScoreArgs a) {
         const Sums r = moved({part[i].x, part[i].y, part[i].z}, most, c);
         z += r.z, s += r.s;
     }
-    const Sums r = {most, wave_sum(z), wave_sum(s)};
+    const Sums r = whole_row({most, wave_sum(z), wave_sum(s)});
     float log_z = 0.0f;
     if (lane == 0) log_z = finish(a, t, r, picked, inside);
     if (a.top == 0) return;
@@ -543,7 +548,7 @@ __global__ __launch_bounds__(LD_WAVE) void k_score_join(ScoreArgs a) {
                 next[i] = ++used[i] < a.top ? entry(p * a.top + used[i]) : 0;
             }
     }
-    if (lane < a.top) write_top(a, t, lane, kept, most, log_z);
+    if (lane < a.top) write_top(a, t, lane, kept, r.high, log_z);
 }
 
 struct GradArgs {
