@@ -92,11 +92,12 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 struct Sums {
     float high, z, s;
 };
-// The same against another, not lower, reference. A sum of nothing stays one, also where that lies an infinity higher.
-__device__ __forceinline__ Sums moved(Sums a, float high, float c) {
-    const float d = (a.high - high) * c, f = __builtin_amdgcn_exp2f(d);
+// The same against another reference, by d <= 0 powers of two. A sum of nothing stays one, also where that lies an infinity higher.
+__device__ __forceinline__ Sums moved_by(Sums a, float high, float d) {
+    const float f = __builtin_amdgcn_exp2f(d);
     return {high, a.z == 0.0f ? 0.0f : a.z * f, a.z == 0.0f || f == 0.0f ? 0.0f : f * __fmaf_rn(d, a.z, a.s)};
 }
+__device__ __forceinline__ Sums moved(Sums a, float high, float c) { return moved_by(a, high, (a.high - high) * c); }
 
 // A row's sums, of all its parts. Maxima pass NaN over, sums do not: a row of nothing but NaN and minus infinities has a sum that is NaN and is
 // no row in which nothing is left (whose sum is 0), and so that none takes it for one, its largest logit is NaN as well.
@@ -255,8 +256,11 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
         }
         high = fmaxf(high, m);
         if (m > limit) {
-            const Sums r = moved({ref, z, s}, m, c);
-            ref = m, ref_c = m * c, limit = m + far, z = r.z, s = r.s;
+            // by what the exponents were taken against, each rounded once: rows around 1e5 were 1e-4 off where the difference of the
+            // references themselves moved them, those around 3e5 2e-3
+            const float now = m * c;
+            const Sums r = moved_by({ref, z, s}, m, ref_c - now);
+            ref = m, ref_c = now, limit = m + far, z = r.z, s = r.s;
         }
 #pragma unroll
         for (int e = 0; e < kGroup; ++e) {
@@ -278,7 +282,7 @@ __global__ __launch_bounds__(THREADS) void k_score(ScoreArgs a) {
     for (; g < whole; g += THREADS) take(R::load(body + g * kGroup), headed + g);
     if (g < n_body) take(R::load_some(body + g * kGroup, rest), headed + g);
 
-    // What rounding ref_c has moved all exponents by.
+    // What rounding the last ref_c has moved all exponents by.
     if (ref != lowest) {
         const float off = -__fmaf_rn(ref, c, -ref_c), f = __builtin_amdgcn_exp2f(off);
         s = f * __fmaf_rn(off, z, s);
