@@ -875,6 +875,13 @@ def _sides(mats: Sequence[torch.Tensor], name: str) -> Tuple[np.ndarray, np.ndar
     return np.ascontiguousarray(both[:, 0]), np.ascontiguousarray(both[:, 1])
 
 
+def _apart(name: str, written: Sequence[int], read: Sequence[int]) -> None:
+    """Refuses tensors, by their addresses, of which one is written for two matrices, or written for one and read for another."""
+    once = set(written)
+    if len(once) < len(written) or not once.isdisjoint(read):
+        raise ValueError(f"{name}: a tensor stands for two matrices")
+
+
 def _coefficients(coeffs, steps: int) -> Optional[np.ndarray]:
     """Three a step: from None (the usual ones), three for all steps, or three for each."""
     if coeffs is None:
@@ -925,10 +932,8 @@ def ld_orthogonalize(mats: Sequence[torch.Tensor], outs: Optional[Sequence[torch
         dp[i], _, ds[i] = _rows(t, "outs", written=True)
         if dp[i] == sp[i] and t.numel() and (t.dtype != first.dtype or ds[i] != ss[i]):
             raise ValueError("outs: in place a matrix keeps its type and stride")
-    source = {int(p): i for i, p in enumerate(sp) if mats[i].numel()}
-    written = [int(p) for i, p in enumerate(dp) if mats[i].numel()]
-    if len(set(written)) < len(written) or any(int(p) in source and dp[i] != sp[i] for i, p in enumerate(dp) if mats[i].numel()):
-        raise ValueError("outs: a tensor stands for two matrices")
+    kept = [i for i, t in enumerate(mats) if t.numel()]
+    _apart("outs", [int(dp[i]) for i in kept], [int(sp[i]) for i in kept if sp[i] != dp[i]])
     if workspace is None and (need := lib.ld_orthogonalize_workspace(_hp(rows), _hp(cols), n)) > 0:
         workspace = _scratch(need, first.device, stream)
     st = lib.ld_orthogonalize(_hp(sp), _hp(ss), _hp(dp), _hp(ds), _hp(rows), _hp(cols), n, code, _elem(outs[0], "outs"), int(steps),
@@ -971,9 +976,9 @@ def ld_merge_dense_muon(ws: Sequence[torch.Tensor], ms: Sequence[torch.Tensor], 
     _one_device(ws[0], (workspace,), w, m, g)
     wp, mp, gp = w.checked("ws"), m.checked("ms"), g.checked("grads")
     _on_device_of(stream, ws[0])
-    written = [a for p in (wp, mp) for a, k in zip(np.frombuffer(p, np.uint64).tolist(), w.numel().tolist()) if k]
-    if len(set(written)) < len(written):
-        raise ValueError("ws, ms: a tensor stands for two matrices")
+    kept = [i for i, k in enumerate(w.numel().tolist()) if k]
+    at = [np.frombuffer(p, np.uint64).reshape(-1, n)[:, kept].ravel().tolist() for p in (wp, mp, gp)]
+    _apart("ws, ms", at[0] + at[1], at[2])
     factor = None
     if scale is not None:
         factor = np.ascontiguousarray(np.broadcast_to(np.asarray(scale, dtype=np.float32), (n,)))
