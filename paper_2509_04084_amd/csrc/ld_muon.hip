@@ -7,7 +7,7 @@
 // 22 bits, and a product is three MFMA products: hh + hl + lh, summed in 32 bits. Values are scaled by powers of two that the
 // coefficients bound. A run of steps works on the Gram matrix alone: with P = a I + b A + c A^2, A' = P A P and Q' = P Q, all of m by
 // m, symmetric and commuting, so that half of each is computed and mirrored; X is read for its Gram matrix and multiplied by Q once a
-// run (ld_muon_shape.h says when a run ends, and why): 6 m^2 n + 14 m^3 products' operations for five steps of a wide matrix instead of
+// run (ld_muon_shape.h says when a run ends, and why): 9 m^2 n + 11 m^3 products' operations for five steps of a wide matrix instead of
 // 15 m^2 n + 5 m^3 (symmetric halves there too). Matrices of up to 64 rows go a way of their own, in 64 bits.
 //
 // In memory a matrix lies as blocks of 32 columns, in each of them row after row: 32 upper halves, 32 lower halves, 128 bytes, whose eight
@@ -937,8 +937,8 @@ int64_t scratch_of(int64_t rows, int64_t cols) {
     return (ld_muon_scratch(static_cast<int32_t>(m), static_cast<int32_t>(n)) + 255) / 256 * 256;
 }
 
-// Appends a problem; whether it still has room. The first always has.
-bool append(Batch& b, int64_t& used, char* scratch, int64_t room, int64_t rows, int64_t cols) {
+// Appends a problem, whose result goes to out_type; whether it still has room. The first always has.
+bool append(Batch& b, int64_t& used, char* scratch, int64_t room, int64_t rows, int64_t cols, int32_t out_type) {
     const int64_t need = scratch_of(rows, cols);
     if (b.count == kMost || (b.count > 0 && used + need > room)) return false;
     const int32_t i = b.count++;
@@ -946,7 +946,7 @@ bool append(Batch& b, int64_t& used, char* scratch, int64_t room, int64_t rows, 
     b.flipped[i] = rows > cols;
     b.m[i] = static_cast<int32_t>(rows > cols ? cols : rows);
     b.n[i] = static_cast<int32_t>(rows > cols ? rows : cols);
-    b.kind[i] = b.m[i] <= kMuonFewSide ? kMuonFew : ld_muon_kind(b.m[i], b.n[i]);
+    b.kind[i] = b.m[i] <= kMuonFewSide ? kMuonFew : ld_muon_kind(b.m[i], b.n[i], out_type != LD_F32);
     used += need;
     return true;
 }
@@ -1186,7 +1186,7 @@ extern "C" ld_status ld_orthogonalize(const void* const* src, const int64_t* src
         int64_t used = 0;
         for (; i < n_mats; ++i) {
             if (rows[i] == 0 || cols[i] == 0) continue;
-            if (!append(b, used, scratch, room_bytes, rows[i], cols[i])) break;
+            if (!append(b, used, scratch, room_bytes, rows[i], cols[i], out_dtype)) break;
             source.src[b.count - 1] = src[i], source.stride[b.count - 1] = src_stride ? src_stride[i] : cols[i];
             out.out[b.count - 1] = dst[i], out.stride[b.count - 1] = dst_stride ? dst_stride[i] : cols[i];
         }
@@ -1248,7 +1248,7 @@ extern "C" ld_status ld_merge_dense_muon(float* const* w, float* const* m, const
                 continue;
             }
             const int32_t from = t;
-            for (; t < W && (room = append(b, used, scratch, room_bytes, rows[i], cols[i])); ++t) {
+            for (; t < W && (room = append(b, used, scratch, room_bytes, rows[i], cols[i], LD_F32)); ++t) {
                 const int32_t k = b.count - 1;
                 mom.grad[k] = grad[static_cast<int64_t>(t) * n_mats + i];
                 source.stride[k] = out.stride[k] = cols[i];

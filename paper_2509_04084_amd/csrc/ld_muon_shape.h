@@ -56,17 +56,21 @@ inline bool ld_muon_bounds(LdMuonBounds& m, int32_t steps, const float* coeff) {
 
 // A run of steps works on one Gram matrix; X is multiplied by what they amount to, and its Gram matrix formed anew, between runs. The
 // Gram matrix loses directions of small singular values, the more the further a run grows them (each usual step 3.4 times), and
-// a matrix that is about square has more of those than a wide one, and one of many rows, whose values are scaled to a norm of 1 in all,
-// smaller ones. So a run of a wide matrix of up to kMuonThreeSide rows (kind 2) ends at three steps or 48 times,
-// counted from the last step on, of a less wide or a larger one (1) at two steps or 16 times, counted from the first, and one that is about square
-// (0), to which a run's matrices of m x m are no smaller than X, has runs of one step: 2 + 3, 2 + 2 + 1 and five times 1 of five usual
-// steps, 6 m^2 n + 14 m^3, 9 m^2 n + 11 m^3 and 15 m^2 n + 5 m^3 operations of products, in 17, 18 and 15 launches. Errors against 64 bits
-// (relative, Frobenius) of products in 32 bits in the order of the formula, and of these three: 768 x 768 2.3e-6, 4.3e-6, 1.9e-6, 1.7e-6;
-// 1000 x 2000 2.9e-6, 2.9e-6, 2.3e-6, 2.1e-6; 1600 x 6400 4.0e-6, 2.6e-6, 2.9e-6, 2.5e-6; 5120 x 2048 with rows of
-// different scales 4.4e-6, 5.4e-6, 3.3e-6; 11008 x 4096 of them 4.8e-6, 6.6e-6, 3.3e-6, 3.3e-6. Up to kMuonFewSide rows a matrix goes another
-// way, in 64 bits (kMuonFew).
+// a matrix that is about square has more of those than a wide one. So a run of a wide matrix (kind 1) ends at two steps or 16 times,
+// counted from the first, and one that is about square (0), to which a run's matrices of m x m are no smaller than X, has runs of one
+// step. Only results that are rounded to 16 bits, of matrices wider still and of up to kMuonThreeSide rows (2), come by runs of three steps
+// or 48 times, counted from the last on. Five usual steps as five times 1, 2 + 2 + 1 and 2 + 3 take 15 m^2 n + 5 m^3, 9 m^2 n + 11 m^3 and
+// 6 m^2 n + 14 m^3 operations of products, in 15, 18 and 17 launches; 768 x 2304 272, 262 and 243 us, 1600 x 4800 849, 716 and 625,
+// 4096 x 11008 by one and two 9660 and 7990. Errors against 64 bits (relative, Frobenius) of products in 32 bits in the order of the formula, and of runs
+// of one, two and three: 768 x 2304 3.6e-6, 2.6e-6, 2.7e-6, 2.6e-6; 1024 x 1024 3.1e-6, and 2.0e-6 by one. Where the sizes of the
+// rows spread over two decades, runs of three lose what 32 bits hold (16 bits are rounded by 2e-4 and more): 2304 x 768 1.9e-6, 1.5e-6, 2.5e-6,
+// 1.6e-5; 5120 x 2048 3.0e-6, 2.1e-6, 3.5e-6, 2.5e-5; 6400 x 1600 3.7e-6, 2.3e-6, 4.2e-6, 2.5e-5. Up to kMuonFewSide rows a matrix goes
+// another way, in 64 bits (kMuonFew).
 constexpr int32_t kMuonKinds = 4, kMuonFew = 3, kMuonFewSide = 64, kMuonThreeSide = 2048;
-inline int32_t ld_muon_kind(int64_t m, int64_t n) { return 2 * n >= 5 * m && m <= kMuonThreeSide ? 2 : 4 * n >= 5 * m ? 1 : 0; }
+// narrow: the result goes to 16 bits
+inline int32_t ld_muon_kind(int64_t m, int64_t n, bool narrow = true) {
+    return 2 * n >= 5 * m && m <= kMuonThreeSide && narrow ? 2 : 4 * n >= 5 * m ? 1 : 0;
+}
 // First steps of the runs, and behind them the number of steps; returns the number of runs.
 inline int32_t ld_muon_runs(const LdMuonBounds& b, int32_t steps, int32_t kind, int32_t* begin) {
     const bool wide = kind == 2;

@@ -904,7 +904,7 @@ def ld_orthogonalize(mats: Sequence[torch.Tensor], outs: Optional[Sequence[torch
                      eps: float = 1e-7, out_dtype: Optional[torch.dtype] = None, workspace: Optional[torch.Tensor] = None,
                      stream=None) -> List[torch.Tensor]:
     """Every matrix's nearest orthogonal one, about: `steps` Newton-Schulz steps of X <- (a I + b X X^T + c (X X^T)^2) X from
-    X = U / (|U|_F + eps), as precise as products in float32. Into `outs` (which may be the matrices themselves) or new tensors
+    X = U / (|U|_F + eps), about as precise as products in float32. Into `outs` (which may be the matrices themselves) or new tensors
     of type `out_dtype` (theirs unless given). Matrices of one call share a type, their shapes are any, and rows may have any stride.
     A matrix's result does not depend on the others of the call. `coeffs`: (a, b, c), or three for every step; those that
     let singular values grow too far are refused."""
