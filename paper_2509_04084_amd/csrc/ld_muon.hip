@@ -54,6 +54,15 @@ __device__ __forceinline__ char* buffer_of(const Batch& b, int32_t i, int32_t wh
     const int64_t large = m * n * 4 + slack, small = m * m * 4 + slack;
     return b.base[i] + (which < 3 ? which * large : 3 * large + (which - 3) * small);
 }
+// A matrix whose norm is far below eps begins as small as that, and halves would not hold it. So X lies in memory times 2^lift, the part of
+// (norm + eps) / norm that is a power of two, or less of it where steps have grown X since (Plan::drop): 0 where eps is below the norm. It is kept behind the
+// last buffer, in the room of rows that nothing writes.
+constexpr int32_t kMostLift = 96;  // 2^-96 and the scales of halves are no subnormals
+__device__ __forceinline__ int32_t* lift_of(const Batch& b, int32_t i) {
+    const int64_t m = padded(b.m[i]);
+    return reinterpret_cast<int32_t*>(buffer_of(b, i, kQ1) + m * m * 4 + 3 * kMuonPad * kMuonRowBytes) - 1;
+}
+__device__ __forceinline__ int32_t left_of(int32_t lift, int32_t drop) { return lift > drop ? lift - drop : 0; }
 // Tiles over a side: all of its padding is written too.
 __host__ __device__ __forceinline__ int32_t tiles_of(int64_t side, int32_t tile) { return static_cast<int32_t>((side + tile - 1) / tile); }
 // Where the eight upper halves of row r, columns [8 c, 8 c + 8) lie, in bytes; the lower ones are 64 bytes on, permuted alike.
@@ -93,6 +102,8 @@ struct Plan {
     float inv;             // 1 / scale of the operands' product
     float scale[2];        // of what is kept
     float ca, cb, cc;      // coefficients, cb times 1 / scale of A
+    int32_t drop;          // powers of two by which X may have grown since it was laid out, of the X that is read
+    int32_t out_drop;      // and of the X that is written; where it goes nothing is left of the lift: kMostLift
 };
 struct Plans {
     Plan of[kMuonKinds];
@@ -299,6 +310,7 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_symmetric(Batch batch,
     ld_muon_lower_tile(tile, side, T::BAND, tr, tc);
     const int32_t m = batch.m[i], r0 = tr * T::SIDE, c0 = tc * T::SIDE;
     const int64_t rows = padded(m);
+    const float inv = a.long_sum ? ldexpf(a.inv, -2 * left_of(*lift_of(batch, i), a.drop)) : a.inv;
     f32x16 acc[T::R][T::C] = {};
     multiply<T>(buffer_of(batch, i, prod.left) + r0 * kMuonRowBytes, rows, buffer_of(batch, i, prod.right) + c0 * kMuonRowBytes, rows,
                 static_cast<int32_t>((a.long_sum ? padded(batch.n[i]) : rows) / kMuonBlock), shared, acc);
@@ -321,7 +333,7 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_symmetric(Batch batch,
                     __builtin_amdgcn_global_load_lds((global_ptr)(gram + ((c0 / kMuonBlock + k) * rows + h0 + 8 * n) * kMuonRowBytes + ld_lane() * 16),
                                                      (shared_ptr)(held + (k * T::ROWS + 8 * n) * kMuonRowBytes), 16, 0, 0);
         }
-        lay_out<T>(acc, h, a.inv, sums, S, a.poly != 0);
+        lay_out<T>(acc, h, inv, sums, S, a.poly != 0);
 #pragma unroll 2
         for (int p = 0; p < WayOut<T>::EACH; ++p) {
             int32_t r, c;
@@ -382,6 +394,8 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Pla
     ld_muon_tile(tile, down, tiles_of(padded(n), T::SIDE), T::BAND, tr, tc);
     const int32_t r0 = tr * T::SIDE, c0 = tc * T::SIDE;
     const int64_t rows = padded(m), cols = padded(n);
+    const int32_t lift = *lift_of(batch, i);
+    const float inv = ldexpf(FINAL ? a.inv : a.inv * a.scale[0], left_of(lift, a.out_drop) - left_of(lift, a.drop));
     f32x16 acc[T::R][T::C] = {};
     multiply<T>(buffer_of(batch, i, a.prod[0].left) + r0 * kMuonRowBytes, rows, buffer_of(batch, i, a.prod[0].right) + c0 * kMuonRowBytes, cols,
                 static_cast<int32_t>(rows / kMuonBlock), shared, acc);
@@ -413,7 +427,7 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Pla
         if (FINAL && batch.flipped[i]) {
             // an odd stride, and the lanes along the columns that are rows of the update: what they write lies side by side
             constexpr int kOdd = T::SIDE + 1, kDeep = T::ROWS / 8;
-            lay_out<T>(acc, h, a.inv, sums, kOdd, false);
+            lay_out<T>(acc, h, inv, sums, kOdd, false);
             for (int32_t p = threadIdx.x; p < kDeep * T::SIDE; p += T::THREADS) {
                 const int32_t c = p / kDeep, r = p % kDeep * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
                 f32x8 x;
@@ -423,7 +437,7 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES) void k_apply(Batch batch, Pla
             }
             continue;
         }
-        lay_out<T>(acc, h, FINAL ? a.inv : a.inv * a.scale[0], sums, S, false);
+        lay_out<T>(acc, h, inv, sums, S, false);
         if (FINAL) {
             for (int32_t p = threadIdx.x; p < T::ROWS * kPieces; p += T::THREADS) {
                 const int32_t r = p / kPieces, c = p % kPieces * 8, ri = r0 + T::ROWS * h + r, ci = c0 + c;
@@ -564,7 +578,10 @@ __global__ __launch_bounds__(kThreads) void k_lay_out(Batch b, Source s, float s
     const int32_t parts = sum_parts(static_cast<int64_t>(rows) * cols);
     const double total = block_sum(static_cast<int32_t>(threadIdx.x) < parts ? s.sums[i * kSumParts + threadIdx.x] : 0.0, sh);
     const double norm = sqrt(total);
-    const double f = norm == 0.0 ? 0.0 : static_cast<double>(scale) / (norm + static_cast<double>(s.eps));
+    const double eps = static_cast<double>(s.eps), ratio = (norm + eps) / norm;
+    const int32_t lift = ratio >= 2.0 && norm > 0.0 ? min(ilogb(ratio), kMostLift) : 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *lift_of(b, i) = lift;
+    const double f = norm == 0.0 ? 0.0 : ldexp(static_cast<double>(scale), lift) / (norm + eps);
     char* straight = buffer_of(b, i, b.flipped[i] ? kXT : kX);
     char* turned = buffer_of(b, i, b.flipped[i] ? kX : kXT);
     const int64_t all_rows = padded(rows), all_cols = padded(cols);
@@ -990,13 +1007,18 @@ void program_of(const Polynomial& p, int32_t kind, Program& out) {
     const int32_t runs = ld_muon_runs(b, p.steps, kind, begin);
     int32_t xt = kXT, other = kYT;
     out.count = 0;
+    // X before a step is no larger than its bound, and than its first norm times what the steps before may have grown it by.
+    const auto drop_of = [&](int32_t step) {
+        const double grown = step == 0 ? 1.0 : ld_muon_grown(b, 0, step - 1);
+        return step == 0 || grown <= b.x[step] ? 0 : static_cast<int32_t>(fmin(ceil(log2(grown / b.x[step])), kMostLift));
+    };
     for (int32_t run = 0; run < runs; ++run) {
         const int32_t from = begin[run], to = begin[run + 1];
         const float sx = scale(b.x[from]);
         float sa = scale(b.x[from] * b.x[from]), sq = 0.0f;
         Plan gram = {};
         gram.prod[0] = {kX, kX, kA, 0};
-        gram.products = 1, gram.long_sum = 1, gram.inv = 1.0f / (sx * sx), gram.scale[0] = sa;
+        gram.products = 1, gram.long_sum = 1, gram.inv = 1.0f / (sx * sx), gram.scale[0] = sa, gram.drop = drop_of(from);
         out.plan[out.count++] = gram;
         int32_t q = kP, free_q = kQ0;
         for (int32_t step = from; step < to; ++step) {
@@ -1036,9 +1058,9 @@ void program_of(const Polynomial& p, int32_t kind, Program& out) {
         }
         Plan a = {};
         a.prod[0] = {q, xt, kX, other};
-        a.products = 1, a.apply = 1, a.inv = 1.0f / (sq * sx);
-        if (run + 1 == runs) a.final = 1;
-        else a.scale[0] = scale(b.x[to]);
+        a.products = 1, a.apply = 1, a.inv = 1.0f / (sq * sx), a.drop = drop_of(from);
+        if (run + 1 == runs) a.final = 1, a.out_drop = kMostLift;
+        else a.scale[0] = scale(b.x[to]), a.out_drop = drop_of(to);
         out.plan[out.count++] = a;
         const int32_t was = xt;
         xt = other, other = was;
