@@ -80,10 +80,6 @@ __device__ __forceinline__ void store_split(char* to, int64_t rows, int64_t r, i
     *reinterpret_cast<half8*>(to + piece_at(rows, r, c, 0)) = h;
     *reinterpret_cast<half8*>(to + piece_at(rows, r, c, 1)) = l;
 }
-__device__ __forceinline__ f32x8 load_split(const char* from, int64_t rows, int64_t r, int64_t c) {
-    const half8 h = *reinterpret_cast<const half8*>(from + piece_at(rows, r, c, 0)), l = *reinterpret_cast<const half8*>(from + piece_at(rows, r, c, 1));
-    return __builtin_convertvector(h, f32x8) + __builtin_convertvector(l, f32x8);
-}
 
 // ------------------------------------------------------------------------------------------------------------------- products
 
