@@ -595,9 +595,9 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
  * (the steps run on the smaller side: for U with more rows than columns, on its transposed, which
  * is the same map).  Sums are 32 bits wide, operands of products 22 bits (of up to 64 rows or columns
  * everything is in 64 bits), and the result is rounded once to out_dtype; U's squares are summed in 64
- * bits.  Against 64 bits (relative, Frobenius) results in 32 bits are off by 0.3 to 2 times what products in
- * 32 bits in the formula's order are, by up to 3 times where a few rows or columns outweigh the others
- * by far; those in 16 bits by their rounding.  A matrix of zeros stays zeros.  An infinity or a NaN
+ * bits.  Against 64 bits (relative, Frobenius, usual coefficients) results in 32 bits are off by 0.3 to 2
+ * times what products in 32 bits in the formula's order are, by up to 3 times where a few rows or
+ * columns outweigh the others by far; those in 16 bits by their rounding.  A matrix of zeros stays zeros.  An infinity or a NaN
  * anywhere in a matrix makes all of it NaN; other matrices of the call are not touched by it.  What a
  * matrix becomes depends on nothing but itself and out_dtype: not on the others of the call.
  *
@@ -621,9 +621,13 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
  *   m <- fl(mu m + g_t)                                       (one fused multiply-add)
  *   u  = nesterov ? fl(mu m + g_t) : m
  *   w <- fl(fl(w keep) - rate O(u)),  keep = fl(1 - lr weight_decay),  rate = fl(lr scale[i])
- * with O the map above, its result in 32 bits.  One call with W gradients gives the same bits as
- * W calls with one.  An infinity or a NaN in a gradient stays in that momentum and makes all of
- * that matrix NaN, from its step on: gradients are checked (ld_grad_norm) before.
+ * with O the map above, its result in 32 bits.  The gradient goes into the momentum as it is: where a
+ * trainer keeps m <- mu m + (1 - mu) g (and takes mu m + (1 - mu) g once more with nesterov), its momentum
+ * and u are (1 - mu) times these.  O sees no factor but through eps, so the weights agree where eps is small
+ * against the norms; a momentum that is handed over between the two has to be scaled.
+ * One call with W gradients gives the same bits as W calls with one.  An infinity or a NaN in a
+ * gradient stays in that momentum and makes all of that matrix NaN, from its step on: gradients are
+ * checked (ld_grad_norm) before.
  *
  *   w, m       host arrays of n_mats dev pointers, fp32 [rows][cols] contiguous, in/out; no two
  *              overlap

@@ -954,7 +954,8 @@ def ld_merge_dense_muon(ws: Sequence[torch.Tensor], ms: Sequence[torch.Tensor], 
                         coeffs=None, eps: float = 1e-7, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """Replays dense gradients, grads[t][i] of matrix i, as steps of the optimizer that orthogonalises its updates, onto the
     weights ws and momenta ms (float32), in place; with one t it is a training step. Per step: m = momentum * m + g, u = g + momentum * m
-    with nesterov, else m, w = (1 - lr * weight_decay) * w - lr * scale[i] * orthogonalize(u). scale: one number, one for every
+    with nesterov, else m, w = (1 - lr * weight_decay) * w - lr * scale[i] * orthogonalize(u). A trainer that keeps
+    momentum * m + (1 - momentum) * g has (1 - momentum) times this m, and the same updates up to eps. scale: one number, one for every
     matrix, or None: sqrt(max(1, rows / cols)). Gradients share one of the types float32, bfloat16 and float16. Any cut of the
     gradients into calls gives the same bits."""
     lib, n, W = load(), len(ws), len(grads)
