@@ -88,3 +88,24 @@ def test_the_same_call_gives_the_same_bits(shapes):
         got = ld.ld_orthogonalize(us, out_dtype=BF16, workspace=torch.full((need,), fill, dtype=torch.uint8, device=DEV))
         want = want or got
         assert all(same_bits(a, b) for a, b in zip(got, want)), fill
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_matrices_of_flat_buffers(dtype):
+    """Weights, momenta and gradients one behind the other in flat buffers, at any element's alignment, and what lies between them."""
+    shapes = [(100, 301), (7, 33), (301, 100), (1, 50), (129, 129)]
+    sizes, g = [r * c for r, c in shapes], gen(71)
+    at = [sum(sizes[:i]) + 3 * i + 1 for i in range(len(shapes))]  # three elements between two
+    flat = [torch.randn(sum(sizes) + 3 * len(sizes) + 1, generator=g, device=DEV) for _ in range(4)]
+    w, m, grads = flat[0], flat[1], [f.to(dtype) for f in flat[2:]]
+    cut = lambda f: [f[a:a + n].view(s) for a, n, s in zip(at, sizes, shapes)]  # noqa: E731
+    own = [[t.clone() for t in cut(f)] for f in (w, m, *grads)]
+    before = w.clone(), m.clone()
+    ld.ld_merge_dense_muon(cut(w), cut(m), [cut(f) for f in grads], 0.02, weight_decay=0.1)
+    ld.ld_merge_dense_muon(own[0], own[1], own[2:], 0.02, weight_decay=0.1)
+    assert all(same_bits(a, b) for a, b in zip(cut(w) + cut(m), own[0] + own[1]))
+    between = torch.ones(w.numel(), dtype=torch.bool, device=DEV)
+    for a, n in zip(at, sizes):
+        between[a:a + n] = False
+    assert same_bits(w[between], before[0][between]) and same_bits(m[between], before[1][between])
+    assert not any(same_bits(a, b) for a, b in zip(cut(w), cut(before[0])))
