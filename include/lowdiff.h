@@ -596,7 +596,7 @@ ld_status ld_token_logprob_grad(const void* logits, int64_t T, int32_t V, int64_
  * is the same map).  Sums are 32 bits wide, operands of products 22 bits (of up to 64 rows or columns
  * everything is in 64 bits), and the result is rounded once to out_dtype; U's squares are summed in 64
  * bits.  Against 64 bits (relative, Frobenius, usual coefficients) results in 32 bits are off by 0.3 to 2
- * times what products in 32 bits in the formula's order are, by up to 3 times where a few rows or
+ * times what products in 32 bits in the formula's order are, by up to 3.2 times where a few rows or
  * columns outweigh the others by far; those in 16 bits by their rounding.  A matrix of zeros stays zeros.  An infinity or a NaN
  * anywhere in a matrix makes all of it NaN; other matrices of the call are not touched by it.  What a
  * matrix becomes depends on nothing but itself and out_dtype: not on the others of the call.
